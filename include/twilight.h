@@ -70,6 +70,8 @@ extern "C" {
 /* status bits (device word) */
 #define TW_STATUS_UNION_TRUNCATED 1u /* a group's union exceeded union_stride */
 #define TW_STATUS_KEPT_TRUNCATED 2u  /* a head's kept list exceeded kept_stride */
+#define TW_STATUS_POOL_EXHAUSTED 4u  /* no free page was left for an entry, which stays unmapped */
+#define TW_STATUS_PAGE_COUNT 8u      /* a page lost more references than it had (its count stays 0) */
 
 /*
  * Paged KV cache of one layer.  Layouts (all row-major, page = 16 tokens):
@@ -362,6 +364,134 @@ int twilight_sparse_decode_per_head(const twilight_kv_t* kv, const void* q, cons
                                     const int32_t* kept_idx, int32_t kept_stride, void* out, float* lse,
                                     void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * Attention of a sequence's newest tokens: several query tokens per sequence,
+ * each over what it may see of the paged cache (Definition 3.1 without a
+ * pruned set; the verification of drafted tokens, layers with a window,
+ * prefill).  The cache holds the new tokens already (twilight_kquant_append);
+ * seq_lens counts them: with n = seq_lens[b] and N = n_new[b], new token i of
+ * sequence b stands at position n - N + i.
+ *   out = sum_t softmax_t(q.K_t / sqrt(128)) V_t over the visible t
+ * bf16 in and out; scores, softmax statistics and sums in fp32, the weights
+ * rounded to bf16 for their product with V.  A token that sees nothing has a
+ * row of zeros and lse -inf.  Tokens on unmapped pages are seen by nobody;
+ * whatever lies behind a sequence's end in its last page is not used.
+ *
+ *   q              bf16 [rows][num_q_heads][128]: new token i of sequence b is
+ *                  row new_offsets[b] + i (as twilight_kquant_append's k_new)
+ *   n_new          i32 [batch], clamped to [0, max_new]; NULL = max_new each
+ *   new_offsets    i32 [batch]; NULL = b * max_new
+ *   max_new        host: upper bound of n_new[] (sizes the launch and the
+ *                  workspace); at most 2^20, max_new * batch < 2^31;
+ *                  max_pages_per_seq <= 2^26
+ *   out            bf16 [rows][num_q_heads][128]; rows of no token are left
+ *   lse            fp32 [rows][num_q_heads] or NULL, as twilight_sparse_decode
+ *   ws             >= twilight_workspace_bytes(TW_WS_NEW_TOKENS, kv, max_new, 0)
+ *
+ * twilight_tree_attention: a tree of drafted tokens.  Every new token sees the
+ * tokens before the first new one, and of the new ones those whose bits are
+ * set in its mask row - itself only if its own bit is.  max_new <= 1024.
+ *   tree_mask      u32 [rows][mask_words]: bit j % 32 of word j / 32 = new
+ *                  token j is visible; bits of j >= n_new[b] are ignored
+ *   mask_words     host: mask_words * 32 >= max_new
+ *
+ * twilight_window_attention: consecutive tokens - one (decode), a chunk, a
+ * whole prompt - with a sliding window and sinks.  The token at position p
+ * sees the positions t <= p with p - t < window or t < num_sinks.
+ *   window         host, >= 1 (INT32_MAX: no window, plain causal attention)
+ *   num_sinks      host, >= 0
+ * Pages that lie wholly between the sinks and every later window may be given
+ * back (twilight_pages_free).
+ */
+int twilight_tree_attention(const twilight_kv_t* kv, const void* q, const int32_t* n_new, const int32_t* new_offsets,
+                            int32_t max_new, const uint32_t* tree_mask, int32_t mask_words, void* out, float* lse,
+                            void* ws, size_t ws_bytes, void* stream);
+int twilight_window_attention(const twilight_kv_t* kv, const void* q, const int32_t* n_new, const int32_t* new_offsets,
+                              int32_t max_new, int32_t window, int32_t num_sinks, void* out, float* lse,
+                              void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Pages of the cache.  The table of a batch is shared by all layers, the rows
+ * are not: the calls that hand out, share and give back pages work on the
+ * table and on one count per pool page, once for all layers; those that move
+ * rows work on one layer's pools.
+ *
+ *   ref_count      i32 [num_pool_pages]: in how many table entries the page
+ *                  stands.  A page with count 0 is free; nothing else is kept.
+ *                  The caller sets it up (all 0 with a table of -1).
+ * Pages are handed out from the lowest free one up, in ascending order of
+ * (row, logical page), so that tables and counts do not depend on timing.
+ * Where no free page is left the entry stays unmapped and *status gets
+ * TW_STATUS_POOL_EXHAUSTED.  Entries outside [0, num_pool_pages) are unmapped.
+ * Only kv's shape, page_table and seq_lens are used by the first three; they
+ * write kv->page_table (twilight_pages_fork does not).  max_pages_per_seq <=
+ * 2^26.
+ *
+ * twilight_pages_reserve: every unmapped entry among the pages that hold the
+ * positions seq_lens[b] .. seq_lens[b] + n_new[b] - 1 gets a page (seq_lens
+ * not yet advanced; beyond the row's max_pages_per_seq nothing happens).
+ *   n_new          i32 [batch], clamped to [0, max_new]
+ *   max_new        host: upper bound of n_new[] (sizes the workspace)
+ *   ws             >= twilight_workspace_bytes(TW_WS_PAGES, kv, max_new, 0)
+ *
+ * twilight_pages_free: logical pages first_page[b] .. end_page[b] - 1 of every
+ * row (clipped to the row) lose a reference, their entries become -1.
+ *   first_page, end_page   i32 [batch]
+ *
+ * twilight_pages_fork: a new batch from the rows of the old one.  Row i of
+ * new_table continues old row parent[i]; old rows without a child are gone.
+ * A parent's pages that are full (below seq_lens / 16) are shared by its
+ * children; the others - the partly filled one and any reserved beyond it - go
+ * to its first child, and each further child gets a free page for the partly
+ * filled one, with the pair to copy in copy_src[i] / copy_dst[i] (-1 where
+ * there is nothing to copy).  One twilight_pages_copy per layer then brings
+ * the rows.  Appending to a child writes no shared page; a sequence cut back
+ * below the length at which it was forked must not be appended to.
+ *   parent         i32 [new_batch]; outside [0, batch): an empty row
+ *   new_batch      host: >= 1, batch + new_batch <= 65535
+ *   new_table      i32 [new_batch][max_pages_per_seq] out (not kv->page_table)
+ *   new_lens       i32 [new_batch] out
+ *   copy_src, copy_dst     i32 [new_batch] out
+ *   ws             >= twilight_workspace_bytes(TW_WS_PAGES, kv, 0, new_batch)
+ *
+ * twilight_pages_copy: whole pages of one layer, all pools (k_pool, v_pool,
+ * kq_pool, kq_meta, page_minmax; those that are NULL are passed over).  Pairs
+ * with an index outside the pool do nothing.  A page must not be the
+ * destination of two pairs, nor of one pair and the source of another.
+ *   copy_src, copy_dst     i32 [n_copy]
+ *   n_copy         host, >= 0
+ *
+ * twilight_tokens_compact: kept tokens moved together in one layer: the token
+ * at position keep_idx[b][i] becomes position dst_start[b] + i, for
+ * i < keep_count[b]; its bf16 rows, codes and (scale, zero), bit for bit.  The
+ * bounds of the pages that hold dst_start[b] .. dst_start[b] + keep_count[b] - 1
+ * are taken again from the rows up to that end, and with keep_count[b] = 0
+ * those of the page that ends at dst_start[b] inside it.  After the
+ * verification of a draft: keep_idx the accepted tokens' positions, dst_start
+ * the position of the first drafted one; the caller sets seq_lens to
+ * dst_start + keep_count.  Entries outside [0, seq_lens[b]) or on unmapped
+ * pages are passed over, their destinations left as they were, and
+ * destinations on unmapped pages are not written.  No page that is written
+ * may be shared with another sequence.
+ *   keep_idx       i32 [batch][keep_stride]
+ *   keep_count     i32 [batch], clamped to [0, keep_stride]
+ *   dst_start      i32 [batch], >= 0
+ *   dst_table      i32 [batch][max_pages_per_seq]: the destination's pages, none
+ *                  of them a page that a kept token is read from; or NULL: in
+ *                  place, where keep_idx is strictly ascending and
+ *                  dst_start[b] <= keep_idx[b][0]
+ */
+int twilight_pages_reserve(const twilight_kv_t* kv, const int32_t* n_new, int32_t max_new, int32_t* ref_count,
+                           uint32_t* status, void* ws, size_t ws_bytes, void* stream);
+int twilight_pages_free(const twilight_kv_t* kv, const int32_t* first_page, const int32_t* end_page, int32_t* ref_count,
+                        uint32_t* status, void* stream);
+int twilight_pages_fork(const twilight_kv_t* kv, const int32_t* parent, int32_t new_batch, int32_t* new_table, int32_t* new_lens,
+                        int32_t* ref_count, int32_t* copy_src, int32_t* copy_dst, uint32_t* status,
+                        void* ws, size_t ws_bytes, void* stream);
+int twilight_pages_copy(const twilight_kv_t* kv, const int32_t* copy_src, const int32_t* copy_dst, int32_t n_copy, void* stream);
+int twilight_tokens_compact(const twilight_kv_t* kv, const int32_t* keep_idx, const int32_t* keep_count, int32_t keep_stride,
+                            const int32_t* dst_start, const int32_t* dst_table, void* stream);
+
 /* Workspace sizes (host-only query; no GPU needed). */
 #define TW_WS_SELECT 0
 #define TW_WS_PRUNE 1
@@ -370,10 +500,14 @@ int twilight_sparse_decode_per_head(const twilight_kv_t* kv, const void* q, cons
 #define TW_WS_PRUNE_TOKENS 4
 #define TW_WS_DS_SELECT 5
 #define TW_WS_SELECT_PRUNE 6
+#define TW_WS_NEW_TOKENS 7
+#define TW_WS_PAGES 8
 /*  max_sel: as passed to the call (0 with sel_pages == NULL; max_cand for
- *  TW_WS_PRUNE_TOKENS);
+ *  TW_WS_PRUNE_TOKENS; max_new for TW_WS_NEW_TOKENS and, 0 if nothing is to
+ *  be reserved, for TW_WS_PAGES);
  *  union_stride: as passed to sparse_decode (0 for dense), kept_stride for
- *  TW_WS_DECODE_PER_HEAD. */
+ *  TW_WS_DECODE_PER_HEAD, new_batch (0 if nothing is to be forked) for
+ *  TW_WS_PAGES. */
 size_t twilight_workspace_bytes(int which, const twilight_kv_t* kv, int32_t max_sel, int32_t union_stride);
 
 /*

@@ -46,7 +46,14 @@ struct twilight_kv;   /* twilight.h */
 #define TW_K_COMBINE 7
 #define TW_K_SCORE_TOPP 8         /* scoring + top-p + union in one launch (twilight_select_prune) */
 #define TW_K_SELECT_SCORE_TOPP 9  /* page selection as well */
-#define TW_K_COUNT 10
+#define TW_K_NEW_TOKENS 10        /* attention of several new tokens: tree or window */
+#define TW_K_NEW_COMBINE 11
+#define TW_K_PAGES_FREE 12
+#define TW_K_PAGES_TAKE 13        /* pages handed out: reserve, and the partly filled ones of a fork */
+#define TW_K_PAGES_FORK 14
+#define TW_K_PAGES_COPY 15
+#define TW_K_COMPACT 16
+#define TW_K_COUNT 17
 int twilight_prof_enable(int mode);
 int twilight_prof_select(int kernel_id, int every);
 int twilight_prof_collect(int32_t* kernel_ids /*host*/, float* ms /*host*/, int32_t cap);

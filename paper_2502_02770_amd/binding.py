@@ -14,10 +14,12 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("TWILIGHT_LIB") or os.path.join(_PKG, "libtwilight.so")   # override: tuning builds
 
 TW_WS_SELECT, TW_WS_PRUNE, TW_WS_DECODE, TW_WS_DECODE_PER_HEAD, TW_WS_PRUNE_TOKENS, TW_WS_DS_SELECT, TW_WS_SELECT_PRUNE = 0, 1, 2, 3, 4, 5, 6
-TW_STATUS_UNION_TRUNCATED, TW_STATUS_KEPT_TRUNCATED = 1, 2
+TW_WS_NEW_TOKENS, TW_WS_PAGES = 7, 8
+TW_STATUS_UNION_TRUNCATED, TW_STATUS_KEPT_TRUNCATED, TW_STATUS_POOL_EXHAUSTED, TW_STATUS_PAGE_COUNT = 1, 2, 4, 8
 TW_STATIC_SELECT_WS_BYTES = 8 << 20
 KERNEL_NAMES = ["kquant_append", "page_score", "page_select", "int4_score", "topp", "union",
-                "sparse_decode", "combine", "score_topp", "select_score_topp"]
+                "sparse_decode", "combine", "score_topp", "select_score_topp", "new_tokens", "new_combine",
+                "pages_free", "pages_take", "pages_fork", "pages_copy", "compact"]
 
 _vp, _i32, _i64, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
 
@@ -57,6 +59,13 @@ def lib():
     L.twilight_topp_prune_tokens.argtypes = [kvp, _vp, _vp, _vp, _i32, _f32, _vp, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _sz, _vp]
     L.twilight_sparse_decode.argtypes = [kvp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _sz, _vp]
     L.twilight_sparse_decode_per_head.argtypes = [kvp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _sz, _vp]
+    L.twilight_tree_attention.argtypes = [kvp, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _sz, _vp]
+    L.twilight_window_attention.argtypes = [kvp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _sz, _vp]
+    L.twilight_pages_reserve.argtypes = [kvp, _vp, _i32, _vp, _vp, _vp, _sz, _vp]
+    L.twilight_pages_free.argtypes = [kvp, _vp, _vp, _vp, _vp, _vp]
+    L.twilight_pages_fork.argtypes = [kvp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+    L.twilight_pages_copy.argtypes = [kvp, _vp, _vp, _i32, _vp]
+    L.twilight_tokens_compact.argtypes = [kvp, _vp, _vp, _i32, _vp, _vp, _vp]
     L.twilight_workspace_bytes.argtypes = [ctypes.c_int, kvp, _i32, _i32]
     L.twilight_pinned_device_pointer.argtypes = [_vp, ctypes.POINTER(_vp)]
     L.twilight_pinned_device_pointer.restype = ctypes.c_int
@@ -75,6 +84,8 @@ def lib():
     L.twilight_kernel_name.restype = ctypes.c_char_p
     for f in ("twilight_select_prune", "twilight_ds_select_tokens", "twilight_kquant_append", "twilight_select_pages", "twilight_select_pages_static", "twilight_append_select", "twilight_int4_score", "twilight_topp_prune",
               "twilight_int4_score_tokens", "twilight_topp_prune_tokens",
+              "twilight_tree_attention", "twilight_window_attention", "twilight_pages_reserve", "twilight_pages_free",
+              "twilight_pages_fork", "twilight_pages_copy", "twilight_tokens_compact",
               "twilight_sparse_decode", "twilight_sparse_decode_per_head", "twilight_prof_enable", "twilight_prof_select", "twilight_prof_collect"):
         getattr(L, f).restype = ctypes.c_int
     _lib = L
@@ -202,6 +213,44 @@ def twilight_sparse_decode_per_head(kv, q, kept_count, kept_idx, kept_stride, ou
     _check(lib().twilight_sparse_decode_per_head(ctypes.byref(kv), _ptr(q), _ptr(kept_count), _ptr(kept_idx),
                                                  int(kept_stride), _ptr(out), _ptr(lse), _ptr(ws),
                                                  ws.numel() * ws.element_size(), _stream()))
+
+
+def twilight_tree_attention(kv, q, n_new, new_offsets, max_new, tree_mask, mask_words, out, lse, ws):
+    _check(lib().twilight_tree_attention(ctypes.byref(kv), _ptr(q), _ptr(n_new), _ptr(new_offsets), int(max_new),
+                                         _ptr(tree_mask), int(mask_words), _ptr(out), _ptr(lse), _ptr(ws),
+                                         ws.numel() * ws.element_size(), _stream()))
+
+
+def twilight_window_attention(kv, q, n_new, new_offsets, max_new, window, num_sinks, out, lse, ws):
+    _check(lib().twilight_window_attention(ctypes.byref(kv), _ptr(q), _ptr(n_new), _ptr(new_offsets), int(max_new),
+                                           int(window), int(num_sinks), _ptr(out), _ptr(lse), _ptr(ws),
+                                           ws.numel() * ws.element_size(), _stream()))
+
+
+def twilight_pages_reserve(kv, n_new, max_new, ref_count, status, ws):
+    _check(lib().twilight_pages_reserve(ctypes.byref(kv), _ptr(n_new), int(max_new), _ptr(ref_count), _ptr(status),
+                                        _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+
+
+def twilight_pages_free(kv, first_page, end_page, ref_count, status):
+    _check(lib().twilight_pages_free(ctypes.byref(kv), _ptr(first_page), _ptr(end_page), _ptr(ref_count), _ptr(status),
+                                     _stream()))
+
+
+def twilight_pages_fork(kv, parent, new_batch, new_table, new_lens, ref_count, copy_src, copy_dst, status, ws):
+    _check(lib().twilight_pages_fork(ctypes.byref(kv), _ptr(parent), int(new_batch), _ptr(new_table), _ptr(new_lens),
+                                     _ptr(ref_count), _ptr(copy_src), _ptr(copy_dst), _ptr(status), _ptr(ws),
+                                     ws.numel() * ws.element_size(), _stream()))
+
+
+def twilight_pages_copy(kv, copy_src, copy_dst, n_copy):
+    _check(lib().twilight_pages_copy(ctypes.byref(kv), _ptr(copy_src), _ptr(copy_dst), int(n_copy), _stream()))
+
+
+def twilight_tokens_compact(kv, keep_idx, keep_count, keep_stride, dst_start, dst_table):
+    """dst_table None: in place."""
+    _check(lib().twilight_tokens_compact(ctypes.byref(kv), _ptr(keep_idx), _ptr(keep_count), int(keep_stride),
+                                         _ptr(dst_start), _ptr(dst_table), _stream()))
 
 
 def twilight_decode_plan(kv, which=TW_WS_DECODE, dense=False):

@@ -45,6 +45,94 @@ class PagedKV:
         self.append(k, v, start, self.seq_lens, offs, int(self.seq_lens.max().item()))
 
 
+    def copy_pages(self, src, dst):
+        """twilight_pages_copy: whole pages src[i] -> dst[i] of this layer; negative entries are passed over."""
+        B.twilight_pages_copy(self.kv, src, dst, src.numel())
+
+    def compact(self, keep_idx, keep_count, dst_start, dst_table=None):
+        """twilight_tokens_compact; does not change seq_lens."""
+        B.twilight_tokens_compact(self.kv, keep_idx, keep_count, keep_idx.shape[1], dst_start, dst_table)
+
+
+class PagePool:
+    """Counts and status word of a pool of pages, shared by the layers whose caches have the same page table.  `cache` is any
+    of those layers; the calls change its page_table, or make a new one (fork)."""
+
+    def __init__(self, cache):
+        self.cache = cache
+        dev = cache.device
+        held = cache.page_table[(cache.page_table >= 0) & (cache.page_table < cache.num_pool_pages)].long()
+        self.ref_count = torch.bincount(held, minlength=cache.num_pool_pages).to(torch.int32)
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self._ws = {}
+
+    def _workspace(self, max_new, new_batch):
+        if (max_new, new_batch) not in self._ws:
+            self._ws[max_new, new_batch] = torch.empty(B.twilight_workspace_bytes(B.TW_WS_PAGES, self.cache.kv, max_new, new_batch),
+                                                       dtype=torch.uint8, device=self.cache.device)
+        return self._ws[max_new, new_batch]
+
+    def reserve(self, n_new, max_new):
+        """Pages for the next n_new[b] positions of every sequence (seq_lens not yet advanced)."""
+        B.twilight_pages_reserve(self.cache.kv, n_new, max_new, self.ref_count, self.status, self._workspace(max_new, 0))
+
+    def free(self, first_page, end_page):
+        """Logical pages first_page[b] .. end_page[b] - 1 of every row given back."""
+        B.twilight_pages_free(self.cache.kv, first_page, end_page, self.ref_count, self.status)
+
+    def free_behind(self, window, num_sinks):
+        """The pages given back that neither the sinks nor the window of the next token reaches (twilight_window_attention)."""
+        lens = self.cache.seq_lens
+        self.free(torch.full_like(lens, -(-num_sinks // 16)), torch.clamp((lens + 1 - window) // 16, min=0))
+
+    def fork(self, parent):
+        """-> (new_table, new_lens, copy_src, copy_dst) of the batch whose row i continues row parent[i]; every layer then
+        copies the pairs (PagedKV.copy_pages)."""
+        c, n = self.cache, parent.numel()
+        i32 = dict(dtype=torch.int32, device=c.device)
+        table, lens = torch.empty(n, c.max_pages, **i32), torch.empty(n, **i32)
+        src, dst = torch.empty(n, **i32), torch.empty(n, **i32)
+        B.twilight_pages_fork(c.kv, parent, n, table, lens, self.ref_count, src, dst, self.status, self._workspace(0, n))
+        return table, lens, src, dst
+
+
+class NewTokens:
+    """Pre-allocated outputs and workspace of attention of up to max_new new tokens per sequence (rows b * max_new + i)."""
+
+    def __init__(self, cache, max_new, with_lse=True):
+        c = self.cache = cache
+        self.max_new = int(max_new)
+        rows = c.batch * self.max_new
+        self.out = torch.zeros(rows, c.Hq, 128, dtype=torch.bfloat16, device=c.device)
+        self.lse = torch.zeros(rows, c.Hq, dtype=torch.float32, device=c.device) if with_lse else None
+        self.ws = torch.empty(B.twilight_workspace_bytes(B.TW_WS_NEW_TOKENS, c.kv, self.max_new), dtype=torch.uint8, device=c.device)
+
+    def tree(self, q, tree_mask, n_new=None):
+        """A drafted tree per sequence; tree_mask i32 [rows, words] (tree_mask_of_parents)."""
+        B.twilight_tree_attention(self.cache.kv, q, n_new, None, self.max_new, tree_mask, tree_mask.shape[1], self.out, self.lse, self.ws)
+        return self.out
+
+    def window(self, q, window, num_sinks=0, n_new=None):
+        """Consecutive tokens under a sliding window with sinks."""
+        B.twilight_window_attention(self.cache.kv, q, n_new, None, self.max_new, window, num_sinks, self.out, self.lse, self.ws)
+        return self.out
+
+
+def tree_mask_of_parents(parents):
+    """Mask words [..., ceil(n / 32)] (i32) of drafted trees from their parents [..., n] (before their children; -1: the last
+    cached token): every token sees its ancestors and itself."""
+    n = parents.shape[-1]
+    see = torch.zeros(*parents.shape, -(-n // 32) * 32, dtype=torch.bool, device=parents.device)
+    for j in range(n):
+        up = parents[..., j].long()
+        row = torch.take_along_dim(see, up.clamp(min=0)[..., None, None], dim=-2).squeeze(-2) & (up >= 0)[..., None]
+        row[..., j] = True
+        see[..., j, :] = row
+    bits = see.view(*parents.shape, -1, 32).long() << torch.arange(32, device=parents.device)
+    words = bits.sum(-1)
+    return torch.where(words >= 1 << 31, words - (1 << 32), words).to(torch.int32)
+
+
 class DecodeStep:
     """Pre-allocated outputs and workspaces of one decode step; runs
     select -> prune -> attend through the C ABI."""

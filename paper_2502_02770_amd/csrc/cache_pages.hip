@@ -1,0 +1,505 @@
+// Pages of the cache: handed out, shared, given back (table and counts, integers only), copied and compacted (one layer's
+// pools, bits only).  The state of the pool is one count per page; a page is free when its count is 0, and pages are
+// handed out from the lowest free one up in the order of the requests.  Counts change by integer atomics, whose order
+// does not matter, and the order of handing out is a prefix sum, so tables and counts never depend on timing.
+#include "tw_common.h"
+
+namespace {
+
+constexpr int TAKE_THREADS = 1024, TAKE_WAVES = TAKE_THREADS / 64;
+constexpr int TAKE_STEPS = 16;                   // counts per lane and pass of the search for free pages
+constexpr int TAKE_PASS = TAKE_THREADS * TAKE_STEPS;
+
+struct PagesArgs {
+  int32_t* table;                                // kv->page_table
+  const int32_t* seq_lens;
+  int32_t* ref;
+  uint32_t* status;
+  int batch, max_pages;
+  unsigned pool_pages;
+  // reserve
+  const int32_t* n_new;
+  int max_new;
+  // free
+  const int32_t* first;
+  const int32_t* end;
+  // fork
+  const int32_t* parent;
+  int new_batch;
+  int32_t* new_table;
+  int32_t* new_lens;
+  int32_t* copy_src;
+  int32_t* copy_dst;
+  // workspace of the hand-out: requests before each row, the pages found
+  int32_t* ws_before;
+  int32_t* ws_found;
+};
+
+__device__ __forceinline__ int row_len(const PagesArgs& a, int b) {
+  return max(0, min(a.seq_lens[b], a.max_pages * TW_PAGE));
+}
+
+// Every entry of the range loses its page.  Bound by the atomics' trips to memory; one thread per entry, all rows at once.
+__global__ __launch_bounds__(256) void pages_free_kernel(PagesArgs a) {
+  const int b = blockIdx.y;
+  const int lo = max(a.first[b], 0), hi = min(a.end[b], a.max_pages);
+  for (int p = lo + (int)(blockIdx.x * 256 + threadIdx.x); p < hi; p += (int)gridDim.x * 256) {
+    int32_t* e = a.table + (long long)b * a.max_pages + p;
+    const int id = *e;
+    if ((unsigned)id >= a.pool_pages) continue;
+    *e = -1;
+    if (atomicAdd(a.ref + id, -1) <= 0) {        // more references given back than there were
+      atomicAdd(a.ref + id, 1);
+      atomicOr(a.status, TW_STATUS_PAGE_COUNT);
+    }
+  }
+}
+
+// Blocks y < new_batch write row y of the new table; the others settle the counts of old row y - new_batch: its full pages by
+// the number of children, the pages that only a first child takes over by whether there is one.
+__global__ __launch_bounds__(256) void pages_fork_kernel(PagesArgs a) {
+  __shared__ int seen;
+  const int tid = threadIdx.x;
+  if (tid == 0) seen = 0;
+  __syncthreads();
+  if ((int)blockIdx.y < a.new_batch) {
+    const int i = blockIdx.y, r = a.parent[i];
+    int32_t* out = a.new_table + (long long)i * a.max_pages;
+    if (r < 0 || r >= a.batch) {                 // an empty row
+      for (int p = (int)blockIdx.x * 256 + tid; p < a.max_pages; p += (int)gridDim.x * 256) out[p] = -1;
+      if (blockIdx.x == 0 && tid == 0) { a.new_lens[i] = 0; a.copy_src[i] = a.copy_dst[i] = -1; }
+      return;
+    }
+    int earlier = 0;
+    for (int j = tid; j < i; j += 256) earlier |= a.parent[j] == r;
+    if (earlier) seen = 1;
+    __syncthreads();
+    const bool first = seen == 0;
+    const int len = row_len(a, r), full = len / TW_PAGE;
+    const int32_t* row = a.table + (long long)r * a.max_pages;
+    for (int p = (int)blockIdx.x * 256 + tid; p < a.max_pages; p += (int)gridDim.x * 256) {
+      const int id = row[p];
+      out[p] = (unsigned)id < a.pool_pages && (p < full || first) ? id : -1;
+    }
+    if (blockIdx.x == 0 && tid == 0) {
+      a.new_lens[i] = len;
+      int src = -1;                              // a request for a page of its own
+      if (!first && len % TW_PAGE) src = row[full];
+      a.copy_src[i] = (unsigned)src < a.pool_pages ? src : -1;
+      a.copy_dst[i] = -1;
+    }
+    return;
+  }
+  const int r = (int)blockIdx.y - a.new_batch;
+  int mine = 0;
+  for (int j = tid; j < a.new_batch; j += 256) mine += a.parent[j] == r;
+  if (mine) atomicAdd(&seen, mine);
+  __syncthreads();
+  const int children = seen;
+  if (children == 1) return;
+  const int full = row_len(a, r) / TW_PAGE, last = children ? full : a.max_pages;
+  const int32_t* row = a.table + (long long)r * a.max_pages;
+  for (int p = (int)blockIdx.x * 256 + tid; p < last; p += (int)gridDim.x * 256) {
+    const int id = row[p];
+    if ((unsigned)id >= a.pool_pages) continue;
+    if (children) atomicAdd(a.ref + id, children - 1);
+    else if (atomicAdd(a.ref + id, -1) <= 0) {
+      atomicAdd(a.ref + id, 1);
+      atomicOr(a.status, TW_STATUS_PAGE_COUNT);
+    }
+  }
+}
+
+// Entries of row b that reserve looks at.
+__device__ __forceinline__ void reserve_range(const PagesArgs& a, int b, int* lo, int* hi) {
+  const int n = max(0, min(a.n_new[b], a.max_new)), len = row_len(a, b);
+  *lo = len / TW_PAGE;
+  *hi = n ? (int)min((long long)a.max_pages, ((long long)len + n + TW_PAGE - 1) / TW_PAGE) : *lo;
+}
+
+// Hands out pages: one workgroup, since the order of the pages is one chain of prefix sums.  Requests are counted row by
+// row, the counts searched from page 0 until there are as many free pages as requests, the pages dealt out by rank.
+// FORK: request i is copy_src[i] >= 0, the entry that row i's partly filled page stands in.  Otherwise (reserve): the
+// unmapped entries of a row's range, a wave per row.
+template <bool FORK>
+__global__ __launch_bounds__(TAKE_THREADS) void pages_take_kernel(PagesArgs a) {
+  __shared__ uint32_t wsum[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int rows = FORK ? a.new_batch : a.batch;
+  // ---- requests before each row
+  if (!FORK) {
+    for (int b = wave; b < rows; b += TAKE_WAVES) {
+      int lo, hi, n = 0;
+      reserve_range(a, b, &lo, &hi);
+      for (int p0 = lo; p0 < hi; p0 += 64) {
+        const int p = p0 + lane;
+        n += __popcll(__ballot(p < hi && (unsigned)a.table[(long long)b * a.max_pages + min(p, hi - 1)] >= a.pool_pages));
+      }
+      if (lane == 0) a.ws_before[b] = n;
+    }
+    __syncthreads();
+  }
+  uint32_t total = 0;
+  for (int b0 = 0; b0 < rows; b0 += TAKE_THREADS) {
+    const int b = b0 + tid;
+    const uint32_t n = b < rows ? (FORK ? (uint32_t)(a.copy_src[b] >= 0) : (uint32_t)a.ws_before[b]) : 0u;
+    uint32_t sum;
+    const uint32_t upto = tw_block_scan_u32(n, wsum, &sum);
+    if (b < rows) a.ws_before[b] = (int)(total + upto - n);
+    total += sum;
+  }
+  if (total == 0) return;
+  // ---- the lowest free pages
+  uint32_t found = 0;
+  for (unsigned base = 0; base < a.pool_pages && found < total; base += TAKE_PASS) {
+    const unsigned p0 = base + (unsigned)wave * (64 * TAKE_STEPS) + (unsigned)lane;
+    int c[TAKE_STEPS];
+#pragma unroll
+    for (int k = 0; k < TAKE_STEPS; ++k) c[k] = p0 + 64u * k < a.pool_pages ? a.ref[p0 + 64u * k] : 1;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int k = 0; k < TAKE_STEPS; ++k) mine += (uint32_t)__popcll(__ballot(c[k] == 0));
+    if (lane == 0) wsum[wave] = mine;
+    __syncthreads();
+    uint32_t rank = found, all = 0;
+#pragma unroll
+    for (int w = 0; w < TAKE_WAVES; ++w) { const uint32_t x = wsum[w]; rank += w < wave ? x : 0u; all += x; }
+    __syncthreads();
+    if (mine) {
+#pragma unroll
+      for (int k = 0; k < TAKE_STEPS; ++k) {
+        const unsigned long long f = __ballot(c[k] == 0);
+        const uint32_t r = rank + tw_bits_below(f);
+        if (c[k] == 0 && r < total) { a.ws_found[r] = (int)(p0 + 64u * k); a.ref[p0 + 64u * k] = 1; }
+        rank += (uint32_t)__popcll(f);
+      }
+    }
+    found += all;
+  }
+  if (found < total && tid == 0) atomicOr(a.status, TW_STATUS_POOL_EXHAUSTED);
+  __syncthreads();
+  // ---- dealt out
+  if (FORK) {
+    for (int i = tid; i < rows; i += TAKE_THREADS) {
+      if (a.copy_src[i] < 0) continue;
+      const uint32_t r = (uint32_t)a.ws_before[i];
+      if (r < found) {
+        const int id = a.ws_found[r];
+        a.copy_dst[i] = id;
+        a.new_table[(long long)i * a.max_pages + a.new_lens[i] / TW_PAGE] = id;
+      } else {
+        a.copy_src[i] = -1;
+      }
+    }
+    return;
+  }
+  for (int b = wave; b < rows; b += TAKE_WAVES) {
+    int lo, hi;
+    reserve_range(a, b, &lo, &hi);
+    uint32_t r = lo < hi ? (uint32_t)a.ws_before[b] : 0u;
+    for (int p0 = lo; p0 < hi; p0 += 64) {
+      const int p = p0 + lane;
+      int32_t* e = a.table + (long long)b * a.max_pages + min(p, hi - 1);
+      const unsigned long long want = __ballot(p < hi && (unsigned)*e >= a.pool_pages);
+      const uint32_t k = r + tw_bits_below(want);
+      if (want >> lane & 1ull) *e = k < found ? a.ws_found[k] : -1;
+      r += (uint32_t)__popcll(want);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- one layer's rows
+struct RowsArgs {
+  uint4* k;
+  uint4* v;
+  uint4* codes;
+  uint4* meta;
+  uint4* bounds;
+  const int32_t* src;                            // copy: pairs
+  const int32_t* dst;
+  const int32_t* table;                          // compact
+  const int32_t* to;
+  const int32_t* seq_lens;
+  const int32_t* keep;
+  const int32_t* count;
+  const int32_t* start;
+  int batch, Hkv, bits, max_pages, stride;
+  unsigned pool_pages;
+};
+
+// One workgroup per (pair, KV head): 4096 + 4096 + 256 * bits + 256 + 512 bytes, all loads before the stores.  HBM.
+__global__ __launch_bounds__(256) void pages_copy_kernel(RowsArgs a) {
+  const int h = (int)(blockIdx.x % (unsigned)a.Hkv), i = (int)(blockIdx.x / (unsigned)a.Hkv), tid = threadIdx.x;
+  const int s = a.src[i], d = a.dst[i];
+  if ((unsigned)s >= a.pool_pages || (unsigned)d >= a.pool_pages || s == d) return;
+  const long long sp = (long long)s * a.Hkv + h, dp = (long long)d * a.Hkv + h;
+  const int nc = 16 * a.bits;
+  uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x, z = x;
+  uint4* to = nullptr;                           // codes, (scale, zero), bounds: at most 176 pieces
+  if (a.k) x = tw_ld_stream(a.k + sp * 256 + tid);
+  if (a.v) y = tw_ld_stream(a.v + sp * 256 + tid);
+  const uint4* from = nullptr;
+  if (tid < nc) { if (a.codes) { from = a.codes + sp * nc + tid; to = a.codes + dp * nc + tid; } }
+  else if (tid < nc + 16) { if (a.meta) { from = a.meta + sp * 16 + (tid - nc); to = a.meta + dp * 16 + (tid - nc); } }
+  else if (tid < nc + 48) { if (a.bounds) { from = a.bounds + sp * 32 + (tid - nc - 16); to = a.bounds + dp * 32 + (tid - nc - 16); } }
+  if (to) z = *from;
+  if (a.k) a.k[dp * 256 + tid] = x;
+  if (a.v) a.v[dp * 256 + tid] = y;
+  if (to) *to = z;
+}
+
+// Compaction.  The pieces of a row do not depend on each other, so the columns of a sequence's rows go to five
+// workgroups per KV head: K and V in halves of 128 bytes, codes with (scale, zero).  A workgroup takes the destination
+// positions in steps of 128 (8 whole pages): to another table every step is a workgroup of its own; in place one
+// workgroup walks them all, and reads a step's rows before it writes them - destinations lie at or before their
+// sources, so no step overwrites what a later one reads.
+constexpr int STEP = 128;
+constexpr int CODE_UNITS = STEP * 9 / 256 + 1;   // 16-byte pieces of a step's codes and (scale, zero) per thread, at most
+
+__device__ __forceinline__ void hold(uint4& x) { asm volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w)); }
+
+// Source and destination row (page * 16 + slot, of the pools without their head index) of destination position t; -1: none.
+struct Move { int src, dst; };
+template <bool INPLACE>
+__device__ __forceinline__ Move move_of(const RowsArgs& a, int b, int t, int start, int end, int len) {
+  Move m = {-1, -1};
+  if (t >= end || t >= a.max_pages * TW_PAGE) return m;
+  const long long row = (long long)b * a.max_pages;
+  const int dp = (INPLACE ? a.table : a.to)[row + t / TW_PAGE];
+  if ((unsigned)dp >= a.pool_pages) return m;
+  m.dst = dp * TW_PAGE + t % TW_PAGE;
+  if (t < start) return m;
+  const int s = a.keep[(long long)b * a.stride + (t - start)];
+  if (s < 0 || s >= len) return m;
+  const int sp = a.table[row + s / TW_PAGE];
+  if ((unsigned)sp < a.pool_pages) m.src = sp * TW_PAGE + s % TW_PAGE;
+  return m;
+}
+
+template <bool INPLACE>
+__global__ __launch_bounds__(256) void compact_kernel(RowsArgs a) {
+  const int col = (int)(blockIdx.x % 5u), h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int start = a.start[b];
+  if (start < 0) return;
+  const int len = max(0, min(a.seq_lens[b], a.max_pages * TW_PAGE));
+  const int end = (int)min((long long)start + max(0, min(a.count[b], a.stride)), 0x7FFFFF00ll);
+  int t0 = start & ~(TW_PAGE - 1);
+  int last = end;
+  if (!INPLACE) {
+    const long long at = (long long)t0 + (long long)(blockIdx.x / 5u) * STEP;
+    if (at >= end) return;
+    t0 = (int)at;
+    last = t0 + 1;
+  }
+  last = min(last, a.max_pages * TW_PAGE);
+  // row (page, slot) of head h in a pool of `pieces` 16-byte pieces per row
+  auto at = [&](int r, int pieces) -> long long { return (((long long)(r / TW_PAGE) * a.Hkv + h) * TW_PAGE + r % TW_PAGE) * pieces; };
+
+  if (col < 4) {
+    uint4* pool = col < 2 ? a.k : a.v;
+    if (!pool) return;
+    const int piece = (col & 1) * 8 + (lane & 7);
+    const bool bounds = col < 2 && a.bounds;
+    for (; t0 < last; t0 += STEP) {
+      // a wave holds two pages: four pieces per lane, tokens 16 j + 8 i + lane / 8 (j page, i half of it)
+      Move m[4];
+      uint4 x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        m[u] = move_of<INPLACE>(a, b, t0 + wave * 32 + u * 8 + (lane >> 3), start, end, len);
+        const int r = m[u].src >= 0 ? m[u].src : bounds ? m[u].dst : -1;       // rows that stay count for the bounds
+        x[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (r >= 0) x[u] = pool[at(r, 16) + piece];
+      }
+      if (INPLACE) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) hold(x[u]);  // every load of the step has returned
+        __syncthreads();
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (m[u].src >= 0) pool[at(m[u].dst, 16) + piece] = x[u];
+      if (bounds) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float lo[8], hi[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) { lo[k] = __builtin_inff(); hi[k] = -__builtin_inff(); }
+          bool any = false;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int u = 2 * j + i;
+            if (m[u].dst < 0) continue;
+            any = true;
+            float f[8];
+            tw_unpack8(x[u], f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { lo[k] = fminf(lo[k], f[k]); hi[k] = fmaxf(hi[k], f[k]); }
+          }
+#pragma unroll
+          for (int s = 8; s < 64; s <<= 1)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { lo[k] = fminf(lo[k], __shfl_xor(lo[k], s)); hi[k] = fmaxf(hi[k], __shfl_xor(hi[k], s)); }
+          if (!__ballot(any)) continue;
+          // the page's first position is held by lanes 0..7, and is a token whenever any of the page is
+          if (lane < 8) {
+            const long long page = (long long)(m[2 * j].dst / TW_PAGE) * a.Hkv + h;
+            uint32_t w[8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              w[k] = (__float_as_uint(lo[2 * k]) >> 16) | (__float_as_uint(lo[2 * k + 1]) & 0xFFFF0000u);
+              w[4 + k] = (__float_as_uint(hi[2 * k]) >> 16) | (__float_as_uint(hi[2 * k + 1]) & 0xFFFF0000u);
+            }
+            a.bounds[page * 32 + piece] = make_uint4(w[0], w[1], w[2], w[3]);
+            a.bounds[page * 32 + 16 + piece] = make_uint4(w[4], w[5], w[6], w[7]);
+          }
+        }
+      }
+    }
+    return;
+  }
+  // codes (bits pieces per row) and (scale, zero) (one piece)
+  const int pieces = a.bits + 1;
+  for (; t0 < last; t0 += STEP) {
+    uint4 x[CODE_UNITS];
+    uint4* to[CODE_UNITS];
+#pragma unroll
+    for (int u = 0; u < CODE_UNITS; ++u) {
+      const int unit = tid + 256 * u, tok = unit / pieces, pc = unit - tok * pieces;
+      to[u] = nullptr;
+      x[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (tok >= STEP) continue;
+      const Move m = move_of<INPLACE>(a, b, t0 + tok, start, end, len);
+      if (m.src < 0) continue;
+      if (pc < a.bits) {
+        if (a.codes) { x[u] = a.codes[at(m.src, a.bits) + pc]; to[u] = a.codes + at(m.dst, a.bits) + pc; }
+      } else if (a.meta) {
+        x[u] = a.meta[at(m.src, 1)]; to[u] = a.meta + at(m.dst, 1);
+      }
+    }
+    if (INPLACE) {
+#pragma unroll
+      for (int u = 0; u < CODE_UNITS; ++u) hold(x[u]);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int u = 0; u < CODE_UNITS; ++u)
+      if (to[u]) *to[u] = x[u];
+  }
+}
+
+// ---------------------------------------------------------------- host side
+size_t align256p(size_t x) { return (x + 255) & ~(size_t)255; }
+
+int check_pages(const twilight_kv_t* kv, TwDims* d) {
+  if (int e = tw_check_kv(kv, d)) return e;
+  return d->max_pages > TW_MAX_ROW_PAGES ? TW_EINVAL : TW_OK;
+}
+
+PagesArgs pages_args(const twilight_kv_t* kv, const TwDims& d, int32_t* ref, uint32_t* status) {
+  PagesArgs a = {};
+  a.table = const_cast<int32_t*>(kv->page_table); a.seq_lens = kv->seq_lens; a.ref = ref; a.status = status;
+  a.batch = d.batch; a.max_pages = d.max_pages; a.pool_pages = (unsigned)d.pool_pages;
+  return a;
+}
+unsigned row_blocks(int max_pages) { return (unsigned)min((max_pages + 255) / 256, 64); }
+
+size_t take_rows_bytes(long long rows) { return align256p((size_t)rows * 4); }
+
+}  // namespace
+
+size_t tw_pages_workspace(const TwDims& d, int max_new, int new_batch) {
+  if (max_new < 0 || new_batch < 0 || new_batch > 65535) return 0;
+  const long long rows = d.batch > new_batch ? d.batch : new_batch;
+  const long long pages = min((long long)d.max_pages, max_new ? (max_new + TW_PAGE - 1ll) / TW_PAGE + 1 : 0ll);
+  const long long most = min(max((long long)d.batch * pages, (long long)new_batch), d.pool_pages);
+  return take_rows_bytes(rows) + align256p((size_t)most * 4);
+}
+
+extern "C" int twilight_pages_reserve(const twilight_kv_t* kv, const int32_t* n_new, int32_t max_new, int32_t* ref_count,
+                                      uint32_t* status, void* ws, size_t ws_bytes, void* stream) {
+  TwDims d;
+  if (int e = check_pages(kv, &d)) return e;
+  if (!n_new || max_new <= 0 || !ref_count || !status) return TW_EINVAL;
+  if (!ws || ws_bytes < tw_pages_workspace(d, max_new, 0)) return TW_EWORKSPACE;
+  hipStream_t s = (hipStream_t)stream;
+  PagesArgs a = pages_args(kv, d, ref_count, status);
+  a.n_new = n_new; a.max_new = max_new;
+  a.ws_before = (int32_t*)ws;
+  a.ws_found = (int32_t*)((char*)ws + take_rows_bytes(d.batch));
+  tw_prof_before(TW_K_PAGES_TAKE, s);
+  TW_LAUNCH((pages_take_kernel<false>), dim3(1), dim3(TAKE_THREADS), 0, s, a);
+  return tw_prof_after(s);
+}
+
+extern "C" int twilight_pages_free(const twilight_kv_t* kv, const int32_t* first_page, const int32_t* end_page, int32_t* ref_count,
+                                   uint32_t* status, void* stream) {
+  TwDims d;
+  if (int e = check_pages(kv, &d)) return e;
+  if (!first_page || !end_page || !ref_count || !status) return TW_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  PagesArgs a = pages_args(kv, d, ref_count, status);
+  a.first = first_page; a.end = end_page;
+  tw_prof_before(TW_K_PAGES_FREE, s);
+  TW_LAUNCH(pages_free_kernel, dim3(row_blocks(d.max_pages), (unsigned)d.batch), dim3(256), 0, s, a);
+  return tw_prof_after(s);
+}
+
+extern "C" int twilight_pages_fork(const twilight_kv_t* kv, const int32_t* parent, int32_t new_batch, int32_t* new_table, int32_t* new_lens,
+                                   int32_t* ref_count, int32_t* copy_src, int32_t* copy_dst, uint32_t* status,
+                                   void* ws, size_t ws_bytes, void* stream) {
+  TwDims d;
+  if (int e = check_pages(kv, &d)) return e;
+  if (!parent || !new_table || !new_lens || !ref_count || !copy_src || !copy_dst || !status) return TW_EINVAL;
+  if (new_batch <= 0 || new_batch > 65535 || d.batch + new_batch > 65535 || new_table == kv->page_table || new_lens == kv->seq_lens) return TW_EINVAL;
+  if (!ws || ws_bytes < tw_pages_workspace(d, 0, new_batch)) return TW_EWORKSPACE;
+  hipStream_t s = (hipStream_t)stream;
+  PagesArgs a = pages_args(kv, d, ref_count, status);
+  a.parent = parent; a.new_batch = new_batch; a.new_table = new_table; a.new_lens = new_lens; a.copy_src = copy_src; a.copy_dst = copy_dst;
+  a.ws_before = (int32_t*)ws;
+  a.ws_found = (int32_t*)((char*)ws + take_rows_bytes(new_batch));
+  tw_prof_before(TW_K_PAGES_FORK, s);
+  TW_LAUNCH(pages_fork_kernel, dim3(row_blocks(d.max_pages), (unsigned)(d.batch + new_batch)), dim3(256), 0, s, a);
+  if (int e = tw_prof_after(s)) return e;
+  tw_prof_before(TW_K_PAGES_TAKE, s);
+  TW_LAUNCH((pages_take_kernel<true>), dim3(1), dim3(TAKE_THREADS), 0, s, a);
+  return tw_prof_after(s);
+}
+
+static RowsArgs rows_args(const twilight_kv_t* kv, const TwDims& d) {
+  RowsArgs a = {};
+  a.k = (uint4*)kv->k_pool; a.v = (uint4*)kv->v_pool; a.codes = (uint4*)kv->kq_pool; a.meta = (uint4*)kv->kq_meta; a.bounds = (uint4*)kv->page_minmax;
+  a.batch = d.batch; a.Hkv = d.Hkv; a.bits = d.bits; a.max_pages = d.max_pages; a.pool_pages = (unsigned)d.pool_pages;
+  return a;
+}
+
+extern "C" int twilight_pages_copy(const twilight_kv_t* kv, const int32_t* copy_src, const int32_t* copy_dst, int32_t n_copy, void* stream) {
+  TwDims d;
+  if (int e = check_pages(kv, &d)) return e;
+  if (!copy_src || !copy_dst || n_copy < 0 || (long long)n_copy * d.Hkv > 0x7FFFFFFFll) return TW_EINVAL;
+  if (n_copy == 0) return TW_OK;
+  hipStream_t s = (hipStream_t)stream;
+  RowsArgs a = rows_args(kv, d);
+  a.src = copy_src; a.dst = copy_dst;
+  tw_prof_before(TW_K_PAGES_COPY, s);
+  TW_LAUNCH(pages_copy_kernel, dim3((unsigned)(n_copy * d.Hkv)), dim3(256), 0, s, a);
+  return tw_prof_after(s);
+}
+
+extern "C" int twilight_tokens_compact(const twilight_kv_t* kv, const int32_t* keep_idx, const int32_t* keep_count, int32_t keep_stride,
+                                       const int32_t* dst_start, const int32_t* dst_table, void* stream) {
+  TwDims d;
+  if (int e = check_pages(kv, &d)) return e;
+  if (!keep_idx || !keep_count || keep_stride <= 0 || !dst_start || !kv->k_pool) return TW_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  RowsArgs a = rows_args(kv, d);
+  a.table = kv->page_table; a.to = dst_table; a.seq_lens = kv->seq_lens;
+  a.keep = keep_idx; a.count = keep_count; a.start = dst_start; a.stride = keep_stride;
+  const long long most = min((long long)keep_stride, (long long)d.max_pages * TW_PAGE) + TW_PAGE - 1;
+  const unsigned steps = (unsigned)((most + STEP - 1) / STEP);
+  const bool in_place = !dst_table || dst_table == kv->page_table;
+  tw_prof_before(TW_K_COMPACT, s);
+  if (in_place) TW_LAUNCH((compact_kernel<true>), dim3(5, (unsigned)d.Hkv, (unsigned)d.batch), dim3(256), 0, s, a);
+  else TW_LAUNCH((compact_kernel<false>), dim3(5 * steps, (unsigned)d.Hkv, (unsigned)d.batch), dim3(256), 0, s, a);
+  return tw_prof_after(s);
+}

@@ -5,6 +5,8 @@
 #include "topp_common.h"
 
 int tw_decode_chunk(bool dense);
+size_t tw_new_tokens_workspace(const TwDims& d, int max_new);
+size_t tw_pages_workspace(const TwDims& d, int max_new, int new_batch);
 long long tw_decode_max_items(const TwDims& d, bool dense, int union_stride);
 
 int tw_check_kv(const twilight_kv_t* kv, TwDims* d) {
@@ -86,6 +88,10 @@ extern "C" size_t twilight_workspace_bytes(int which, const twilight_kv_t* kv, i
       const size_t items = (size_t)tw_decode_max_items(d, false, union_stride) / d.Hkv * d.Hq;
       return align256((size_t)(d.batch * d.Hq + 1) * 4) + align256(items * 8) + align256(items * 128 * 4);
     }
+    case TW_WS_NEW_TOKENS:
+      return tw_new_tokens_workspace(d, max_sel);
+    case TW_WS_PAGES:
+      return tw_pages_workspace(d, max_sel, union_stride);
     default:
       return 0;
   }
@@ -106,7 +112,8 @@ extern "C" int twilight_abi_version(void) { return TW_ABI_VERSION; }
 
 extern "C" const char* twilight_kernel_name(int id) {
   static const char* names[TW_K_COUNT] = {"kquant_append", "page_score", "page_select", "int4_score",
-                                          "topp", "union", "sparse_decode", "combine", "score_topp", "select_score_topp"};
+                                          "topp", "union", "sparse_decode", "combine", "score_topp", "select_score_topp",
+                                          "new_tokens", "new_combine", "pages_free", "pages_take", "pages_fork", "pages_copy", "compact"};
   return (id >= 0 && id < TW_K_COUNT) ? names[id] : "?";
 }
 

@@ -20,6 +20,12 @@ struct TwDims {
 int tw_check_kv(const twilight_kv_t* kv, TwDims* d);   // TW_OK or TW_EINVAL
 int tw_num_cus();                                        // compute units of the current device
 
+// Most new tokens per sequence: of a chunk or prompt (row blocks of a launch stay in 32 bits), of a tree.
+#define TW_MAX_NEW (1 << 20)
+#define TW_MAX_TREE 1024
+// Most pages of a row where token positions are added to in 32 bits (the operators on new tokens and on pages).
+#define TW_MAX_ROW_PAGES (1 << 26)
+
 // Launch bracket used by every entry point: tw_prof_before opens a timing record when the
 // kernel is to be timed, TW_LAUNCH then launches with the record's event pair attached to the
 // dispatch itself (start / stop timestamps of the kernel, no extra packets on the stream; a plain

@@ -1,0 +1,116 @@
+"""Host-side refusals, workspace sizes and the mask helper of the operators on new tokens and on the cache's pages (no GPU)."""
+import ctypes
+import os
+
+import numpy as np
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def T():
+    import paper_2502_02770_amd as T
+    if not os.path.exists(T.binding.LIB_PATH):
+        from paper_2502_02770_amd.build import build
+        build(verbose=False)
+    return T
+
+
+ONE = ctypes.c_void_p(4096)                                        # never dereferenced: the checks fail first
+PLENTY = 1 << 40
+
+
+def _kv(T, batch=2, hq=32, hkv=8, max_pages=16, pool=64, pools=True, bits=4):
+    kv = T.make_kv(batch, hq, hkv, max_pages, pool, None, None, quant_bits=bits)
+    kv.page_table = kv.seq_lens = 4096
+    if pools:
+        kv.k_pool = kv.v_pool = kv.kq_pool = kv.kq_meta = kv.page_minmax = 4096
+    return kv
+
+
+def test_attention_of_new_tokens_refuses(T):
+    L, kv = T.binding.lib(), _kv(T)
+    ref = ctypes.byref
+    tree = lambda kv=kv, q=ONE, max_new=8, mask=ONE, words=1, out=ONE, ws=ONE, n=PLENTY: L.twilight_tree_attention(
+        ref(kv), q, None, None, max_new, mask, words, out, None, ws, n, None)
+    win = lambda kv=kv, q=ONE, max_new=8, window=64, sinks=4, out=ONE, ws=ONE, n=PLENTY: L.twilight_window_attention(
+        ref(kv), q, None, None, max_new, window, sinks, out, None, ws, n, None)
+    for f in (tree, win):
+        assert f(q=None) == f(out=None) == f(max_new=0) == f(max_new=-1) == f(max_new=(1 << 20) + 1) == -1
+        assert f(ws=None) == f(n=16) == -2
+        assert f(kv=_kv(T, pools=False)) == -1
+        assert f(kv=_kv(T, max_pages=(1 << 26) + 1)) == -1
+        bad = _kv(T)
+        bad.head_dim = 64
+        assert f(kv=bad) == -1
+    assert tree(mask=None) == tree(words=0) == tree(max_new=33, words=1) == tree(max_new=1025, words=64) == -1
+    assert win(window=0) == win(window=-5) == win(sinks=-1) == -1
+    assert win(kv=_kv(T, batch=8000, hq=8, hkv=1), max_new=1 << 20) == -1       # rows beyond 31 bits
+    no_v = _kv(T)
+    no_v.v_pool = None
+    assert tree(kv=no_v) == win(kv=no_v) == -1
+
+
+def test_page_operators_refuse(T):
+    L, kv = T.binding.lib(), _kv(T)
+    ref = ctypes.byref
+    assert L.twilight_pages_reserve(ref(kv), None, 4, ONE, ONE, ONE, PLENTY, None) == -1
+    assert L.twilight_pages_reserve(ref(kv), ONE, 0, ONE, ONE, ONE, PLENTY, None) == -1
+    assert L.twilight_pages_reserve(ref(kv), ONE, 4, None, ONE, ONE, PLENTY, None) == -1
+    assert L.twilight_pages_reserve(ref(kv), ONE, 4, ONE, None, ONE, PLENTY, None) == -1
+    assert L.twilight_pages_reserve(ref(kv), ONE, 4, ONE, ONE, None, PLENTY, None) == -2
+    assert L.twilight_pages_reserve(ref(kv), ONE, 4, ONE, ONE, ONE, 8, None) == -2
+    for k in range(4):
+        args = [ONE] * 4
+        args[k] = None
+        assert L.twilight_pages_free(ref(kv), *args, None) == -1
+    fork = lambda parent=ONE, n=3, table=ctypes.c_void_p(8192), lens=ctypes.c_void_p(8192), rc=ONE, src=ONE, dst=ONE, st=ONE, ws=ONE, b=PLENTY: (
+        L.twilight_pages_fork(ref(kv), parent, n, table, lens, rc, src, dst, st, ws, b, None))
+    for name in ("parent", "table", "lens", "rc", "src", "dst", "st"):
+        assert fork(**{name: None}) == -1
+    assert fork(n=0) == fork(n=65535) == fork(table=ONE) == fork(lens=ONE) == -1      # in place: the old rows would be read after they change
+    assert fork(ws=None) == fork(b=8) == -2
+    assert L.twilight_pages_copy(ref(kv), None, ONE, 3, None) == L.twilight_pages_copy(ref(kv), ONE, None, 3, None) == -1
+    assert L.twilight_pages_copy(ref(kv), ONE, ONE, -1, None) == L.twilight_pages_copy(ref(kv), ONE, ONE, 1 << 30, None) == -1
+    assert L.twilight_pages_copy(ref(kv), ONE, ONE, 0, None) == 0
+    for k in (0, 1, 3):
+        args = [ONE, ONE, 4, ONE, None]
+        args[k] = None
+        assert L.twilight_tokens_compact(ref(kv), *args, None) == -1
+    assert L.twilight_tokens_compact(ref(kv), ONE, ONE, 0, ONE, None, None) == -1
+    assert L.twilight_tokens_compact(ref(_kv(T, pools=False)), ONE, ONE, 4, ONE, None, None) == -1
+    big = _kv(T, max_pages=(1 << 26) + 1)
+    assert L.twilight_pages_free(ref(big), ONE, ONE, ONE, ONE, None) == -1
+    assert L.twilight_tokens_compact(ref(big), ONE, ONE, 4, ONE, None, None) == -1
+    no_table = _kv(T)
+    no_table.page_table = None
+    assert L.twilight_pages_free(ref(no_table), ONE, ONE, ONE, ONE, None) == -1
+
+
+def test_workspace_sizes_of_the_new_operators(T):
+    kv = _kv(T)
+    assert T.twilight_workspace_bytes(T.TW_WS_NEW_TOKENS, kv, 0) == T.twilight_workspace_bytes(T.TW_WS_NEW_TOKENS, kv, (1 << 20) + 1) == 0
+    small, large = (T.twilight_workspace_bytes(T.TW_WS_NEW_TOKENS, kv, n) for n in (1, 64))
+    assert 0 < small < large
+    assert T.twilight_workspace_bytes(T.TW_WS_NEW_TOKENS, kv, 1 << 20) == large       # rows beyond a workgroup's do not count
+    # a count per row, and every page that can be asked for
+    assert T.twilight_workspace_bytes(T.TW_WS_PAGES, kv, 33, 0) >= 2 * 4 + 2 * 4 * 4
+    assert T.twilight_workspace_bytes(T.TW_WS_PAGES, kv, 0, 100) >= 100 * 4 + 64 * 4
+    assert T.twilight_workspace_bytes(T.TW_WS_PAGES, kv, 0, 65536) == 0
+
+
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 70])
+def test_mask_of_parents(n):
+    from paper_2502_02770_amd.cache import tree_mask_of_parents
+    rng = np.random.default_rng(n)
+    parents = np.stack([[int(rng.integers(-1, j)) if j else -1 for j in range(n)] for _ in range(3)])
+    got = tree_mask_of_parents(torch.from_numpy(parents)).numpy()
+    assert got.shape == (3, n, -(-n // 32)) and got.dtype == np.int32
+    for b in range(3):
+        for j in range(n):
+            see, k = set(), j
+            while k >= 0:
+                see.add(k)
+                k = int(parents[b, k])
+            bits = {w * 32 + i for w in range(got.shape[2]) for i in range(32) if int(got[b, j, w]) >> i & 1}
+            assert bits == see

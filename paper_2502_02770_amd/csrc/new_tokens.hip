@@ -32,11 +32,15 @@ typedef float tw_f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kScaleLog2 = 0.08838834764831845f * 1.4426950408889634f;   // log2(e) / sqrt(128)
 constexpr float kLn2n = 0.6931471805599453f;
 constexpr float kLow = -1e30f;                   // running maximum before any visible token: exp2(-inf - kLow) = 0
+constexpr float kGrowth = 8.f;                   // by how much (in powers of 2) a row's scores may exceed its m before m follows
 constexpr int TILE = 64, TILE_BYTES = TILE * 256;
 enum { MODE_TREE = 0, MODE_WINDOW = 1 };
 constexpr int PLAN_ROUNDS = 2;                   // items per resident workgroup at most, as planned
+constexpr long long COMBINE_FEW = 2048;          // rows of a launch up to which a workgroup joins one row's parts
 constexpr int PLAN_MIN_TILES = 2;                // shortest chunk of a list
-constexpr int PLAN_ITEM_TILES = 2;               // fixed cost of an item in tiles: its plan, page and query loads, its partial result
+// fixed cost of an item in tiles: its plan, page and query loads; its partial result of M rows, written and read again
+template <int M>
+constexpr int item_tiles() { return M / 16; }
 
 // rows of K and V that no token stands for (beyond the sequence's end, on an unmapped page) are read from here
 __device__ const uint4 tw_zero_row[16] = {};
@@ -92,6 +96,7 @@ __device__ __forceinline__ Span span_of(const NewArgs& a, int len, int p_lo, int
 // into the same number of chunks.
 struct Item {
   int b, rb, h, chunk, chunks, slot;
+  uint32_t items;                                // of the launch, where one wave's lanes hold all sequences (no need to look for a next one)
 };
 
 template <int MODE, int M>
@@ -102,74 +107,74 @@ __device__ __forceinline__ void lists_of(const NewArgs& a, int b, int* lists, in
   *tiles = blocks == 0 ? 0 : max(1, span_of<MODE>(a, len, len - min(n, M / a.G), len - 1).tiles);
 }
 
-__device__ __forceinline__ uint32_t quotient(unsigned long long x, uint32_t y) {   // at most 2^26, more tiles than a list has
-  const unsigned long long r = x >> 32 ? x / y : (unsigned long long)((uint32_t)x / y);
-  return r < (1ull << 26) ? (uint32_t)r : 1u << 26;
+// Sum over the 64 lanes, for all of them.
+__device__ __forceinline__ float wave_sum_f(float v) {
+  v = tw_row16_sum(v);
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), TW_DPP_BCAST15, 0xA, 0xF, false));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), TW_DPP_BCAST31, 0xC, 0xF, false));
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 // Chunk length in tiles for `grid` resident workgroups: of a few lengths that give every workgroup one or two items, the
-// one whose rounds are cheapest by the items that it really makes.  With c > total / (W r) there are fewer than W r + lists
-// items, and fewer than 2 W r of lists that are cut: what the launch's grid and the workspace are sized for.
+// one whose rounds are cheapest by the items that it makes.  With c > total / (W r) there are fewer than W r + lists
+// items, and fewer than 2 W r of lists that are cut: what the workspace is sized for.  (Sums in
+// fp32, a thousandth more than their errors added.)  Every workgroup does this before it knows its item, so few and short
+// steps: with exact quotients by integer division it took 3 us of the 10 us that a single chat's call runs.
+// lists, tiles: of this lane's sequence where 64 lanes hold them all.
 template <int MODE, int M>
-__device__ __forceinline__ int plan_chunk(const NewArgs& a, int lane) {
-  unsigned long long total = 0;
-  uint32_t lists_all = 0;
-  int lists = 0, tiles = 0;                      // of this lane's sequence, where 64 lanes hold them all
+__device__ __forceinline__ int plan_chunk(const NewArgs& a, int lane, int* lists, int* tiles) {
+  float total = 0.f, lists_all = 0.f;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    lists = tiles = 0;
-    if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, &lists, &tiles);
-    total += tw_readlane_u64(tw_wave_scan_u64((unsigned long long)lists * (unsigned)tiles), 63);
-    lists_all += (uint32_t)__builtin_amdgcn_readlane((int)tw_wave_scan_u32((uint32_t)lists), 63);
+    *lists = *tiles = 0;
+    if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, lists, tiles);
+    total += wave_sum_f((float)*lists * (float)*tiles);
+    lists_all += wave_sum_f((float)*lists);
   }
-  const uint32_t W = (uint32_t)a.grid;
-  uint32_t best = 0xFFFFFFFFu, chunk = PLAN_MIN_TILES;
-  for (uint32_t k = 0; k < 2u * PLAN_ROUNDS; ++k) {
-    const uint32_t r = 1u + (k >> 1), room = W * r > lists_all / 2u ? W * r - lists_all / 2u : 0u;
-    uint32_t c;
-    if (room == 0u) {
-      if (k + 1u < 2u * PLAN_ROUNDS || best != 0xFFFFFFFFu) continue;
-      c = quotient(total, W) + 1u;               // far more lists than workgroups: only the longest are cut
+  const float W = (float)a.grid;
+  total *= 1.001f;
+  if (total <= W * PLAN_MIN_TILES) return PLAN_MIN_TILES;
+  float best = __builtin_inff(), chunk = 0.f;
+  for (int k = 0; k < 2 * PLAN_ROUNDS; ++k) {
+    const float r = (float)(1 + (k >> 1));
+    const float room = W * r - 0.5f * lists_all;
+    float c;
+    if (room < 1.f) {
+      if (k + 1 < 2 * PLAN_ROUNDS || chunk > 0.f) continue;
+      c = __builtin_floorf(total / W) + 1.f;     // far more lists than workgroups: only the longest are cut
     } else {
-      c = quotient(total, room) + 1u;
-      if (k & 1u) c += c / 8u + 1u;
+      c = __builtin_floorf(total * 1.001f * __builtin_amdgcn_rcpf(room)) + 1.f;
+      if (k & 1) c = __builtin_ceilf(1.125f * c);
     }
-    c = max(c, (uint32_t)PLAN_MIN_TILES);
-    uint32_t items = 0;
+    c = __builtin_fminf(__builtin_fmaxf(c, (float)PLAN_MIN_TILES), (float)(1 << 26));
+    const float inv = __builtin_amdgcn_rcpf(c);
+    float items = 0.f;
     for (int b0 = 0; b0 < a.batch; b0 += 64) {
       if (a.batch > 64) {
-        lists = tiles = 0;
-        if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, &lists, &tiles);
+        *lists = *tiles = 0;
+        if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, lists, tiles);
       }
-      items += (uint32_t)__builtin_amdgcn_readlane((int)tw_wave_scan_u32((uint32_t)lists * (((uint32_t)tiles + c - 1u) / c)), 63);
+      items += wave_sum_f((float)*lists * __builtin_ceilf((float)*tiles * inv - 1e-4f));
     }
-    const uint32_t cost = (items + W - 1u) / W * (c + PLAN_ITEM_TILES);
+    const float cost = __builtin_ceilf(items / W - 1e-4f) * (c + (float)item_tiles<M>());
     if (cost < best) { best = cost; chunk = c; }
   }
   return (int)chunk;
 }
 
-// This workgroup's item; false: none.
-template <int MODE, int M, bool SPLIT>
-__device__ __forceinline__ bool find_item(const NewArgs& a, int lane, Item* it) {
-  if (!SPLIT) {                                  // row blocks from the last (longest under a causal mask) to the first
-    unsigned i = blockIdx.x;
-    it->h = (int)(i % (unsigned)a.Hkv); i /= (unsigned)a.Hkv;
-    it->b = (int)(i % (unsigned)a.batch);
-    it->rb = a.rb_max - 1 - (int)(i / (unsigned)a.batch);
-    it->chunk = 0; it->chunks = 1; it->slot = 0;
-    return it->rb * M < seq_new(a, it->b) * a.G;
-  }
-  const int chunk = plan_chunk<MODE, M>(a, lane);
+// Item `want` of a launch whose lists are cut into chunks of `chunk` tiles; false: there are fewer.
+template <int MODE, int M>
+__device__ __forceinline__ bool find_item(const NewArgs& a, int lane, int chunk, int lists, int tiles, uint32_t want, Item* it) {
   uint32_t items = 0, slots = 0;
-  const uint32_t want = blockIdx.x;
   bool found = false;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    int lists = 0, tiles = 0;
-    if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, &lists, &tiles);
+    if (a.batch > 64) {
+      lists = tiles = 0;
+      if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, &lists, &tiles);
+    }
     const int chunks = (tiles + chunk - 1) / chunk;
     const uint32_t mine = (uint32_t)(lists * chunks), part = chunks > 1 ? mine : 0u;
     const uint32_t ie = tw_wave_scan_u32(mine), se = tw_wave_scan_u32(part);
-    if (blockIdx.x == 0 && threadIdx.x < 64 && b0 + lane < a.batch) {   // for the combine kernel
+    if (want == 0 && threadIdx.x < 64 && b0 + lane < a.batch) {         // for the combine kernel
       a.ws_plan[2 * (b0 + lane)] = chunks;
       a.ws_plan[2 * (b0 + lane) + 1] = (int)(slots + se - part);
     }
@@ -187,7 +192,8 @@ __device__ __forceinline__ bool find_item(const NewArgs& a, int lane, Item* it) 
       it->h = (int)(rest - (uint32_t)it->rb * (uint32_t)a.Hkv);
       it->slot = (int)(slots + (uint32_t)__builtin_amdgcn_readlane((int)(se - part), l) + k);
       found = true;
-      if (blockIdx.x != 0) return true;
+      it->items = a.batch <= 64 ? (uint32_t)__builtin_amdgcn_readlane((int)ie, 63) : 0xFFFFFFFFu;
+      if (want != 0) return true;
     }
     items += (uint32_t)__builtin_amdgcn_readlane((int)ie, 63);
     slots += (uint32_t)__builtin_amdgcn_readlane((int)se, 63);
@@ -195,16 +201,23 @@ __device__ __forceinline__ bool find_item(const NewArgs& a, int lane, Item* it) 
   return found;
 }
 
-template <int MODE, int WR, int WT, bool SPLIT>
-__global__ __launch_bounds__(64 * WR * WT, WR * WT >= 4 ? 2 : 1) void new_tokens_kernel(NewArgs a) {
-  constexpr int NW = WR * WT, M = 32 * WR, MT = 2 / WT, PPW = 4 / NW;
-  __shared__ __align__(1024) unsigned char buf0[2 * TILE_BYTES];
-  __shared__ __align__(1024) unsigned char buf1[2 * TILE_BYTES];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const int wr = wave / WT, wt = wave % WT, half = lane >> 5;
+// Item of a launch that cuts nothing: row blocks from the last (longest under a causal mask) to the first.
+template <int M>
+__device__ __forceinline__ bool whole_item(const NewArgs& a, Item* it) {
+  unsigned i = blockIdx.x;
+  it->h = (int)(i % (unsigned)a.Hkv); i /= (unsigned)a.Hkv;
+  it->b = (int)(i % (unsigned)a.batch);
+  it->rb = a.rb_max - 1 - (int)(i / (unsigned)a.batch);
+  it->chunk = 0; it->chunks = 1; it->slot = 0;
+  return it->rb * M < seq_new(a, it->b) * a.G;
+}
 
-  Item it;
-  if (!find_item<MODE, M, SPLIT>(a, lane, &it)) return;
+// One item: a chunk of a list.
+template <int MODE, int WR, int WT, bool SPLIT>
+__device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, unsigned char (&buf0)[2 * TILE_BYTES], unsigned char (&buf1)[2 * TILE_BYTES],
+                                            int lane, int wave) {
+  constexpr int NW = WR * WT, M = 32 * WR, MT = 2 / WT, PPW = 4 / NW;
+  const int wr = wave / WT, wt = wave % WT, half = lane >> 5;
   const int b = __builtin_amdgcn_readfirstlane(it.b), rb = __builtin_amdgcn_readfirstlane(it.rb), h = __builtin_amdgcn_readfirstlane(it.h);
   const int n = __builtin_amdgcn_readfirstlane(seq_new(a, b)), len = __builtin_amdgcn_readfirstlane(seq_len(a, b));
   const int off = __builtin_amdgcn_readfirstlane(a.offsets ? a.offsets[b] : b * a.max_new);
@@ -304,6 +317,21 @@ __global__ __launch_bounds__(64 * WR * WT, WR * WT >= 4 ? 2 : 1) void new_tokens
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
   float m = kLow, l = 0.f;                       // m: of the whole row; l: of this lane's tokens
 
+  // the mask words of this lane's row that a tile's positions stand in, asked for ahead of the next tile's rows, so that they
+  // are not waited for behind those
+  struct Words { uint32_t w[3]; };
+  auto mask_words = [&](int u) -> Words {
+    Words x = {{0u, 0u, 0u}};
+    const int j0 = sp.tile(u) * TILE - ctx;      // draft token of the tile's first position
+    if (MODE == MODE_TREE && j0 > -TILE) {
+      const uint32_t* mrow = a.mask + (long long)(off + tok) * a.mask_words;
+      const int w0 = j0 >= 0 ? j0 >> 5 : 0;
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        if (w0 + k < a.mask_words) x.w[k] = mrow[w0 + k];
+    }
+    return x;
+  };
   auto held_pages = [&](int u) -> unsigned {     // of a tile: which of its four pages are mapped
     const int k = u - base;
     return (unsigned)(mapped[0] >> k & 1) | (unsigned)(mapped[1] >> k & 1) << 1 | (unsigned)(mapped[2] >> k & 1) << 2 | (unsigned)(mapped[3] >> k & 1) << 3;
@@ -312,7 +340,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR * WT >= 4 ? 2 : 1) void new_tokens
     __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): this wave's rows are in LDS
     __syncthreads();
   };
-  auto compute = [&](const unsigned char* buf, int u, unsigned held) {
+  auto compute = [&](const unsigned char* buf, int u, unsigned held, const Words& x) {
     const int t0 = sp.tile(u) * TILE;
     bool all = held == 15u && t0 + TILE <= len;
     if (MODE == MODE_TREE) {
@@ -322,34 +350,54 @@ __global__ __launch_bounds__(64 * WR * WT, WR * WT >= 4 ? 2 : 1) void new_tokens
       if (idle_wave || t0 > w_hi || (t0 + TILE - 1 <= w_lo - a.window && t0 >= a.sinks)) return;    // no row of the wave sees the tile
       all = all && t0 + TILE - 1 <= w_lo && (t0 > w_hi - a.window || t0 + TILE <= a.sinks);
     }
+    // K of the whole slice, then the products, each later operand's read behind a product; the first V operands come with
+    // the last products, so that they wait for nothing behind the softmax
     tw_f32x16 s[MT];
+    tw_bf16x8 kf[MT][8];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int st = 0; st < 8; ++st) kf[mt][st] = *(const tw_bf16x8*)(buf + k_rd[st] + mt * 32 * 256);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[mt][r] = 0.f;
 #pragma unroll
-      for (int st = 0; st < 8; ++st) {
-        const tw_bf16x8 kf = *(const tw_bf16x8*)(buf + k_rd[st] + mt * 32 * 256);
-        s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[mt], 0, 0, 0);
+      for (int st = 0; st < 8; ++st) s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[mt][st], qf[st], s[mt], 0, 0, 0);
+    }
+    union Frag { tw_s16x4 s[2]; tw_bf16x8 v; };
+    Frag vf[2 * MT][4];
+    auto read_v = [&](int ks) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        vf[ks][d].s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TW_LDS tw_s16x4*)(buf + v_rd[d] + ks * 4096));
+        vf[ks][d].s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TW_LDS tw_s16x4*)(buf + v_rd[d] + ks * 4096 + 2048));
       }
+    };
+    read_v(0);
+    read_v(1);
+    __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+    if (MT == 2) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
     if (!all) {
       unsigned long long vis;
       if (MODE == MODE_TREE) {
         vis = low_bits(ctx - t0);
-        const int j0 = t0 - ctx;                 // draft token of the tile's first position
+        const int j0 = t0 - ctx;
         if (j0 > -TILE) {
-          const uint32_t* mrow = a.mask + (long long)(off + tok) * a.mask_words;
-          const int w0 = j0 >= 0 ? j0 >> 5 : 0;
-          const uint32_t m0 = w0 < a.mask_words ? mrow[w0] : 0u, m1 = w0 + 1 < a.mask_words ? mrow[w0 + 1] : 0u;
-          const unsigned long long w = (unsigned long long)m1 << 32 | m0;
-          if (j0 >= 0) {
-            const int sh = j0 & 31;
-            const uint32_t m2 = w0 + 2 < a.mask_words ? mrow[w0 + 2] : 0u;
-            vis |= sh ? w >> sh | (unsigned long long)m2 << (64 - sh) : w;
-          } else {
-            vis |= w << -j0;
-          }
+          const unsigned long long w = (unsigned long long)x.w[1] << 32 | x.w[0];
+          const int sh = j0 & 31;
+          vis |= j0 < 0 ? w << -j0 : sh ? w >> sh | (unsigned long long)x.w[2] << (64 - sh) : w;
         }
         vis &= low_bits(len - t0);
       } else {
@@ -376,7 +424,7 @@ __global__ __launch_bounds__(64 * WR * WT, WR * WT >= 4 ? 2 : 1) void new_tokens
       mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
     }
     const float mn = fmaxf(m, mx * kScaleLog2);
-    if (__any(mn > m)) {                         // some row's maximum grew
+    if (__any(mn > m + kGrowth)) {
       const float al = __builtin_amdgcn_exp2f(m - mn);
       l *= al;
 #pragma unroll
@@ -395,15 +443,11 @@ __global__ __launch_bounds__(64 * WR * WT, WR * WT >= 4 ? 2 : 1) void new_tokens
         p[2 * mt + r / 8][r % 8] = (__bf16)w;
       }
 #pragma unroll
+    for (int ks = 2; ks < 2 * MT; ++ks) read_v(ks);
+#pragma unroll
     for (int ks = 0; ks < 2 * MT; ++ks)
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const tw_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TW_LDS tw_s16x4*)(buf + v_rd[d] + ks * 4096));
-        const tw_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TW_LDS tw_s16x4*)(buf + v_rd[d] + ks * 4096 + 2048));
-        union { tw_s16x4 s[2]; tw_bf16x8 v; } f;
-        f.s[0] = lo; f.s[1] = hi;
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, p[ks], o[d], 0, 0, 0);
-      }
+      for (int d = 0; d < 4; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ks][d].v, p[ks], o[d], 0, 0, 0);
   };
 
   if (u0 < u1) {
@@ -413,16 +457,18 @@ __global__ __launch_bounds__(64 * WR * WT, WR * WT >= 4 ? 2 : 1) void new_tokens
     for (int u = u0; u < u1; u += 2) {
       arrived();                                 // the tile's rows, for every wave; nobody reads the other buffer any more
       unsigned held = held_pages(u);
+      Words x = mask_words(u);
       if (u + 1 < u1) issue(buf1, u + 1);
-      compute(buf0, u, held);
+      compute(buf0, u, held, x);
       if (u + 1 >= u1) break;
       arrived();
       held = held_pages(u + 1);
+      x = mask_words(u + 1);
       if (u + 2 < u1) {
         if (u + 2 - base >= 64) { base = u + 2; refill(base); }
         issue(buf0, u + 2);
       }
-      compute(buf1, u + 1, held);
+      compute(buf1, u + 1, held, x);
     }
   }
 
@@ -479,44 +525,78 @@ __global__ __launch_bounds__(64 * WR * WT, WR * WT >= 4 ? 2 : 1) void new_tokens
   if (half == 0) a.ws_ml[prow] = make_float2(m, l);
 }
 
-// One wave per (sequence, new token, query head) whose list was cut: two half waves of 32 lanes x 4 dims fold every other
-// partial result.
-template <int M>
+// SPLIT: resident workgroups stride over the items (workgroups beyond those would wait for a slot to find out that there is
+// nothing left for them); otherwise a workgroup per list.
+template <int MODE, int WR, int WT, bool SPLIT>
+__global__ __launch_bounds__(64 * WR * WT, WR * WT >= 4 ? 2 : 1) void new_tokens_kernel(NewArgs a) {
+  constexpr int M = 32 * WR;
+  __shared__ __align__(1024) unsigned char buf0[2 * TILE_BYTES];
+  __shared__ __align__(1024) unsigned char buf1[2 * TILE_BYTES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  Item it;
+  if (!SPLIT) {
+    if (whole_item<M>(a, &it)) attend_item<MODE, WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave);
+    return;
+  }
+  int lists, tiles;
+  const int chunk = plan_chunk<MODE, M>(a, lane, &lists, &tiles);
+  uint32_t want = blockIdx.x;
+  while (find_item<MODE, M>(a, lane, chunk, lists, tiles, want, &it)) {
+    attend_item<MODE, WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave);
+    want += gridDim.x;
+    if (want >= it.items) break;
+    __syncthreads();                             // the buffers have been read
+  }
+}
+
+// The parts of cut lists joined.  A row (new token, head) is folded by LANES half waves of 32 lanes x 4 dims: two (a wave; four
+// rows to a workgroup) where there are many rows, eight (a workgroup) where few rows have many parts each and the wait
+// for one part after the other is what counts: 256 rows of 32 parts 4.0 us with eight, 8.3 us with two.
+template <int M, int LANES>
 __global__ __launch_bounds__(256) void new_tokens_combine_kernel(NewArgs a) {
-  const int lane = threadIdx.x & 63, half = lane >> 5, dl = lane & 31;
-  const int b = blockIdx.y, idx = blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int ROWS = 8 / LANES;
+  const int lane = threadIdx.x & 63, dl = lane & 31, part = (threadIdx.x >> 5) % LANES;
+  const int b = blockIdx.y, idx = (int)(blockIdx.x * ROWS + threadIdx.x / (32 * LANES));
+  const int n = seq_new(a, b);
   const int tok = idx / a.Hq, head = idx - tok * a.Hq;
-  if (tok >= seq_new(a, b)) return;
   const int chunks = a.ws_plan[2 * b];
   if (chunks <= 1) return;                       // written by the attention kernel itself
-  const int n = seq_new(a, b), blocks = (n * a.G + M - 1) / M, h = head >> a.lgG;
-  const int row = tok * a.G + (head & (a.G - 1)), rb = row / M;
+  const bool live = tok < n;
+  const int blocks = (n * a.G + M - 1) / M, row = min(tok, n - 1) * a.G + (head & (a.G - 1));
   const long long step = (long long)blocks * a.Hkv * M;
-  long long at = ((long long)a.ws_plan[2 * b + 1] + rb * a.Hkv + h) * M + row % M + half * step;
+  long long at = ((long long)a.ws_plan[2 * b + 1] + (row / M) * a.Hkv + (head >> a.lgG)) * M + row % M + part * step;
   float m = kLow, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int c = half; c < chunks; c += 2, at += 2 * step) {
-    const float2 ml = a.ws_ml[at];
-    const float4 v = ((const float4*)a.ws_acc)[at * 32 + dl];
-    const float mn = fmaxf(m, ml.x), so = __builtin_amdgcn_exp2f(m - mn), sn = __builtin_amdgcn_exp2f(ml.x - mn);
-    l = l * so + ml.y * sn;
+  auto join = [&](float m2, float l2, const float4& v) {
+    const float mn = fmaxf(m, m2), so = __builtin_amdgcn_exp2f(m - mn), sn = __builtin_amdgcn_exp2f(m2 - mn);
+    l = l * so + l2 * sn;
     o.x = o.x * so + v.x * sn; o.y = o.y * so + v.y * sn; o.z = o.z * so + v.z * sn; o.w = o.w * so + v.w * sn;
     m = mn;
+  };
+#pragma unroll 4
+  for (int c = part; c < chunks; c += LANES, at += LANES * step) {
+    const float2 ml = a.ws_ml[at];
+    join(ml.x, ml.y, ((const float4*)a.ws_acc)[at * 32 + dl]);
   }
-  const float m2 = __shfl_xor(m, 32), l2 = __shfl_xor(l, 32), mn = fmaxf(m, m2);
-  const float s0 = __builtin_amdgcn_exp2f(m - mn), s1 = __builtin_amdgcn_exp2f(m2 - mn);
-  l = l * s0 + l2 * s1;
-  o.x = o.x * s0 + __shfl_xor(o.x, 32) * s1; o.y = o.y * s0 + __shfl_xor(o.y, 32) * s1;
-  o.z = o.z * s0 + __shfl_xor(o.z, 32) * s1; o.w = o.w * s0 + __shfl_xor(o.w, 32) * s1;
+  join(__shfl_xor(m, 32), __shfl_xor(l, 32), make_float4(__shfl_xor(o.x, 32), __shfl_xor(o.y, 32), __shfl_xor(o.z, 32), __shfl_xor(o.w, 32)));
+  if (LANES == 8) {
+    __shared__ float4 so4[4][32];
+    __shared__ float2 sml[4];
+    const int wave = threadIdx.x >> 6;
+    if (lane < 32) so4[wave][dl] = o;
+    if (lane == 0) sml[wave] = make_float2(m, l);
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) join(sml[w].x, sml[w].y, so4[w][dl]);
+  }
+  if (!live || (lane >> 5)) return;
   const long long qrow = (long long)((a.offsets ? a.offsets[b] : b * a.max_new) + tok) * a.Hq + head;
   const float inv = l > 0.f ? 1.0f / l : 0.f;
-  if (half == 0) {
-    union { __bf16 e[4]; uint2 v; } w;
-    w.e[0] = (__bf16)(o.x * inv); w.e[1] = (__bf16)(o.y * inv); w.e[2] = (__bf16)(o.z * inv); w.e[3] = (__bf16)(o.w * inv);
-    a.out[qrow * 32 + dl] = w.v;
-    if (a.lse && lane == 0) a.lse[qrow] = l > 0.f ? (mn + __log2f(l)) * kLn2n : -__builtin_inff();
-  }
+  union { __bf16 e[4]; uint2 v; } w;
+  w.e[0] = (__bf16)(o.x * inv); w.e[1] = (__bf16)(o.y * inv); w.e[2] = (__bf16)(o.z * inv); w.e[3] = (__bf16)(o.w * inv);
+  a.out[qrow * 32 + dl] = w.v;
+  if (a.lse && lane == 0) a.lse[qrow] = l > 0.f ? (m + __log2f(l)) * kLn2n : -__builtin_inff();
 }
 
 // ---------------------------------------------------------------- host side
@@ -540,10 +620,16 @@ int launch_new(NewArgs a, bool cut, long long lists, hipStream_t s) {
     return tw_prof_after(s);
   }
   a.grid = plan_grid();
-  TW_LAUNCH((new_tokens_kernel<MODE, WR, WT, true>), dim3((unsigned)(a.grid * PLAN_ROUNDS + lists)), dim3(64 * WR * WT), 0, s, a);
+  // no more workgroups than items that the longest lists could make
+  long long longest = ((long long)a.max_pages * TW_PAGE + TILE - 1) / TILE;
+  if (MODE == MODE_WINDOW) longest = min(longest, ((long long)a.sinks + TILE - 1) / TILE + ((long long)a.window + M / a.G + TILE - 2) / TILE + 1);
+  const long long most = lists * ((longest + PLAN_MIN_TILES - 1) / PLAN_MIN_TILES);
+  TW_LAUNCH((new_tokens_kernel<MODE, WR, WT, true>), dim3((unsigned)min(most, (long long)a.grid)), dim3(64 * WR * WT), 0, s, a);
   if (int e = tw_prof_after(s)) return e;
   tw_prof_before(TW_K_NEW_COMBINE, s);
-  TW_LAUNCH((new_tokens_combine_kernel<M>), dim3((unsigned)(((long long)a.max_new * a.Hq + 3) / 4), (unsigned)a.batch), dim3(256), 0, s, a);
+  const long long rows = (long long)a.max_new * a.Hq;
+  if (rows * a.batch <= COMBINE_FEW) TW_LAUNCH((new_tokens_combine_kernel<M, 8>), dim3((unsigned)rows, (unsigned)a.batch), dim3(256), 0, s, a);
+  else TW_LAUNCH((new_tokens_combine_kernel<M, 2>), dim3((unsigned)((rows + 3) / 4), (unsigned)a.batch), dim3(256), 0, s, a);
   return tw_prof_after(s);
 }
 

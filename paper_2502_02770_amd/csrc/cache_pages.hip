@@ -117,45 +117,75 @@ __device__ __forceinline__ void reserve_range(const PagesArgs& a, int b, int* lo
   *hi = n ? (int)min((long long)a.max_pages, ((long long)len + n + TW_PAGE - 1) / TW_PAGE) : *lo;
 }
 
+// Unmapped entries among [lo, hi) of row b; a lane has a row of its own, and ranges longer than SHORT are looked through by the
+// whole wave, one after the other.
+constexpr int SHORT = 2;
+__device__ __forceinline__ int unmapped_in(const PagesArgs& a, int b, int lo, int hi, int lane) {
+  int n = 0;
+  if (hi - lo <= SHORT)
+    for (int p = lo; p < hi; ++p) n += (unsigned)a.table[(long long)b * a.max_pages + p] >= a.pool_pages;
+  for (unsigned long long rest = __ballot(hi - lo > SHORT); rest; rest &= rest - 1) {
+    const int l = __builtin_ctzll(rest), bl = __builtin_amdgcn_readlane(b, l), from = __builtin_amdgcn_readlane(lo, l), to = __builtin_amdgcn_readlane(hi, l);
+    int sum = 0;
+    for (int p0 = from; p0 < to; p0 += 64) {
+      const int p = p0 + lane;
+      sum += __popcll(__ballot(p < to && (unsigned)a.table[(long long)bl * a.max_pages + min(p, to - 1)] >= a.pool_pages));
+    }
+    if (lane == l) n = sum;
+  }
+  return n;
+}
+
 // Hands out pages: one workgroup, since the order of the pages is one chain of prefix sums.  Requests are counted row by
 // row, the counts searched from page 0 until there are as many free pages as requests, the pages dealt out by rank.
 // FORK: request i is copy_src[i] >= 0, the entry that row i's partly filled page stands in.  Otherwise (reserve): the
-// unmapped entries of a row's range, a wave per row.
+// unmapped entries of a row's range.  Bound by the trips to memory one after the other and, in a large pool, by what one CU
+// reads (a pass of the search reads 64 KiB, the next one's counts are asked for before a pass is looked at).  Rows go to
+// the waves in turn, so that few long ranges are not one wave's; the requests before each row and the pages found stay in
+// LDS while they fit.
+constexpr int TAKE_LDS = 4096;
 template <bool FORK>
 __global__ __launch_bounds__(TAKE_THREADS) void pages_take_kernel(PagesArgs a) {
   __shared__ uint32_t wsum[16];
+  __shared__ int s_before[TAKE_LDS], s_found[TAKE_LDS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int rows = FORK ? a.new_batch : a.batch;
-  // ---- requests before each row
+  int* before = rows <= TAKE_LDS ? s_before : a.ws_before;
+  auto counts_of = [&](unsigned base, int* c) {  // of page base + 64 * (16 * wave + k) + lane
+    const unsigned p0 = base + (unsigned)wave * (64 * TAKE_STEPS) + (unsigned)lane;
+#pragma unroll
+    for (int k = 0; k < TAKE_STEPS; ++k) c[k] = p0 + 64u * k < a.pool_pages ? a.ref[p0 + 64u * k] : 1;
+  };
+  int c[TAKE_STEPS], next[TAKE_STEPS];
+  counts_of(0, next);
+  // ---- requests before each row; a thread's row in round j is TAKE_THREADS j + 16 * lane + wave
   if (!FORK) {
-    for (int b = wave; b < rows; b += TAKE_WAVES) {
-      int lo, hi, n = 0;
-      reserve_range(a, b, &lo, &hi);
-      for (int p0 = lo; p0 < hi; p0 += 64) {
-        const int p = p0 + lane;
-        n += __popcll(__ballot(p < hi && (unsigned)a.table[(long long)b * a.max_pages + min(p, hi - 1)] >= a.pool_pages));
-      }
-      if (lane == 0) a.ws_before[b] = n;
+    for (int b0 = 0; b0 < rows; b0 += TAKE_THREADS) {
+      const int b = b0 + lane * TAKE_WAVES + wave;
+      int lo = 0, hi = 0;
+      if (b < rows) reserve_range(a, b, &lo, &hi);
+      const int n = unmapped_in(a, b, lo, hi, lane);
+      if (b < rows) before[b] = n;
     }
     __syncthreads();
   }
   uint32_t total = 0;
   for (int b0 = 0; b0 < rows; b0 += TAKE_THREADS) {
     const int b = b0 + tid;
-    const uint32_t n = b < rows ? (FORK ? (uint32_t)(a.copy_src[b] >= 0) : (uint32_t)a.ws_before[b]) : 0u;
+    const uint32_t n = b < rows ? (FORK ? (uint32_t)(a.copy_src[b] >= 0) : (uint32_t)before[b]) : 0u;
     uint32_t sum;
     const uint32_t upto = tw_block_scan_u32(n, wsum, &sum);
-    if (b < rows) a.ws_before[b] = (int)(total + upto - n);
+    if (b < rows) before[b] = (int)(total + upto - n);
     total += sum;
   }
   if (total == 0) return;
+  int* list = total <= (uint32_t)TAKE_LDS ? s_found : a.ws_found;
   // ---- the lowest free pages
   uint32_t found = 0;
   for (unsigned base = 0; base < a.pool_pages && found < total; base += TAKE_PASS) {
-    const unsigned p0 = base + (unsigned)wave * (64 * TAKE_STEPS) + (unsigned)lane;
-    int c[TAKE_STEPS];
 #pragma unroll
-    for (int k = 0; k < TAKE_STEPS; ++k) c[k] = p0 + 64u * k < a.pool_pages ? a.ref[p0 + 64u * k] : 1;
+    for (int k = 0; k < TAKE_STEPS; ++k) c[k] = next[k];
+    counts_of(base + TAKE_PASS, next);
     uint32_t mine = 0;
 #pragma unroll
     for (int k = 0; k < TAKE_STEPS; ++k) mine += (uint32_t)__popcll(__ballot(c[k] == 0));
@@ -165,12 +195,13 @@ __global__ __launch_bounds__(TAKE_THREADS) void pages_take_kernel(PagesArgs a) {
 #pragma unroll
     for (int w = 0; w < TAKE_WAVES; ++w) { const uint32_t x = wsum[w]; rank += w < wave ? x : 0u; all += x; }
     __syncthreads();
-    if (mine) {
+    if (mine && rank < total) {
+      const unsigned p0 = base + (unsigned)wave * (64 * TAKE_STEPS) + (unsigned)lane;
 #pragma unroll
       for (int k = 0; k < TAKE_STEPS; ++k) {
         const unsigned long long f = __ballot(c[k] == 0);
         const uint32_t r = rank + tw_bits_below(f);
-        if (c[k] == 0 && r < total) { a.ws_found[r] = (int)(p0 + 64u * k); a.ref[p0 + 64u * k] = 1; }
+        if (c[k] == 0 && r < total) { list[r] = (int)(p0 + 64u * k); a.ref[p0 + 64u * k] = 1; }
         rank += (uint32_t)__popcll(f);
       }
     }
@@ -182,9 +213,9 @@ __global__ __launch_bounds__(TAKE_THREADS) void pages_take_kernel(PagesArgs a) {
   if (FORK) {
     for (int i = tid; i < rows; i += TAKE_THREADS) {
       if (a.copy_src[i] < 0) continue;
-      const uint32_t r = (uint32_t)a.ws_before[i];
+      const uint32_t r = (uint32_t)before[i];
       if (r < found) {
-        const int id = a.ws_found[r];
+        const int id = list[r];
         a.copy_dst[i] = id;
         a.new_table[(long long)i * a.max_pages + a.new_lens[i] / TW_PAGE] = id;
       } else {
@@ -193,17 +224,27 @@ __global__ __launch_bounds__(TAKE_THREADS) void pages_take_kernel(PagesArgs a) {
     }
     return;
   }
-  for (int b = wave; b < rows; b += TAKE_WAVES) {
-    int lo, hi;
-    reserve_range(a, b, &lo, &hi);
-    uint32_t r = lo < hi ? (uint32_t)a.ws_before[b] : 0u;
-    for (int p0 = lo; p0 < hi; p0 += 64) {
-      const int p = p0 + lane;
-      int32_t* e = a.table + (long long)b * a.max_pages + min(p, hi - 1);
-      const unsigned long long want = __ballot(p < hi && (unsigned)*e >= a.pool_pages);
-      const uint32_t k = r + tw_bits_below(want);
-      if (want >> lane & 1ull) *e = k < found ? a.ws_found[k] : -1;
-      r += (uint32_t)__popcll(want);
+  for (int b0 = 0; b0 < rows; b0 += TAKE_THREADS) {
+    const int b = b0 + lane * TAKE_WAVES + wave;
+    int lo = 0, hi = 0;
+    uint32_t r = 0;
+    if (b < rows) { reserve_range(a, b, &lo, &hi); r = (uint32_t)before[b]; }
+    if (hi - lo <= SHORT)
+      for (int p = lo; p < hi; ++p) {
+        int32_t* e = a.table + (long long)b * a.max_pages + p;
+        if ((unsigned)*e >= a.pool_pages) { *e = r < found ? list[r] : -1; ++r; }
+      }
+    for (unsigned long long rest = __ballot(hi - lo > SHORT); rest; rest &= rest - 1) {
+      const int l = __builtin_ctzll(rest), bl = __builtin_amdgcn_readlane(b, l), from = __builtin_amdgcn_readlane(lo, l), to = __builtin_amdgcn_readlane(hi, l);
+      uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)r, l);
+      for (int p0 = from; p0 < to; p0 += 64) {
+        const int p = p0 + lane;
+        int32_t* e = a.table + (long long)bl * a.max_pages + min(p, to - 1);
+        const unsigned long long want = __ballot(p < to && (unsigned)*e >= a.pool_pages);
+        const uint32_t k = at + tw_bits_below(want);
+        if (want >> lane & 1ull) *e = k < found ? list[k] : -1;
+        at += (uint32_t)__popcll(want);
+      }
     }
   }
 }

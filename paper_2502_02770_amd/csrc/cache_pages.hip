@@ -289,143 +289,135 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(RowsArgs a) {
   if (to) *to = z;
 }
 
-// Compaction.  The pieces of a row do not depend on each other, so the columns of a sequence's rows go to five
-// workgroups per KV head: K and V in halves of 128 bytes, codes with (scale, zero).  A workgroup takes the destination
-// positions in steps of 128 (8 whole pages): to another table every step is a workgroup of its own; in place one
-// workgroup walks them all, and reads a step's rows before it writes them - destinations lie at or before their
-// sources, so no step overwrites what a later one reads.
-constexpr int STEP = 128;
-constexpr int CODE_UNITS = STEP * 9 / 256 + 1;   // 16-byte pieces of a step's codes and (scale, zero) per thread, at most
-
+// Compaction.  A workgroup takes WAVES destination pages of a KV head at a time, a wave each: the 16 rows of K, V, codes and
+// (scale, zero), all loads before the stores; which row moves where is looked up once per token, through LDS.  To another
+// table every step is a workgroup of its own.  In place one workgroup walks all steps of a (sequence, KV head), reads a
+// step's rows before it writes them (one barrier, behind the loads) - destinations lie at or before their sources, so no
+// step overwrites what a later one reads - and looks up the next step's moves meanwhile.
 __device__ __forceinline__ void hold(uint4& x) { asm volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w)); }
 
 // Source and destination row (page * 16 + slot, of the pools without their head index) of destination position t; -1: none.
 struct Move { int src, dst; };
 template <bool INPLACE>
-__device__ __forceinline__ Move move_of(const RowsArgs& a, int b, int t, int start, int end, int len) {
+__device__ __forceinline__ Move move_of(const RowsArgs& a, int b, long long t, int start, int end, int len) {
   Move m = {-1, -1};
-  if (t >= end || t >= a.max_pages * TW_PAGE) return m;
+  if (t >= end) return m;
   const long long row = (long long)b * a.max_pages;
   const int dp = (INPLACE ? a.table : a.to)[row + t / TW_PAGE];
+  const int s = t >= start ? a.keep[(long long)b * a.stride + (t - start)] : -1;
   if ((unsigned)dp >= a.pool_pages) return m;
-  m.dst = dp * TW_PAGE + t % TW_PAGE;
-  if (t < start) return m;
-  const int s = a.keep[(long long)b * a.stride + (t - start)];
+  m.dst = dp * TW_PAGE + (int)(t % TW_PAGE);
   if (s < 0 || s >= len) return m;
   const int sp = a.table[row + s / TW_PAGE];
   if ((unsigned)sp < a.pool_pages) m.src = sp * TW_PAGE + s % TW_PAGE;
   return m;
 }
 
-template <bool INPLACE>
-__global__ __launch_bounds__(256) void compact_kernel(RowsArgs a) {
-  const int col = (int)(blockIdx.x % 5u), h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// The smaller (larger) of a lane's value and that of the lane 32 or 16 away.
+template <int DIST>
+__device__ __forceinline__ void fold_bounds(float& lo, float& hi) {
+  if (DIST == 32) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(lo), __float_as_uint(lo), false, false);
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(hi), __float_as_uint(hi), false, false);
+    lo = fminf(__uint_as_float(x[0]), __uint_as_float(x[1])); hi = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+  } else {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(lo), __float_as_uint(lo), false, false);
+    const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(hi), __float_as_uint(hi), false, false);
+    lo = fminf(__uint_as_float(x[0]), __uint_as_float(x[1])); hi = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+  }
+}
+
+template <bool INPLACE, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void compact_kernel(RowsArgs a) {
+  constexpr int STEP = WAVES * TW_PAGE;
+  __shared__ Move moves[2][STEP];
+  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int start = a.start[b];
   if (start < 0) return;
   const int len = max(0, min(a.seq_lens[b], a.max_pages * TW_PAGE));
-  const int end = (int)min((long long)start + max(0, min(a.count[b], a.stride)), 0x7FFFFF00ll);
-  int t0 = start & ~(TW_PAGE - 1);
-  int last = end;
-  if (!INPLACE) {
-    const long long at = (long long)t0 + (long long)(blockIdx.x / 5u) * STEP;
-    if (at >= end) return;
-    t0 = (int)at;
-    last = t0 + 1;
-  }
-  last = min(last, a.max_pages * TW_PAGE);
+  const int end = (int)min((long long)start + max(0, min(a.count[b], a.stride)), (long long)a.max_pages * TW_PAGE);
+  long long t0 = start & ~(TW_PAGE - 1);
+  if (!INPLACE) t0 += (long long)blockIdx.x * STEP;
+  if (t0 >= end) return;
   // row (page, slot) of head h in a pool of `pieces` 16-byte pieces per row
   auto at = [&](int r, int pieces) -> long long { return (((long long)(r / TW_PAGE) * a.Hkv + h) * TW_PAGE + r % TW_PAGE) * pieces; };
-
-  if (col < 4) {
-    uint4* pool = col < 2 ? a.k : a.v;
-    if (!pool) return;
-    const int piece = (col & 1) * 8 + (lane & 7);
-    const bool bounds = col < 2 && a.bounds;
-    for (; t0 < last; t0 += STEP) {
-      // a wave holds two pages: four pieces per lane, tokens 16 j + 8 i + lane / 8 (j page, i half of it)
-      Move m[4];
-      uint4 x[4];
+  // a whole cache packed into other pages does not stay in the caches: K and V marked non-temporal both ways (4 x 16384 tokens, half
+  // kept, 8 KV heads: 61.0 -> 52.3 us); the few rows of a draft are read again by the next step
+  auto load = [](const uint4* p) -> uint4 { return INPLACE ? *p : tw_ld_stream(p); };
+  auto store = [](uint4* p, const uint4& x) { if (INPLACE) *p = x; else tw_st_stream(p, x); };
+  if (tid < STEP) moves[0][tid] = move_of<INPLACE>(a, b, t0 + tid, start, end, len);
+  __syncthreads();
+  const int piece = lane & 15, sub = lane >> 4;  // K and V: load j takes rows 4 j + sub; codes and (scale, zero): row lane % 16
+  for (int turn = 0;; turn ^= 1) {
+    const Move* mv = moves[turn] + wave * TW_PAGE;
+    Move m[4];
+    uint4 k[4], v[4], c[2], z;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        m[u] = move_of<INPLACE>(a, b, t0 + wave * 32 + u * 8 + (lane >> 3), start, end, len);
-        const int r = m[u].src >= 0 ? m[u].src : bounds ? m[u].dst : -1;       // rows that stay count for the bounds
-        x[u] = make_uint4(0u, 0u, 0u, 0u);
-        if (r >= 0) x[u] = pool[at(r, 16) + piece];
-      }
-      if (INPLACE) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) hold(x[u]);  // every load of the step has returned
-        __syncthreads();
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (m[u].src >= 0) pool[at(m[u].dst, 16) + piece] = x[u];
-      if (bounds) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float lo[8], hi[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) { lo[k] = __builtin_inff(); hi[k] = -__builtin_inff(); }
-          bool any = false;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int u = 2 * j + i;
-            if (m[u].dst < 0) continue;
-            any = true;
-            float f[8];
-            tw_unpack8(x[u], f);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) { lo[k] = fminf(lo[k], f[k]); hi[k] = fmaxf(hi[k], f[k]); }
-          }
-#pragma unroll
-          for (int s = 8; s < 64; s <<= 1)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) { lo[k] = fminf(lo[k], __shfl_xor(lo[k], s)); hi[k] = fmaxf(hi[k], __shfl_xor(hi[k], s)); }
-          if (!__ballot(any)) continue;
-          // the page's first position is held by lanes 0..7, and is a token whenever any of the page is
-          if (lane < 8) {
-            const long long page = (long long)(m[2 * j].dst / TW_PAGE) * a.Hkv + h;
-            uint32_t w[8];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              w[k] = (__float_as_uint(lo[2 * k]) >> 16) | (__float_as_uint(lo[2 * k + 1]) & 0xFFFF0000u);
-              w[4 + k] = (__float_as_uint(hi[2 * k]) >> 16) | (__float_as_uint(hi[2 * k + 1]) & 0xFFFF0000u);
-            }
-            a.bounds[page * 32 + piece] = make_uint4(w[0], w[1], w[2], w[3]);
-            a.bounds[page * 32 + 16 + piece] = make_uint4(w[4], w[5], w[6], w[7]);
-          }
-        }
-      }
+    for (int j = 0; j < 4; ++j) {
+      m[j] = mv[4 * j + sub];
+      const int r = m[j].src >= 0 ? m[j].src : a.bounds ? m[j].dst : -1;       // rows that stay count for the bounds
+      k[j] = v[j] = make_uint4(0u, 0u, 0u, 0u);
+      if (r >= 0) k[j] = load(a.k + at(r, 16) + piece);
+      if (m[j].src >= 0 && a.v) v[j] = load(a.v + at(m[j].src, 16) + piece);
     }
-    return;
-  }
-  // codes (bits pieces per row) and (scale, zero) (one piece)
-  const int pieces = a.bits + 1;
-  for (; t0 < last; t0 += STEP) {
-    uint4 x[CODE_UNITS];
-    uint4* to[CODE_UNITS];
+    const Move mc = mv[piece];
 #pragma unroll
-    for (int u = 0; u < CODE_UNITS; ++u) {
-      const int unit = tid + 256 * u, tok = unit / pieces, pc = unit - tok * pieces;
-      to[u] = nullptr;
-      x[u] = make_uint4(0u, 0u, 0u, 0u);
-      if (tok >= STEP) continue;
-      const Move m = move_of<INPLACE>(a, b, t0 + tok, start, end, len);
-      if (m.src < 0) continue;
-      if (pc < a.bits) {
-        if (a.codes) { x[u] = a.codes[at(m.src, a.bits) + pc]; to[u] = a.codes + at(m.dst, a.bits) + pc; }
-      } else if (a.meta) {
-        x[u] = a.meta[at(m.src, 1)]; to[u] = a.meta + at(m.dst, 1);
-      }
+    for (int i = 0; i < 2; ++i) {
+      c[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (mc.src >= 0 && a.codes && sub + 4 * i < a.bits) c[i] = a.codes[at(mc.src, a.bits) + sub + 4 * i];
     }
+    z = make_uint4(0u, 0u, 0u, 0u);
+    if (mc.src >= 0 && a.meta && sub == 0) z = a.meta[at(mc.src, 1)];
+    const bool more = INPLACE && t0 + STEP < end;
     if (INPLACE) {
+      if (more && tid < STEP) moves[turn ^ 1][tid] = move_of<INPLACE>(a, b, t0 + STEP + tid, start, end, len);
 #pragma unroll
-      for (int u = 0; u < CODE_UNITS; ++u) hold(x[u]);
+      for (int j = 0; j < 4; ++j) { hold(k[j]); hold(v[j]); }                  // every load of the step has returned
+      hold(c[0]); hold(c[1]); hold(z);
       __syncthreads();
     }
 #pragma unroll
-    for (int u = 0; u < CODE_UNITS; ++u)
-      if (to[u]) *to[u] = x[u];
+    for (int j = 0; j < 4; ++j)
+      if (m[j].src >= 0) {
+        store(a.k + at(m[j].dst, 16) + piece, k[j]);
+        if (a.v) store(a.v + at(m[j].dst, 16) + piece, v[j]);
+      }
+    if (mc.src >= 0) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (a.codes && sub + 4 * i < a.bits) a.codes[at(mc.dst, a.bits) + sub + 4 * i] = c[i];
+      if (a.meta && sub == 0) a.meta[at(mc.dst, 1)] = z;
+    }
+    // the wave's page: its first position is a token whenever any of it is
+    const int first = __builtin_amdgcn_readfirstlane(m[0].dst);
+    if (a.bounds && first >= 0) {
+      float lo[8], hi[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { lo[i] = __builtin_inff(); hi[i] = -__builtin_inff(); }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float f[8];
+        tw_unpack8(k[j], f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          lo[i] = fminf(lo[i], m[j].dst >= 0 ? f[i] : __builtin_inff());
+          hi[i] = fmaxf(hi[i], m[j].dst >= 0 ? f[i] : -__builtin_inff());
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { fold_bounds<32>(lo[i], hi[i]); fold_bounds<16>(lo[i], hi[i]); }
+      if (sub < 2) {                             // lanes 0..15 the lower bounds, 16..31 the upper ones
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = __float_as_uint(sub ? hi[2 * i] : lo[2 * i]), y = __float_as_uint(sub ? hi[2 * i + 1] : lo[2 * i + 1]);
+          w[i] = x >> 16 | (y & 0xFFFF0000u);
+        }
+        a.bounds[((long long)(first / TW_PAGE) * a.Hkv + h) * 32 + lane] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    if (!more) return;
+    t0 += STEP;
   }
 }
 
@@ -536,11 +528,11 @@ extern "C" int twilight_tokens_compact(const twilight_kv_t* kv, const int32_t* k
   RowsArgs a = rows_args(kv, d);
   a.table = kv->page_table; a.to = dst_table; a.seq_lens = kv->seq_lens;
   a.keep = keep_idx; a.count = keep_count; a.start = dst_start; a.stride = keep_stride;
-  const long long most = min((long long)keep_stride, (long long)d.max_pages * TW_PAGE) + TW_PAGE - 1;
-  const unsigned steps = (unsigned)((most + STEP - 1) / STEP);
+  const long long most = min((long long)keep_stride, (long long)d.max_pages * TW_PAGE) + TW_PAGE - 1;   // positions from a page's start on
   const bool in_place = !dst_table || dst_table == kv->page_table;
   tw_prof_before(TW_K_COMPACT, s);
-  if (in_place) TW_LAUNCH((compact_kernel<true>), dim3(5, (unsigned)d.Hkv, (unsigned)d.batch), dim3(256), 0, s, a);
-  else TW_LAUNCH((compact_kernel<false>), dim3(5 * steps, (unsigned)d.Hkv, (unsigned)d.batch), dim3(256), 0, s, a);
+  if (!in_place) TW_LAUNCH((compact_kernel<false, 4>), dim3((unsigned)((most + 63) / 64), (unsigned)d.Hkv, (unsigned)d.batch), dim3(256), 0, s, a);
+  else if (most <= 8 * TW_PAGE) TW_LAUNCH((compact_kernel<true, 8>), dim3(1, (unsigned)d.Hkv, (unsigned)d.batch), dim3(512), 0, s, a);
+  else TW_LAUNCH((compact_kernel<true, 16>), dim3(1, (unsigned)d.Hkv, (unsigned)d.batch), dim3(1024), 0, s, a);
   return tw_prof_after(s);
 }

@@ -36,11 +36,8 @@ constexpr float kGrowth = 8.f;                   // by how much (in powers of 2)
 constexpr int TILE = 64, TILE_BYTES = TILE * 256;
 enum { MODE_TREE = 0, MODE_WINDOW = 1 };
 constexpr int PLAN_ROUNDS = 2;                   // items per resident workgroup at most, as planned
-constexpr long long COMBINE_FEW = 2048;          // rows of a launch up to which a workgroup joins one row's parts
 constexpr int PLAN_MIN_TILES = 2;                // shortest chunk of a list
-// fixed cost of an item in tiles: its plan, page and query loads; its partial result of M rows, written and read again
-template <int M>
-constexpr int item_tiles() { return M / 16; }
+constexpr long long COMBINE_FEW = 2048;          // rows of a launch up to which a workgroup joins one row's parts
 
 // rows of K and V that no token stands for (beyond the sequence's end, on an unmapped page) are read from here
 __device__ const uint4 tw_zero_row[16] = {};
@@ -59,7 +56,7 @@ struct NewArgs {
   int32_t* ws_plan;            // [batch][2]: chunks of the sequence's lists, first partial result
   float2* ws_ml;
   float* ws_acc;
-  int batch, Hq, Hkv, G, lgG, max_pages, max_new, mask_words, window, sinks, rb_max, grid;
+  int batch, Hq, Hkv, G, lgG, max_pages, max_new, mask_words, window, sinks, rb_max, cus;
   unsigned pool_pages;
 };
 
@@ -115,50 +112,60 @@ __device__ __forceinline__ float wave_sum_f(float v) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
-// Chunk length in tiles for `grid` resident workgroups: of a few lengths that give every workgroup one or two items, the
-// one whose rounds are cheapest by the items that it makes.  With c > total / (W r) there are fewer than W r + lists
-// items, and fewer than 2 W r of lists that are cut: what the workspace is sized for.  (Sums in
-// fp32, a thousandth more than their errors added.)  Every workgroup does this before it knows its item, so few and short
-// steps: with exact quotients by integer division it took 3 us of the 10 us that a single chat's call runs.
+// Chunk length in tiles, for W = 2 workgroups per CU: lists whole, or cut into lengths that give every workgroup one or two
+// items, or, with far more lists than workgroups, cut down to a workgroup's share of the tiles.  The cheapest, counted in the
+// time of a tile beside another workgroup on the CU (128 rows 1.7 us, 32 rows from HBM 2.8 us): per round the chunk (0.8 of
+// it where no CU has two: 1.1 to 1.5 us a tile) and 2 for plan, queries and first rows; where lists are cut 1.5 more for the
+// launch that joins the parts, and 2e-4 per item and row for parts of 528 bytes a row, written and read.  With c > total / (W r)
+// there are fewer than W r + lists items, and fewer than 2 W r of lists that are cut: what the workspace is sized for.
+// (Sums in fp32, a thousandth more than their errors added.)  Every workgroup does this before it knows its item, so in
+// few and short steps: with exact quotients by integer division it took 3 us of the 10 us that a single chat's call runs.
 // lists, tiles: of this lane's sequence where 64 lanes hold them all.
 template <int MODE, int M>
 __device__ __forceinline__ int plan_chunk(const NewArgs& a, int lane, int* lists, int* tiles) {
-  float total = 0.f, lists_all = 0.f;
+  constexpr float kJoin = 1.5f, kPart = 2e-4f * M;
+  float total = 0.f, lists_all = 0.f, longest = 0.f;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     *lists = *tiles = 0;
     if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, lists, tiles);
     total += wave_sum_f((float)*lists * (float)*tiles);
     lists_all += wave_sum_f((float)*lists);
+    longest = __builtin_fmaxf(longest, tw_wave_max_f((float)*tiles));
   }
-  const float W = (float)a.grid;
+  const float cus = (float)a.cus, W = 2.f * cus;
   total *= 1.001f;
-  if (total <= W * PLAN_MIN_TILES) return PLAN_MIN_TILES;
-  float best = __builtin_inff(), chunk = 0.f;
-  for (int k = 0; k < 2 * PLAN_ROUNDS; ++k) {
-    const float r = (float)(1 + (k >> 1));
-    const float room = W * r - 0.5f * lists_all;
-    float c;
-    if (room < 1.f) {
-      if (k + 1 < 2 * PLAN_ROUNDS || chunk > 0.f) continue;
-      c = __builtin_floorf(total / W) + 1.f;     // far more lists than workgroups: only the longest are cut
-    } else {
-      c = __builtin_floorf(total * 1.001f * __builtin_amdgcn_rcpf(room)) + 1.f;
-      if (k & 1) c = __builtin_ceilf(1.125f * c);
-    }
-    c = __builtin_fminf(__builtin_fmaxf(c, (float)PLAN_MIN_TILES), (float)(1 << 26));
-    const float inv = __builtin_amdgcn_rcpf(c);
-    float items = 0.f;
-    for (int b0 = 0; b0 < a.batch; b0 += 64) {
-      if (a.batch > 64) {
-        *lists = *tiles = 0;
-        if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, lists, tiles);
+  auto cost_of = [&](float items, float c) { return __builtin_ceilf(items / W - 1e-4f) * (c * (items <= cus ? 0.8f : 1.f) + 2.f); };
+  float best = cost_of(lists_all, longest), chunk = longest;
+  if (total <= W * PLAN_MIN_TILES) {             // little work: the shortest chunks, if any
+    const float items = total / PLAN_MIN_TILES;
+    if (cost_of(items, PLAN_MIN_TILES) + kJoin + items * kPart < best) chunk = PLAN_MIN_TILES;
+  } else {
+    for (int k = 0; k < 3; ++k) {                // one item per workgroup, somewhat fewer, two
+      const float room = W * (k == 2 ? 2.f : 1.f) - 0.5f * lists_all;
+      float c;
+      if (room < 1.f) {
+        if (k) continue;
+        c = __builtin_floorf(total * 1.001f / W) + 1.f;
+      } else {
+        c = __builtin_floorf(total * 1.001f * __builtin_amdgcn_rcpf(room)) + 1.f;
+        if (k == 1) c = __builtin_ceilf(1.125f * c);
       }
-      items += wave_sum_f((float)*lists * __builtin_ceilf((float)*tiles * inv - 1e-4f));
+      c = __builtin_fmaxf(c, (float)PLAN_MIN_TILES);
+      if (c >= longest) continue;                // the same as whole lists
+      const float inv = __builtin_amdgcn_rcpf(c);
+      float items = 0.f;
+      for (int b0 = 0; b0 < a.batch; b0 += 64) {
+        if (a.batch > 64) {
+          *lists = *tiles = 0;
+          if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, lists, tiles);
+        }
+        items += wave_sum_f((float)*lists * __builtin_ceilf((float)*tiles * inv - 1e-4f));
+      }
+      const float cost = cost_of(items, c) + kJoin + items * kPart;
+      if (cost < best) { best = cost; chunk = c; }
     }
-    const float cost = __builtin_ceilf(items / W - 1e-4f) * (c + (float)item_tiles<M>());
-    if (cost < best) { best = cost; chunk = c; }
   }
-  return (int)chunk;
+  return (int)__builtin_fminf(__builtin_fmaxf(chunk, 1.f), (float)(1 << 26));
 }
 
 // Item `want` of a launch whose lists are cut into chunks of `chunk` tiles; false: there are fewer.
@@ -201,13 +208,15 @@ __device__ __forceinline__ bool find_item(const NewArgs& a, int lane, int chunk,
   return found;
 }
 
-// Item of a launch that cuts nothing: row blocks from the last (longest under a causal mask) to the first.
+// Item of a launch that cuts nothing: the row blocks of a (sequence, KV head) one after the other, as they read the same rows (64
+// drafts of 128 tokens over 2048, four row blocks each: 433 us with all sequences' last blocks ahead of their others), from
+// the last (longest under a causal mask) to the first.
 template <int M>
 __device__ __forceinline__ bool whole_item(const NewArgs& a, Item* it) {
   unsigned i = blockIdx.x;
   it->h = (int)(i % (unsigned)a.Hkv); i /= (unsigned)a.Hkv;
-  it->b = (int)(i % (unsigned)a.batch);
-  it->rb = a.rb_max - 1 - (int)(i / (unsigned)a.batch);
+  it->rb = a.rb_max - 1 - (int)(i % (unsigned)a.rb_max);
+  it->b = (int)(i / (unsigned)a.rb_max);
   it->chunk = 0; it->chunks = 1; it->slot = 0;
   return it->rb * M < seq_new(a, it->b) * a.G;
 }
@@ -411,7 +420,10 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
       for (int mt = 0; mt < MT; ++mt) {
         const uint32_t w = (uint32_t)(vis >> (32 * mt));
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[mt][r] = w >> (8 * (r / 4) + r % 4) & 1u ? s[mt][r] : -__builtin_inff();
+        for (int r = 0; r < 16; ++r) {           // the row's bit, spread over a word, chooses the score or -inf: two instructions
+          const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)w, 8 * (r / 4) + r % 4, 1);
+          s[mt][r] = __uint_as_float((keep & __float_as_uint(s[mt][r])) | (~keep & 0xFF800000u));
+        }
       }
     }
     float mx = s[0][0];
@@ -602,29 +614,33 @@ __global__ __launch_bounds__(256) void new_tokens_combine_kernel(NewArgs a) {
 // ---------------------------------------------------------------- host side
 int rows_per_block(long long rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
-// Workgroups that the plan counts on: 64 KiB of LDS each, two to a CU.
-int plan_grid() { return 2 * tw_num_cus(); }
-
-// Lists that fill the chip by themselves are not cut: the row blocks of a chunk or prompt under a window.
-bool cut_lists(const TwDims& d, bool window, long long max_new, int M) {
-  const long long blocks = (max_new * d.G + M - 1) / M;
-  return !(window && blocks >= 8 && blocks * d.batch * d.Hkv >= 2ll * tw_num_cus());
+// Lists that cannot be long are not cut, which saves the launch that joins the parts and their way through memory: up to 6 tiles,
+// one more for every 32 lists, at most 32.  Few lists run no faster whole than cut from there on; many would leave CUs idle
+// only where few of them are as long as the longest may be.  us, cut / whole, by tiles of all lists:
+//   32 rows    8 lists  4: 10.9 /  8.3  6: 10.9 / 10.2  8: 10.9 / 12.2     160 lists   8: 18.7 / 15.0  16: 25.5 / 26.1  24: 36.2 / 44.0
+//   64         8        6: 11.1 /  9.5  8: 11.2 / 10.9 12: 11.4 / 14.1     160        12: 23.9 / 19.1  16: 28.3 / 24.8  24: 39.6 / 41.9
+//   128        8        6: 12.6 / 11.6  8: 12.8 / 13.9                     160        12: 35.4 / 22.2  16: 42.0 / 31.2  24: 50.5 / 48.5
+//   32       512       16: 51.7 / 51.5 24: 79.1 / 73.4 32: 100.6 / 94.8
+// Nor are the row blocks of chunks and prompts under a window that fill the chip by themselves: their lists are alike.
+bool cut_lists(bool window, int blocks, long long lists, long long longest) {
+  if (longest <= min(32ll, 6 + lists / 32)) return false;
+  return !(window && blocks >= 8 && lists >= 2ll * tw_num_cus());
 }
 
 template <int MODE, int WR, int WT>
-int launch_new(NewArgs a, bool cut, long long lists, hipStream_t s) {
+int launch_new(NewArgs a, hipStream_t s) {
   constexpr int M = 32 * WR;
+  const long long lists = (long long)a.rb_max * a.batch * a.Hkv;
+  long long longest = ((long long)a.max_pages * TW_PAGE + TILE - 1) / TILE;      // tiles that a list can have
+  if (MODE == MODE_WINDOW) longest = min(longest, ((long long)a.sinks + TILE - 1) / TILE + ((long long)a.window + M / a.G + TILE - 2) / TILE + 1);
   tw_prof_before(TW_K_NEW_TOKENS, s);
-  if (MODE == MODE_WINDOW && !cut) {
-    TW_LAUNCH((new_tokens_kernel<MODE_WINDOW, WR, WT, false>), dim3((unsigned)lists), dim3(64 * WR * WT), 0, s, a);
+  if (!cut_lists(MODE == MODE_WINDOW, a.rb_max, lists, longest)) {
+    TW_LAUNCH((new_tokens_kernel<MODE, WR, WT, false>), dim3((unsigned)lists), dim3(64 * WR * WT), 0, s, a);
     return tw_prof_after(s);
   }
-  a.grid = plan_grid();
-  // no more workgroups than items that the longest lists could make
-  long long longest = ((long long)a.max_pages * TW_PAGE + TILE - 1) / TILE;
-  if (MODE == MODE_WINDOW) longest = min(longest, ((long long)a.sinks + TILE - 1) / TILE + ((long long)a.window + M / a.G + TILE - 2) / TILE + 1);
+  // resident workgroups (64 KiB of LDS each, two to a CU), no more than the lists could make items
   const long long most = lists * ((longest + PLAN_MIN_TILES - 1) / PLAN_MIN_TILES);
-  TW_LAUNCH((new_tokens_kernel<MODE, WR, WT, true>), dim3((unsigned)min(most, (long long)a.grid)), dim3(64 * WR * WT), 0, s, a);
+  TW_LAUNCH((new_tokens_kernel<MODE, WR, WT, true>), dim3((unsigned)min(most, 2ll * a.cus)), dim3(64 * WR * WT), 0, s, a);
   if (int e = tw_prof_after(s)) return e;
   tw_prof_before(TW_K_NEW_COMBINE, s);
   const long long rows = (long long)a.max_new * a.Hq;
@@ -633,6 +649,8 @@ int launch_new(NewArgs a, bool cut, long long lists, hipStream_t s) {
   return tw_prof_after(s);
 }
 
+size_t part_slots() { return (size_t)tw_num_cus() * 4 * PLAN_ROUNDS; }          // parts that a plan can make
+
 size_t align256n(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
@@ -640,7 +658,7 @@ size_t align256n(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t tw_new_tokens_workspace(const TwDims& d, int max_new) {
   if (max_new <= 0 || max_new > TW_MAX_NEW) return 0;
   const int M = rows_per_block((long long)max_new * d.G);
-  const size_t slots = (size_t)plan_grid() * 2 * PLAN_ROUNDS;
+  const size_t slots = part_slots();
   return align256n((size_t)d.batch * 8) + align256n(slots * M * 8) + slots * M * 512;
 }
 
@@ -657,28 +675,27 @@ static int new_tokens_impl(const twilight_kv_t* kv, const void* q, const int32_t
   a.q = (const uint4*)q; a.k_pool = (const char*)kv->k_pool; a.v_pool = (const char*)kv->v_pool;
   a.page_table = kv->page_table; a.seq_lens = kv->seq_lens; a.n_new = n_new; a.offsets = new_offsets; a.mask = mask;
   a.out = (uint2*)out; a.lse = lse;
-  const size_t slots = (size_t)plan_grid() * 2 * PLAN_ROUNDS;
+  const size_t slots = part_slots();
   a.ws_plan = (int32_t*)ws;
   a.ws_ml = (float2*)((char*)ws + align256n((size_t)d.batch * 8));
   a.ws_acc = (float*)((char*)a.ws_ml + align256n(slots * M * 8));
   a.batch = d.batch; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.G; a.lgG = __builtin_ctz(d.G); a.max_pages = d.max_pages;
   a.max_new = max_new; a.mask_words = mask_words; a.window = window; a.sinks = sinks; a.pool_pages = (unsigned)d.pool_pages;
-  a.rb_max = (int)(((long long)max_new * d.G + M - 1) / M); a.grid = 0;
+  a.rb_max = (int)(((long long)max_new * d.G + M - 1) / M); a.cus = tw_num_cus();
   const long long lists = (long long)a.rb_max * d.batch * d.Hkv;
   if (lists > (1ll << 30) || (long long)max_new * d.Hq >= (1ll << 31) || (long long)max_new * d.batch >= (1ll << 31)) return TW_EINVAL;
-  const bool cut = cut_lists(d, !tree, max_new, M);
   hipStream_t s = (hipStream_t)stream;
   if (tree) {
     switch (M) {
-      case 32: return launch_new<MODE_TREE, 1, 2>(a, cut, lists, s);
-      case 64: return launch_new<MODE_TREE, 2, 2>(a, cut, lists, s);
-      default: return launch_new<MODE_TREE, 4, 1>(a, cut, lists, s);
+      case 32: return launch_new<MODE_TREE, 1, 2>(a, s);
+      case 64: return launch_new<MODE_TREE, 2, 2>(a, s);
+      default: return launch_new<MODE_TREE, 4, 1>(a, s);
     }
   }
   switch (M) {
-    case 32: return launch_new<MODE_WINDOW, 1, 2>(a, cut, lists, s);
-    case 64: return launch_new<MODE_WINDOW, 2, 2>(a, cut, lists, s);
-    default: return launch_new<MODE_WINDOW, 4, 1>(a, cut, lists, s);
+    case 32: return launch_new<MODE_WINDOW, 1, 2>(a, s);
+    case 64: return launch_new<MODE_WINDOW, 2, 2>(a, s);
+    default: return launch_new<MODE_WINDOW, 4, 1>(a, s);
   }
 }
 

@@ -136,9 +136,11 @@ __device__ __forceinline__ int plan_chunk(const NewArgs& a, int lane, int* lists
   total *= 1.001f;
   auto cost_of = [&](float items, float c) { return __builtin_ceilf(items / W - 1e-4f) * (c * (items <= cus ? 0.8f : 1.f) + 2.f); };
   float best = cost_of(lists_all, longest), chunk = longest;
-  if (total <= W * PLAN_MIN_TILES) {             // little work: the shortest chunks, if any
-    const float items = total / PLAN_MIN_TILES;
-    if (cost_of(items, PLAN_MIN_TILES) + kJoin + items * kPart < best) chunk = PLAN_MIN_TILES;
+  if (total <= W * PLAN_MIN_TILES) {             // little work: the length where chunk and parts cost the same, short of the shortest none
+    // (parts at half their price: they do not fill the memory's time)
+    const float c = __builtin_fmaxf((float)PLAN_MIN_TILES, __builtin_floorf(__builtin_amdgcn_sqrtf(0.5f * kPart * total) + 0.5f));
+    const float items = total * __builtin_amdgcn_rcpf(c);
+    if (cost_of(items, c) + kJoin + items * (0.5f * kPart) < best) chunk = c;
   } else {
     for (int k = 0; k < 3; ++k) {                // one item per workgroup, somewhat fewer, two
       const float room = W * (k == 2 ? 2.f : 1.f) - 0.5f * lists_all;

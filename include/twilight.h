@@ -383,10 +383,17 @@ int twilight_sparse_decode_per_head(const twilight_kv_t* kv, const void* q, cons
  *   new_offsets    i32 [batch]; NULL = b * max_new
  *   max_new        host: upper bound of n_new[] (sizes the launch and the
  *                  workspace); at most 2^20, max_new * batch < 2^31;
- *                  max_pages_per_seq <= 2^26
- *   out            bf16 [rows][num_q_heads][128]; rows of no token are left
+ *                  max_pages_per_seq <= 2^24; row blocks (of 32, 64 or 128
+ *                  rows of new tokens x heads of a group) x batch x
+ *                  num_kv_heads < 2^24
+ *   out            bf16 [rows][num_q_heads][128], not overlapping q; rows of no
+ *                  token are left
  *   lse            fp32 [rows][num_q_heads] or NULL, as twilight_sparse_decode
- *   ws             >= twilight_workspace_bytes(TW_WS_NEW_TOKENS, kv, max_new, 0)
+ *   ws             >= twilight_workspace_bytes(TW_WS_NEW_TOKENS, kv, max_new, 0),
+ *                  for one call at a time
+ * q, out, ws and the pools are 16-byte aligned (TW_EINVAL).  The values of V
+ * that a token of the batch sees have to be finite, whichever tokens see them
+ * (a weight of 0 times an infinity is no number).
  *
  * twilight_tree_attention: a tree of drafted tokens.  Every new token sees the
  * tokens before the first new one, and of the new ones those whose bits are
@@ -425,7 +432,7 @@ int twilight_window_attention(const twilight_kv_t* kv, const void* q, const int3
  * TW_STATUS_POOL_EXHAUSTED.  Entries outside [0, num_pool_pages) are unmapped.
  * Only kv's shape, page_table and seq_lens are used by the first three; they
  * write kv->page_table (twilight_pages_fork does not).  max_pages_per_seq <=
- * 2^26.
+ * 2^24.
  *
  * twilight_pages_reserve: every unmapped entry among the pages that hold the
  * positions seq_lens[b] .. seq_lens[b] + n_new[b] - 1 gets a page (seq_lens

@@ -99,6 +99,19 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _on_gpu(t, dtype):
+    """Pointer of a tensor of this type on the current device (whose stream the call is given)."""
+    if t is None:
+        return None
+    assert t.dtype == dtype and t.is_cuda and t.is_contiguous() and t.get_device() == torch._C._cuda_getDevice(), \
+        "contiguous %s tensor on the current device required" % dtype
+    return t.data_ptr()
+
+
+def _ints(t):
+    return _on_gpu(t, torch.int32)
+
+
 def _stream():
     """The current stream of the current device, without the Stream object around it: a decode step of a short sequence
     takes about as long on the device as its two calls take here."""
@@ -216,41 +229,41 @@ def twilight_sparse_decode_per_head(kv, q, kept_count, kept_idx, kept_stride, ou
 
 
 def twilight_tree_attention(kv, q, n_new, new_offsets, max_new, tree_mask, mask_words, out, lse, ws):
-    _check(lib().twilight_tree_attention(ctypes.byref(kv), _ptr(q), _ptr(n_new), _ptr(new_offsets), int(max_new),
-                                         _ptr(tree_mask), int(mask_words), _ptr(out), _ptr(lse), _ptr(ws),
-                                         ws.numel() * ws.element_size(), _stream()))
+    _check(lib().twilight_tree_attention(ctypes.byref(kv), _on_gpu(q, torch.bfloat16), _ints(n_new), _ints(new_offsets), int(max_new),
+                                         _ints(tree_mask), int(mask_words), _on_gpu(out, torch.bfloat16), _on_gpu(lse, torch.float32),
+                                         _ptr(ws), ws.numel() * ws.element_size(), _stream()))
 
 
 def twilight_window_attention(kv, q, n_new, new_offsets, max_new, window, num_sinks, out, lse, ws):
-    _check(lib().twilight_window_attention(ctypes.byref(kv), _ptr(q), _ptr(n_new), _ptr(new_offsets), int(max_new),
-                                           int(window), int(num_sinks), _ptr(out), _ptr(lse), _ptr(ws),
-                                           ws.numel() * ws.element_size(), _stream()))
+    _check(lib().twilight_window_attention(ctypes.byref(kv), _on_gpu(q, torch.bfloat16), _ints(n_new), _ints(new_offsets), int(max_new),
+                                           int(window), int(num_sinks), _on_gpu(out, torch.bfloat16), _on_gpu(lse, torch.float32),
+                                           _ptr(ws), ws.numel() * ws.element_size(), _stream()))
 
 
 def twilight_pages_reserve(kv, n_new, max_new, ref_count, status, ws):
-    _check(lib().twilight_pages_reserve(ctypes.byref(kv), _ptr(n_new), int(max_new), _ptr(ref_count), _ptr(status),
+    _check(lib().twilight_pages_reserve(ctypes.byref(kv), _ints(n_new), int(max_new), _ints(ref_count), _ints(status),
                                         _ptr(ws), ws.numel() * ws.element_size(), _stream()))
 
 
 def twilight_pages_free(kv, first_page, end_page, ref_count, status):
-    _check(lib().twilight_pages_free(ctypes.byref(kv), _ptr(first_page), _ptr(end_page), _ptr(ref_count), _ptr(status),
+    _check(lib().twilight_pages_free(ctypes.byref(kv), _ints(first_page), _ints(end_page), _ints(ref_count), _ints(status),
                                      _stream()))
 
 
 def twilight_pages_fork(kv, parent, new_batch, new_table, new_lens, ref_count, copy_src, copy_dst, status, ws):
-    _check(lib().twilight_pages_fork(ctypes.byref(kv), _ptr(parent), int(new_batch), _ptr(new_table), _ptr(new_lens),
-                                     _ptr(ref_count), _ptr(copy_src), _ptr(copy_dst), _ptr(status), _ptr(ws),
+    _check(lib().twilight_pages_fork(ctypes.byref(kv), _ints(parent), int(new_batch), _ints(new_table), _ints(new_lens),
+                                     _ints(ref_count), _ints(copy_src), _ints(copy_dst), _ints(status), _ptr(ws),
                                      ws.numel() * ws.element_size(), _stream()))
 
 
 def twilight_pages_copy(kv, copy_src, copy_dst, n_copy):
-    _check(lib().twilight_pages_copy(ctypes.byref(kv), _ptr(copy_src), _ptr(copy_dst), int(n_copy), _stream()))
+    _check(lib().twilight_pages_copy(ctypes.byref(kv), _ints(copy_src), _ints(copy_dst), int(n_copy), _stream()))
 
 
 def twilight_tokens_compact(kv, keep_idx, keep_count, keep_stride, dst_start, dst_table):
     """dst_table None: in place."""
-    _check(lib().twilight_tokens_compact(ctypes.byref(kv), _ptr(keep_idx), _ptr(keep_count), int(keep_stride),
-                                         _ptr(dst_start), _ptr(dst_table), _stream()))
+    _check(lib().twilight_tokens_compact(ctypes.byref(kv), _ints(keep_idx), _ints(keep_count), int(keep_stride),
+                                         _ints(dst_start), _ints(dst_table), _stream()))
 
 
 def twilight_decode_plan(kv, which=TW_WS_DECODE, dense=False):

@@ -45,6 +45,17 @@ class PagedKV:
         self.append(k, v, start, self.seq_lens, offs, int(self.seq_lens.max().item()))
 
 
+    def over(self, page_table, seq_lens):
+        """A cache of another batch over the same pools (rows of a fork, a larger or smaller batch)."""
+        c = object.__new__(PagedKV)
+        c.__dict__.update(self.__dict__)
+        c.page_table = page_table.to(self.device, torch.int32).contiguous()
+        c.seq_lens = seq_lens.to(self.device, torch.int32).contiguous()
+        c.batch, c.max_pages = c.page_table.shape
+        c.kv = B.make_kv(c.batch, c.Hq, c.Hkv, c.max_pages, c.num_pool_pages, c.page_table, c.seq_lens, c.k_pool, c.v_pool,
+                         c.kq_pool, c.kq_meta, c.page_minmax, quant_bits=c.quant_bits)
+        return c
+
     def copy_pages(self, src, dst):
         """twilight_pages_copy: whole pages src[i] -> dst[i] of this layer; negative entries are passed over."""
         B.twilight_pages_copy(self.kv, src, dst, src.numel())
@@ -65,6 +76,12 @@ class PagePool:
         self.ref_count = torch.bincount(held, minlength=cache.num_pool_pages).to(torch.int32)
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
         self._ws = {}
+
+    def over(self, cache):
+        """The same pool for a cache of another batch (PagedKV.over): counts and status are shared."""
+        p = object.__new__(PagePool)
+        p.cache, p.ref_count, p.status, p._ws = cache, self.ref_count, self.status, {}
+        return p
 
     def _workspace(self, max_new, new_batch):
         if (max_new, new_batch) not in self._ws:
@@ -87,7 +104,7 @@ class PagePool:
 
     def fork(self, parent):
         """-> (new_table, new_lens, copy_src, copy_dst) of the batch whose row i continues row parent[i]; every layer then
-        copies the pairs (PagedKV.copy_pages)."""
+        copies the pairs (PagedKV.copy_pages) and goes on over the new table (PagedKV.over, and PagePool.over)."""
         c, n = self.cache, parent.numel()
         i32 = dict(dtype=torch.int32, device=c.device)
         table, lens = torch.empty(n, c.max_pages, **i32), torch.empty(n, **i32)

@@ -264,13 +264,12 @@ struct RowsArgs {
   const int32_t* keep;
   const int32_t* count;
   const int32_t* start;
-  int batch, Hkv, bits, max_pages, stride;
+  int batch, Hkv, bits, max_pages, stride, n_copy;
   unsigned pool_pages;
 };
 
-// One workgroup per (pair, KV head): 4096 + 4096 + 256 * bits + 256 + 512 bytes, all loads before the stores.  HBM.
-__global__ __launch_bounds__(256) void pages_copy_kernel(RowsArgs a) {
-  const int h = (int)(blockIdx.x % (unsigned)a.Hkv), i = (int)(blockIdx.x / (unsigned)a.Hkv), tid = threadIdx.x;
+// A (pair, KV head): 4096 + 4096 + 256 * bits + 256 + 512 bytes by one workgroup, all loads before the stores.  HBM.
+__device__ __forceinline__ void copy_page(const RowsArgs& a, int i, int h, int tid) {
   const int s = a.src[i], d = a.dst[i];
   if ((unsigned)s >= a.pool_pages || (unsigned)d >= a.pool_pages || s == d) return;
   const long long sp = (long long)s * a.Hkv + h, dp = (long long)d * a.Hkv + h;
@@ -287,6 +286,10 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(RowsArgs a) {
   if (a.k) a.k[dp * 256 + tid] = x;
   if (a.v) a.v[dp * 256 + tid] = y;
   if (to) *to = z;
+}
+__global__ __launch_bounds__(256) void pages_copy_kernel(RowsArgs a) {
+  const long long all = (long long)a.n_copy * a.Hkv;
+  for (long long i = blockIdx.x; i < all; i += gridDim.x) copy_page(a, (int)(i / a.Hkv), (int)(i % a.Hkv), (int)threadIdx.x);
 }
 
 // Compaction.  A workgroup takes WAVES destination pages of a KV head at a time, a wave each: the 16 rows of K, V, codes and
@@ -499,6 +502,10 @@ extern "C" int twilight_pages_fork(const twilight_kv_t* kv, const int32_t* paren
   return tw_prof_after(s);
 }
 
+static bool pools_aligned(const twilight_kv_t* kv) {           // rows move in pieces of 16 bytes
+  return !(((uintptr_t)kv->k_pool | (uintptr_t)kv->v_pool | (uintptr_t)kv->kq_pool | (uintptr_t)kv->kq_meta | (uintptr_t)kv->page_minmax) & 15);
+}
+
 static RowsArgs rows_args(const twilight_kv_t* kv, const TwDims& d) {
   RowsArgs a = {};
   a.k = (uint4*)kv->k_pool; a.v = (uint4*)kv->v_pool; a.codes = (uint4*)kv->kq_pool; a.meta = (uint4*)kv->kq_meta; a.bounds = (uint4*)kv->page_minmax;
@@ -509,13 +516,13 @@ static RowsArgs rows_args(const twilight_kv_t* kv, const TwDims& d) {
 extern "C" int twilight_pages_copy(const twilight_kv_t* kv, const int32_t* copy_src, const int32_t* copy_dst, int32_t n_copy, void* stream) {
   TwDims d;
   if (int e = check_pages(kv, &d)) return e;
-  if (!copy_src || !copy_dst || n_copy < 0 || (long long)n_copy * d.Hkv > 0x7FFFFFFFll) return TW_EINVAL;
+  if (!copy_src || !copy_dst || n_copy < 0 || !pools_aligned(kv)) return TW_EINVAL;
   if (n_copy == 0) return TW_OK;
   hipStream_t s = (hipStream_t)stream;
   RowsArgs a = rows_args(kv, d);
-  a.src = copy_src; a.dst = copy_dst;
+  a.src = copy_src; a.dst = copy_dst; a.n_copy = n_copy;
   tw_prof_before(TW_K_PAGES_COPY, s);
-  TW_LAUNCH(pages_copy_kernel, dim3((unsigned)(n_copy * d.Hkv)), dim3(256), 0, s, a);
+  TW_LAUNCH(pages_copy_kernel, dim3((unsigned)min((long long)n_copy * d.Hkv, 1ll << 20)), dim3(256), 0, s, a);
   return tw_prof_after(s);
 }
 
@@ -523,7 +530,7 @@ extern "C" int twilight_tokens_compact(const twilight_kv_t* kv, const int32_t* k
                                        const int32_t* dst_start, const int32_t* dst_table, void* stream) {
   TwDims d;
   if (int e = check_pages(kv, &d)) return e;
-  if (!keep_idx || !keep_count || keep_stride <= 0 || !dst_start || !kv->k_pool) return TW_EINVAL;
+  if (!keep_idx || !keep_count || keep_stride <= 0 || !dst_start || !kv->k_pool || !pools_aligned(kv)) return TW_EINVAL;
   hipStream_t s = (hipStream_t)stream;
   RowsArgs a = rows_args(kv, d);
   a.table = kv->page_table; a.to = dst_table; a.seq_lens = kv->seq_lens;

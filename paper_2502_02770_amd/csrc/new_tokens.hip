@@ -5,20 +5,28 @@
 // tile is loaded once for all of them.  A workgroup takes M = 32 * WR rows and walks tiles of 64 cached tokens:
 //
 //   S^T = K Q^T     v_mfma_f32_32x32x16_bf16, A = 32 tokens of K, B = 32 rows of Q (held in registers throughout)
-//   P^T = exp2(S^T * log2(e)/sqrt(128) - m), m = running maximum of the row
+//   P^T = exp2(S^T * log2(e)/sqrt(128) - m), m = the row's running maximum, followed only where it is 2^8 behind
 //   O^T += V^T P^T  A = V^T (transposed LDS reads), B = P^T
 //
 // In the result layout of the first product a lane holds 16 tokens of ONE row (its partner lane in the other half wave
 // the other 16), so maximum, sum and rescaling are in-lane but for one exchange between the halves, and the lane's own P
 // values are its B operand of the second product as they stand: the order of the 16 tokens within a contraction step is
 // free as long as the V^T operand has the same (slot 8 * h + j of step k = token 16 k + 8 (j / 4) + 4 h + j % 4).
-// P is rounded to bf16 for the product (each weight by at most 2^-8 of itself, the largest of a row exactly 1 at its time;
-// the output is bf16 anyway); scores, maxima, sums and accumulators are fp32, and the sum is of the unrounded weights.
+// P is rounded to bf16 for the product (each weight by at most 2^-8 of itself, independently; the output is bf16 anyway);
+// scores, maxima, sums, accumulators and the parts of cut lists are fp32, and the sum is of the unrounded weights.  A weight
+// may reach 2^8 before m follows (kGrowth): rescaling the accumulators for every new maximum, which some row of 32 has in most
+// tiles, took 54 of 211 vector instructions per tile (prompts of 8192 tokens: 852 us, 811 us without).
 //
 // K and V rows go from HBM to LDS without passing registers, 16 bytes per lane, a page of (token, head) rows being 4 KiB
 // contiguous; the 16-byte pieces of a row are stored in an order that depends on the row (XOR), so that neither the
 // 32-row reads of K nor the transposed reads of V meet in a bank.  Two buffers: a tile's loads are issued before the
 // tile ahead of it is computed.
+//
+// Bounds.  Few rows (32 or 64 to a workgroup, 2 or 4 waves that split a tile's tokens): HBM, 8 drafts of 32 over 32768 tokens
+// 1.08 GB in 208 us (5.2 TB/s; a large copy reads and writes 4.9).  128 rows (4 waves of 32 rows, all tokens each): a wave's tile
+// is 32 matrix instructions of 32 cycles, 16 of which keep the SIMD from issuing vector instructions, and 149 vector
+// instructions of 4 cycles (8 for the 32 exponentials): 1024 cycles of the matrix unit against 1236 of issue.  Two prompts
+// of 8192 tokens under a window of 4096: 811 us, 1.02 PFLOP/s of the pairs that are visible; an 8192^3 library product 1.21.
 #include "tw_common.h"
 
 namespace {
@@ -671,6 +679,7 @@ static int new_tokens_impl(const twilight_kv_t* kv, const void* q, const int32_t
   if (int e = tw_check_kv(kv, &d)) return e;
   if (!q || !out || !kv->k_pool || !kv->v_pool) return TW_EINVAL;
   if (max_new <= 0 || max_new > TW_MAX_NEW || d.max_pages > TW_MAX_ROW_PAGES) return TW_EINVAL;
+  if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)kv->k_pool | (uintptr_t)kv->v_pool | (uintptr_t)ws) & 15) return TW_EINVAL;
   if (!ws || ws_bytes < tw_new_tokens_workspace(d, max_new)) return TW_EWORKSPACE;
   const int M = rows_per_block((long long)max_new * d.G);
   NewArgs a;
@@ -685,7 +694,7 @@ static int new_tokens_impl(const twilight_kv_t* kv, const void* q, const int32_t
   a.max_new = max_new; a.mask_words = mask_words; a.window = window; a.sinks = sinks; a.pool_pages = (unsigned)d.pool_pages;
   a.rb_max = (int)(((long long)max_new * d.G + M - 1) / M); a.cus = tw_num_cus();
   const long long lists = (long long)a.rb_max * d.batch * d.Hkv;
-  if (lists > (1ll << 30) || (long long)max_new * d.Hq >= (1ll << 31) || (long long)max_new * d.batch >= (1ll << 31)) return TW_EINVAL;
+  if (lists >= (1ll << 24) || (long long)max_new * d.batch >= (1ll << 31)) return TW_EINVAL;      // (a launch has fewer than 2^32 threads)
   hipStream_t s = (hipStream_t)stream;
   if (tree) {
     switch (M) {

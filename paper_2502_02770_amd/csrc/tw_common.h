@@ -24,7 +24,7 @@ int tw_num_cus();                                        // compute units of the
 #define TW_MAX_NEW (1 << 20)
 #define TW_MAX_TREE 1024
 // Most pages of a row where token positions are added to in 32 bits (the operators on new tokens and on pages).
-#define TW_MAX_ROW_PAGES (1 << 26)
+#define TW_MAX_ROW_PAGES (1 << 24)
 
 // Launch bracket used by every entry point: tw_prof_before opens a timing record when the
 // kernel is to be timed, TW_LAUNCH then launches with the record's event pair attached to the

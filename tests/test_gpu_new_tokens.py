@@ -197,6 +197,30 @@ def test_trees_of_ragged_batches(hq, hkv, max_new):
 
 
 @pytest.mark.parametrize("hq,hkv", HEADS)
+@pytest.mark.parametrize("max_new", [1, 12, 40, 130])
+def test_short_sequences_in_wide_tables(hq, hkv, max_new):
+    """Rows of the page table could hold long sequences: the lists are planned on the device, and may be cut or not."""
+    lens = [1, 64, 200, 1500, 0, 130]
+    c = Cache(lens, hq, hkv, seed=max_new, max_pages=1000)
+    many = [min(n, max_new) for n in lens]
+    run_tree(c, many, max_new, seed=1)
+    run_window(c, many, max_new, 500, 3, seed=2)
+    run_window(c, many, max_new, NONE, 0, seed=3)
+
+
+def test_values_offloaded_to_the_host():
+    """K and V in pinned host memory, read over the link."""
+    import paper_2502_02770_amd as T
+    c = Cache([90, 300], 8, 2, seed=20)
+    far = T.PagedKV(8, 2, c.table, c.seq, c.k.shape[0], "cuda", offload_kv=True)
+    far.k_pool.copy_(c.k)
+    far.v_pool.copy_(c.v)
+    c.kv = far.kv
+    run_tree(c, [7, 40], 40)
+    run_window(c, [7, 40], 40, 100, 5)
+
+
+@pytest.mark.parametrize("hq,hkv", HEADS)
 @pytest.mark.parametrize("density", [0.0, 0.1, 0.7])
 def test_trees_with_any_mask(hq, hkv, density):
     """Rows that see nothing (no context), no ancestor, not themselves; bits of tokens beyond the draft."""

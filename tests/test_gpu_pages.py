@@ -100,7 +100,7 @@ def cache_of(table, lens, pool, hq=8, hkv=2, bits=4, fill=True, seed=0):
     return c
 
 
-@pytest.mark.parametrize("batch,max_pages,pool,seed", [(1, 1, 1, 0), (3, 7, 12, 1), (9, 40, 300, 2), (70, 33, 2000, 3), (17, 600, 40000, 4), (1100, 5, 5000, 5)])
+@pytest.mark.parametrize("batch,max_pages,pool,seed", [(1, 1, 1, 0), (3, 7, 12, 1), (9, 40, 300, 2), (70, 33, 2000, 3), (17, 600, 40000, 4), (1100, 5, 5000, 5), (5000, 3, 9000, 6)])
 def test_random_life_of_a_pool(batch, max_pages, pool, seed):
     import paper_2502_02770_amd as T
     rng = np.random.default_rng(seed)
@@ -414,6 +414,37 @@ def test_beams():
         kk, vv = (torch.stack([rows(B, hkv, t)[i][r] for t, r in hist[b]]) for i in (0, 1))
         own.append(kk, vv, i32([0]), i32([60]), i32([0]), 60)
         assert torch.equal(T.NewTokens(own, 1).window(q[b:b + 1].contiguous(), 2**31 - 1), out[b:b + 1]), b
+
+
+def test_samples_of_one_prompt():
+    """One row forked into a larger batch over the same pools: full pages shared, the partly filled one copied, each sample going on
+    by itself; then the samples but one dropped."""
+    import paper_2502_02770_amd as T
+    hq, hkv, n, N = 8, 2, 37, 5
+    c = cache_of([[-1] * 6], [0], 20, hq, hkv, fill=False)
+    p = T.PagePool(c)
+    p.reserve(i32([n]), n)
+    k, v = rows(n, hkv, 1)
+    c.append(k, v, i32([0]), i32([n]), i32([0]), n)
+    c.seq_lens += n
+    table, lens, src, dst = p.fork(i32([0] * N))
+    c.copy_pages(src, dst)
+    s = c.over(table, lens)
+    ps = p.over(s)
+    assert ps.ref_count[table[0, :2].long()].tolist() == [N, N] and len(set(table[:, 2].tolist())) == N
+    kn, vn = rows(N, hkv, 2)
+    ps.reserve(i32([1] * N), 1)
+    s.append(kn, vn, s.seq_lens.clone(), i32([1] * N), i32(range(N)), 1)
+    s.seq_lens += 1
+    q = torch.randn(N, hq, 128, device="cuda").to(torch.bfloat16)
+    out = T.NewTokens(s, 1).window(q, 2**31 - 1).clone()
+    for b in range(N):
+        own = cache_of([list(range(3))], [n + 1], 3, hq, hkv, fill=False)
+        own.append(torch.cat([k, kn[b:b + 1]]), torch.cat([v, vn[b:b + 1]]), i32([0]), i32([n + 1]), i32([0]), n + 1)
+        assert torch.equal(T.NewTokens(own, 1).window(q[b:b + 1].contiguous(), 2**31 - 1), out[b:b + 1]), b
+    table, lens, src, dst = ps.fork(i32([3]))
+    assert lens.tolist() == [n + 1] and src.tolist() == dst.tolist() == [-1]
+    assert int((ps.ref_count > 0).sum()) == 3 and int(ps.ref_count.sum()) == 3 and int(ps.status) == 0
 
 
 def test_pages_captured_and_replayed():

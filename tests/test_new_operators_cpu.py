@@ -6,6 +6,8 @@ import numpy as np
 import pytest
 import torch
 
+from tests.test_kernel_resources_cpu import _fits, kernels  # noqa: F401  (a fixture)
+
 
 @pytest.fixture(scope="module")
 def T():
@@ -39,13 +41,19 @@ def test_attention_of_new_tokens_refuses(T):
         assert f(q=None) == f(out=None) == f(max_new=0) == f(max_new=-1) == f(max_new=(1 << 20) + 1) == -1
         assert f(ws=None) == f(n=16) == -2
         assert f(kv=_kv(T, pools=False)) == -1
-        assert f(kv=_kv(T, max_pages=(1 << 26) + 1)) == -1
+        assert f(kv=_kv(T, max_pages=(1 << 24) + 1)) == -1
         bad = _kv(T)
         bad.head_dim = 64
         assert f(kv=bad) == -1
     assert tree(mask=None) == tree(words=0) == tree(max_new=33, words=1) == tree(max_new=1025, words=64) == -1
     assert win(window=0) == win(window=-5) == win(sinks=-1) == -1
     assert win(kv=_kv(T, batch=8000, hq=8, hkv=1), max_new=1 << 20) == -1       # rows beyond 31 bits
+    for f in (tree, win):
+        for odd in (dict(q=ctypes.c_void_p(4104)), dict(out=ctypes.c_void_p(4100)), dict(ws=ctypes.c_void_p(4097))):
+            assert f(**odd) == -1                                  # 16-byte pieces
+        odd = _kv(T)
+        odd.v_pool = 4104
+        assert f(kv=odd) == -1
     no_v = _kv(T)
     no_v.v_pool = None
     assert tree(kv=no_v) == win(kv=no_v) == -1
@@ -71,7 +79,7 @@ def test_page_operators_refuse(T):
     assert fork(n=0) == fork(n=65535) == fork(table=ONE) == fork(lens=ONE) == -1      # in place: the old rows would be read after they change
     assert fork(ws=None) == fork(b=8) == -2
     assert L.twilight_pages_copy(ref(kv), None, ONE, 3, None) == L.twilight_pages_copy(ref(kv), ONE, None, 3, None) == -1
-    assert L.twilight_pages_copy(ref(kv), ONE, ONE, -1, None) == L.twilight_pages_copy(ref(kv), ONE, ONE, 1 << 30, None) == -1
+    assert L.twilight_pages_copy(ref(kv), ONE, ONE, -1, None) == -1
     assert L.twilight_pages_copy(ref(kv), ONE, ONE, 0, None) == 0
     for k in (0, 1, 3):
         args = [ONE, ONE, 4, ONE, None]
@@ -79,9 +87,12 @@ def test_page_operators_refuse(T):
         assert L.twilight_tokens_compact(ref(kv), *args, None) == -1
     assert L.twilight_tokens_compact(ref(kv), ONE, ONE, 0, ONE, None, None) == -1
     assert L.twilight_tokens_compact(ref(_kv(T, pools=False)), ONE, ONE, 4, ONE, None, None) == -1
-    big = _kv(T, max_pages=(1 << 26) + 1)
+    big = _kv(T, max_pages=(1 << 24) + 1)
     assert L.twilight_pages_free(ref(big), ONE, ONE, ONE, ONE, None) == -1
     assert L.twilight_tokens_compact(ref(big), ONE, ONE, 4, ONE, None, None) == -1
+    odd = _kv(T)
+    odd.kq_meta = 4104
+    assert L.twilight_pages_copy(ref(odd), ONE, ONE, 3, None) == L.twilight_tokens_compact(ref(odd), ONE, ONE, 4, ONE, None, None) == -1
     no_table = _kv(T)
     no_table.page_table = None
     assert L.twilight_pages_free(ref(no_table), ONE, ONE, ONE, ONE, None) == -1
@@ -97,6 +108,23 @@ def test_workspace_sizes_of_the_new_operators(T):
     assert T.twilight_workspace_bytes(T.TW_WS_PAGES, kv, 33, 0) >= 2 * 4 + 2 * 4 * 4
     assert T.twilight_workspace_bytes(T.TW_WS_PAGES, kv, 0, 100) >= 100 * 4 + 64 * 4
     assert T.twilight_workspace_bytes(T.TW_WS_PAGES, kv, 0, 65536) == 0
+
+
+def test_the_binding_takes_the_documented_types_only(T):
+    for bad in (torch.zeros(4, dtype=torch.int64), torch.zeros(4, 4, dtype=torch.int32).t(), torch.zeros(4, dtype=torch.int32)):
+        with pytest.raises(AssertionError):                        # another type, not contiguous, not on the GPU
+            T.binding._ints(bad)
+    assert T.binding._ints(None) is None
+
+
+def test_kernels_of_the_new_operators_spill_nothing(kernels):
+    """Two workgroups to a compute unit where they have four waves (64 KiB of LDS each), no scratch in any."""
+    new = {n: k for n, k in kernels.items() if n.startswith(("new_tokens_", "pages_", "compact_kernel"))}
+    assert len(new) == 12 + 6 + 8
+    for n, k in new.items():
+        assert k[".vgpr_spill_count"] == 0 and k[".private_segment_fixed_size"] == 0, n
+        if n.startswith("new_tokens_kernel"):
+            assert _fits(k, 2) and k[".group_segment_fixed_size"] * 2 <= 160 * 1024, (n, k[".vgpr_count"])
 
 
 @pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 70])

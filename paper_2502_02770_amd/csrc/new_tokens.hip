@@ -45,6 +45,7 @@ constexpr int TILE = 64, TILE_BYTES = TILE * 256;
 enum { MODE_TREE = 0, MODE_WINDOW = 1 };
 constexpr int PLAN_ROUNDS = 2;                   // items per resident workgroup at most, as planned
 constexpr int PLAN_MIN_TILES = 2;                // shortest chunk of a list
+constexpr int STREAM_TILES = (128 << 20) / (2 * TILE_BYTES);   // tiles of K and V from which on they pass by the last-level cache
 constexpr long long COMBINE_FEW = 2048;          // rows of a launch up to which a workgroup joins one row's parts
 
 // rows of K and V that no token stands for (beyond the sequence's end, on an unmapped page) are read from here
@@ -64,7 +65,7 @@ struct NewArgs {
   int32_t* ws_plan;            // [batch][2]: chunks of the sequence's lists, first partial result
   float2* ws_ml;
   float* ws_acc;
-  int batch, Hq, Hkv, G, lgG, max_pages, max_new, mask_words, window, sinks, rb_max, cus;
+  int batch, Hq, Hkv, G, lgG, max_pages, max_new, mask_words, window, sinks, rb_max, cus, stream;
   unsigned pool_pages;
 };
 
@@ -128,9 +129,9 @@ __device__ __forceinline__ float wave_sum_f(float v) {
 // there are fewer than W r + lists items, and fewer than 2 W r of lists that are cut: what the workspace is sized for.
 // (Sums in fp32, a thousandth more than their errors added.)  Every workgroup does this before it knows its item, so in
 // few and short steps: with exact quotients by integer division it took 3 us of the 10 us that a single chat's call runs.
-// lists, tiles: of this lane's sequence where 64 lanes hold them all.
+// lists, tiles: of this lane's sequence where 64 lanes hold them all; *stream stays true where that many tiles are read.
 template <int MODE, int M>
-__device__ __forceinline__ int plan_chunk(const NewArgs& a, int lane, int* lists, int* tiles) {
+__device__ __forceinline__ int plan_chunk(const NewArgs& a, int lane, int* lists, int* tiles, bool* stream) {
   constexpr float kJoin = 1.5f, kPart = 2e-4f * M;
   float total = 0.f, lists_all = 0.f, longest = 0.f;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
@@ -141,6 +142,7 @@ __device__ __forceinline__ int plan_chunk(const NewArgs& a, int lane, int* lists
     longest = __builtin_fmaxf(longest, tw_wave_max_f((float)*tiles));
   }
   const float cus = (float)a.cus, W = 2.f * cus;
+  *stream = *stream && total > (float)STREAM_TILES;
   total *= 1.001f;
   auto cost_of = [&](float items, float c) { return __builtin_ceilf(items / W - 1e-4f) * (c * (items <= cus ? 0.8f : 1.f) + 2.f); };
   float best = cost_of(lists_all, longest), chunk = longest;
@@ -231,10 +233,21 @@ __device__ __forceinline__ bool whole_item(const NewArgs& a, Item* it) {
   return it->rb * M < seq_new(a, it->b) * a.G;
 }
 
+// The 16 rows of a page's K and V for one head, 16 bytes per lane.  HINT 2: non-temporal.
+template <int HINT>
+__device__ __forceinline__ void page_to_lds(const char* kp, const char* vp, unsigned k_off, unsigned v_off, unsigned char* dst) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    __builtin_amdgcn_global_load_lds((const TW_GLB unsigned int*)(kp + ((k_off ^ (unsigned)(64 * j)) + 1024u * j)), (TW_LDS unsigned int*)(dst + 1024 * j), 16, 0, HINT);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    __builtin_amdgcn_global_load_lds((const TW_GLB unsigned int*)(vp + ((v_off ^ (unsigned)(32 * (j & 1))) + 1024u * j)), (TW_LDS unsigned int*)(dst + TILE_BYTES + 1024 * j), 16, 0, HINT);
+}
+
 // One item: a chunk of a list.
 template <int MODE, int WR, int WT, bool SPLIT>
 __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, unsigned char (&buf0)[2 * TILE_BYTES], unsigned char (&buf1)[2 * TILE_BYTES],
-                                            int lane, int wave) {
+                                            int lane, int wave, bool stream) {
   constexpr int NW = WR * WT, M = 32 * WR, MT = 2 / WT, PPW = 4 / NW;
   const int wr = wave / WT, wt = wave % WT, half = lane >> 5;
   const int b = __builtin_amdgcn_readfirstlane(it.b), rb = __builtin_amdgcn_readfirstlane(it.rb), h = __builtin_amdgcn_readfirstlane(it.h);
@@ -310,12 +323,8 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
       const char* kp = a.k_pool + (long long)id * page_stride + head_off;
       const char* vp = a.v_pool + (long long)id * page_stride + head_off;
       if (left >= TW_PAGE) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          __builtin_amdgcn_global_load_lds((const TW_GLB unsigned int*)(kp + ((k_off ^ (unsigned)(64 * j)) + 1024u * j)), (TW_LDS unsigned int*)(dst + 1024 * j), 16, 0, 0);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          __builtin_amdgcn_global_load_lds((const TW_GLB unsigned int*)(vp + ((v_off ^ (unsigned)(32 * (j & 1))) + 1024u * j)), (TW_LDS unsigned int*)(dst + TILE_BYTES + 1024 * j), 16, 0, 0);
+        if (stream) page_to_lds<2>(kp, vp, k_off, v_off, dst);
+        else page_to_lds<0>(kp, vp, k_off, v_off, dst);
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -556,15 +565,29 @@ __global__ __launch_bounds__(64 * WR * WT, WR * WT >= 4 ? 2 : 1) void new_tokens
   __shared__ __align__(1024) unsigned char buf1[2 * TILE_BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   Item it;
+  // K and V that one workgroup alone reads and that are more than half of the last-level cache (256 MB) together pass by it: non-temporal
+  // loads, tree of 16 over 4 x 8192 tokens of 32 KV heads 104 -> 91 us (5.9 TB/s), 64 tokens under windows of 4096 156 -> 139 (6.1).
+  // Less would still lie there for the next call on the same cache (60 MB over and over 20.5 us, non-temporal 24.6), and row
+  // blocks that share their rows read them from the caches (two prompts of 8192 tokens 806 us, 894).
+  bool stream = a.stream != 0;
   if (!SPLIT) {
-    if (whole_item<M>(a, &it)) attend_item<MODE, WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave);
+    if (stream) {                                // as the lists really are
+      float total = 0.f;
+      for (int b0 = 0; b0 < a.batch; b0 += 64) {
+        int lists = 0, tiles = 0;
+        if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, &lists, &tiles);
+        total += wave_sum_f((float)lists * (float)tiles);
+      }
+      stream = total > (float)STREAM_TILES;
+    }
+    if (whole_item<M>(a, &it)) attend_item<MODE, WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave, stream);
     return;
   }
   int lists, tiles;
-  const int chunk = plan_chunk<MODE, M>(a, lane, &lists, &tiles);
+  const int chunk = plan_chunk<MODE, M>(a, lane, &lists, &tiles, &stream);
   uint32_t want = blockIdx.x;
   while (find_item<MODE, M>(a, lane, chunk, lists, tiles, want, &it)) {
-    attend_item<MODE, WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave);
+    attend_item<MODE, WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave, stream);
     want += gridDim.x;
     if (want >= it.items) break;
     __syncthreads();                             // the buffers have been read
@@ -643,6 +666,7 @@ int launch_new(NewArgs a, hipStream_t s) {
   const long long lists = (long long)a.rb_max * a.batch * a.Hkv;
   long long longest = ((long long)a.max_pages * TW_PAGE + TILE - 1) / TILE;      // tiles that a list can have
   if (MODE == MODE_WINDOW) longest = min(longest, ((long long)a.sinks + TILE - 1) / TILE + ((long long)a.window + M / a.G + TILE - 2) / TILE + 1);
+  a.stream = a.rb_max == 1 && lists * longest > STREAM_TILES;
   tw_prof_before(TW_K_NEW_TOKENS, s);
   if (!cut_lists(MODE == MODE_WINDOW, a.rb_max, lists, longest)) {
     TW_LAUNCH((new_tokens_kernel<MODE, WR, WT, false>), dim3((unsigned)lists), dim3(64 * WR * WT), 0, s, a);
@@ -692,7 +716,7 @@ static int new_tokens_impl(const twilight_kv_t* kv, const void* q, const int32_t
   a.ws_acc = (float*)((char*)a.ws_ml + align256n(slots * M * 8));
   a.batch = d.batch; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.G; a.lgG = __builtin_ctz(d.G); a.max_pages = d.max_pages;
   a.max_new = max_new; a.mask_words = mask_words; a.window = window; a.sinks = sinks; a.pool_pages = (unsigned)d.pool_pages;
-  a.rb_max = (int)(((long long)max_new * d.G + M - 1) / M); a.cus = tw_num_cus();
+  a.rb_max = (int)(((long long)max_new * d.G + M - 1) / M); a.cus = tw_num_cus(); a.stream = 0;
   const long long lists = (long long)a.rb_max * d.batch * d.Hkv;
   if (lists >= (1ll << 24) || (long long)max_new * d.batch >= (1ll << 31)) return TW_EINVAL;      // (a launch has fewer than 2^32 threads)
   hipStream_t s = (hipStream_t)stream;

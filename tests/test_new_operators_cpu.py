@@ -110,6 +110,11 @@ def test_workspace_sizes_of_the_new_operators(T):
     assert T.twilight_workspace_bytes(T.TW_WS_PAGES, kv, 0, 65536) == 0
 
 
+def test_names_of_the_timed_kernels(T):
+    L, names = T.binding.lib(), T.binding.KERNEL_NAMES
+    assert [L.twilight_kernel_name(i).decode() for i in range(len(names))] == names and L.twilight_kernel_name(len(names)) == b"?"
+
+
 def test_the_binding_takes_the_documented_types_only(T):
     for bad in (torch.zeros(4, dtype=torch.int64), torch.zeros(4, 4, dtype=torch.int32).t(), torch.zeros(4, dtype=torch.int32)):
         with pytest.raises(AssertionError):                        # another type, not contiguous, not on the GPU

@@ -391,9 +391,10 @@ int twilight_sparse_decode_per_head(const twilight_kv_t* kv, const void* q, cons
  *   lse            fp32 [rows][num_q_heads] or NULL, as twilight_sparse_decode
  *   ws             >= twilight_workspace_bytes(TW_WS_NEW_TOKENS, kv, max_new, 0),
  *                  for one call at a time
- * q, out, ws and the pools are 16-byte aligned (TW_EINVAL).  The values of V
- * that a token of the batch sees have to be finite, whichever tokens see them
- * (a weight of 0 times an infinity is no number).
+ * q, out, ws and the pools are 16-byte aligned (TW_EINVAL).  The rows of V of
+ * a sequence's own tokens have to be finite, whoever sees them (a weight of 0
+ * times an infinity is no number); a row of q or K that is not reaches only
+ * the tokens that it is of or that see it.
  *
  * twilight_tree_attention: a tree of drafted tokens.  Every new token sees the
  * tokens before the first new one, and of the new ones those whose bits are

@@ -325,6 +325,69 @@ def test_cache_beyond_32_bits():
     run_window(c, [20], 20, 700, 5)
 
 
+def test_a_long_prompt():
+    """20000 tokens at once, a window of 79 tiles: some rows of every part against the definition."""
+    import paper_2502_02770_amd as T
+    n, W, S = 20003, 5000, 5
+    c = Cache([n], 8, 2, seed=21)
+    q = queries(n, 8, 1)
+    out, lse = sent(q, 8)
+    T.twilight_window_attention(c.kv, q, None, None, n, W, S, out, lse, workspace(c.kv, n))
+    rows = torch.cat([torch.arange(a, a + 12, device="cuda") for a in (0, 58, 4990, 5060, 12345, n - 12)])
+    t = torch.arange(n, device="cuda")[None]
+    see = (t <= rows[:, None]) & ((rows[:, None] - t < W) | (t < S))
+    o, l, bo, bl = reference(c, 0, q[rows], see)
+    assert ((out[rows].double() - o).abs() <= bo).all() and ((lse[rows].double() - l).abs() <= bl).all()
+
+
+def test_a_long_context():
+    """Few lists of thousands of tiles."""
+    c = Cache([200013], 8, 2, seed=22)
+    run_tree(c, [3], 3)
+    run_window(c, [40], 40, 150000, 100)
+
+
+def test_a_row_that_is_not_finite_keeps_to_itself():
+    import paper_2502_02770_amd as T
+    c = Cache([300, 70], 8, 2, seed=23)
+    q = queries(20, 8, 1)
+    run = lambda q: T.twilight_window_attention(c.kv, q, None, None, 10, 100, 3, *(keep := sent(q, 8)), workspace(c.kv, 10)) or keep
+    a = run(q)
+    q2 = q.clone()
+    q2[4, 3] = math.nan
+    q2[13, 7, 5] = math.inf
+    b = run(q2)
+    others = torch.ones(20, 8, dtype=torch.bool, device="cuda")
+    others[4, 3] = others[13, 7] = False
+    assert torch.isnan(b[0][4, 3]).all() and torch.equal(a[0][others], b[0][others]) and torch.equal(a[1][others], b[1][others])
+    # a drafted token whose K is not finite, hidden from the others by their masks
+    p = int(c.table[1, 69 // 16])
+    c.k[p, :, 69 % 16] = math.nan                                  # the last token of the second sequence
+    x = run(q)
+    hidden = torch.ones(20, dtype=torch.bool, device="cuda")
+    hidden[19] = False                                             # only its own row sees it
+    assert torch.equal(x[0][hidden], a[0][hidden]) and torch.isnan(x[0][19]).all()
+
+
+def test_two_streams_at_once():
+    import paper_2502_02770_amd as T
+    c = Cache([5000, 40, 900], 32, 8, seed=24)
+    qs = [queries(3 * 4, 32, k) for k in (1, 2)]
+    ws = [workspace(c.kv, 4) for _ in qs]
+    alone, both = [sent(q, 32) for q in qs], [sent(q, 32) for q in qs]
+    for q, o, w in zip(qs, alone, ws):
+        T.twilight_window_attention(c.kv, q, None, None, 4, NONE, 0, *o, w)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    for _ in range(10):
+        for s, q, o, w in zip(streams, qs, both, ws):
+            with torch.cuda.stream(s):
+                T.twilight_window_attention(c.kv, q, None, None, 4, NONE, 0, *o, w)
+    torch.cuda.synchronize()
+    for a, b in zip(alone, both):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 def test_without_lse_and_default_rows():
     import paper_2502_02770_amd as T
     c = Cache([100, 700], 8, 2, seed=16)

@@ -99,17 +99,34 @@ def _ptr(t):
     return t.data_ptr()
 
 
-def _on_gpu(t, dtype):
-    """Pointer of a tensor of this type on the current device (whose stream the call is given)."""
-    if t is None:
-        return None
-    assert t.dtype == dtype and t.is_cuda and t.is_contiguous() and t.get_device() == torch._C._cuda_getDevice(), \
-        "contiguous %s tensor on the current device required" % dtype
-    return t.data_ptr()
+_I32, _F32, _BF16 = torch.int32, torch.float32, torch.bfloat16
+_NEEDED = "contiguous i32 (lists, tables, counts), bf16 (rows) and f32 (lse) tensors on the GPU required"
 
 
 def _ints(t):
-    return _on_gpu(t, torch.int32)
+    if t is None:
+        return None
+    assert t.dtype is _I32 and t.is_cuda and t.is_contiguous(), _NEEDED
+    return t.data_ptr()
+
+
+def _rows(t):
+    assert t.dtype is _BF16 and t.is_cuda and t.is_contiguous(), _NEEDED
+    return t.data_ptr()
+
+
+def _sums(t):
+    if t is None:
+        return None
+    assert t.dtype is _F32 and t.is_cuda and t.is_contiguous(), _NEEDED
+    return t.data_ptr()
+
+
+def _stream_of(t):
+    """The current stream, on which the call runs: of the tensors' device."""
+    d = torch._C._cuda_getDevice()
+    assert t.get_device() == d, "tensors on the current device required"
+    return torch._C._cuda_getCurrentRawStream(d)
 
 
 def _stream():
@@ -229,41 +246,41 @@ def twilight_sparse_decode_per_head(kv, q, kept_count, kept_idx, kept_stride, ou
 
 
 def twilight_tree_attention(kv, q, n_new, new_offsets, max_new, tree_mask, mask_words, out, lse, ws):
-    _check(lib().twilight_tree_attention(ctypes.byref(kv), _on_gpu(q, torch.bfloat16), _ints(n_new), _ints(new_offsets), int(max_new),
-                                         _ints(tree_mask), int(mask_words), _on_gpu(out, torch.bfloat16), _on_gpu(lse, torch.float32),
-                                         _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    _check(lib().twilight_tree_attention(ctypes.byref(kv), _rows(q), _ints(n_new), _ints(new_offsets), int(max_new),
+                                         _ints(tree_mask), int(mask_words), _rows(out), _sums(lse),
+                                         _ptr(ws), ws.numel() * ws.element_size(), _stream_of(q)))
 
 
 def twilight_window_attention(kv, q, n_new, new_offsets, max_new, window, num_sinks, out, lse, ws):
-    _check(lib().twilight_window_attention(ctypes.byref(kv), _on_gpu(q, torch.bfloat16), _ints(n_new), _ints(new_offsets), int(max_new),
-                                           int(window), int(num_sinks), _on_gpu(out, torch.bfloat16), _on_gpu(lse, torch.float32),
-                                           _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    _check(lib().twilight_window_attention(ctypes.byref(kv), _rows(q), _ints(n_new), _ints(new_offsets), int(max_new),
+                                           int(window), int(num_sinks), _rows(out), _sums(lse),
+                                           _ptr(ws), ws.numel() * ws.element_size(), _stream_of(q)))
 
 
 def twilight_pages_reserve(kv, n_new, max_new, ref_count, status, ws):
     _check(lib().twilight_pages_reserve(ctypes.byref(kv), _ints(n_new), int(max_new), _ints(ref_count), _ints(status),
-                                        _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+                                        _ptr(ws), ws.numel() * ws.element_size(), _stream_of(ref_count)))
 
 
 def twilight_pages_free(kv, first_page, end_page, ref_count, status):
     _check(lib().twilight_pages_free(ctypes.byref(kv), _ints(first_page), _ints(end_page), _ints(ref_count), _ints(status),
-                                     _stream()))
+                                     _stream_of(ref_count)))
 
 
 def twilight_pages_fork(kv, parent, new_batch, new_table, new_lens, ref_count, copy_src, copy_dst, status, ws):
     _check(lib().twilight_pages_fork(ctypes.byref(kv), _ints(parent), int(new_batch), _ints(new_table), _ints(new_lens),
                                      _ints(ref_count), _ints(copy_src), _ints(copy_dst), _ints(status), _ptr(ws),
-                                     ws.numel() * ws.element_size(), _stream()))
+                                     ws.numel() * ws.element_size(), _stream_of(ref_count)))
 
 
 def twilight_pages_copy(kv, copy_src, copy_dst, n_copy):
-    _check(lib().twilight_pages_copy(ctypes.byref(kv), _ints(copy_src), _ints(copy_dst), int(n_copy), _stream()))
+    _check(lib().twilight_pages_copy(ctypes.byref(kv), _ints(copy_src), _ints(copy_dst), int(n_copy), _stream_of(copy_src)))
 
 
 def twilight_tokens_compact(kv, keep_idx, keep_count, keep_stride, dst_start, dst_table):
     """dst_table None: in place."""
     _check(lib().twilight_tokens_compact(ctypes.byref(kv), _ints(keep_idx), _ints(keep_count), int(keep_stride),
-                                         _ints(dst_start), _ints(dst_table), _stream()))
+                                         _ints(dst_start), _ints(dst_table), _stream_of(keep_idx)))
 
 
 def twilight_decode_plan(kv, which=TW_WS_DECODE, dense=False):

@@ -45,7 +45,7 @@ constexpr int TILE = 64, TILE_BYTES = TILE * 256;
 enum { MODE_TREE = 0, MODE_WINDOW = 1 };
 constexpr int PLAN_ROUNDS = 2;                   // items per resident workgroup at most, as planned
 constexpr int PLAN_MIN_TILES = 2;                // shortest chunk of a list
-constexpr int STREAM_TILES = (128 << 20) / (2 * TILE_BYTES);   // tiles of K and V from which on they pass by the last-level cache
+constexpr int STREAM_TILES = (96 << 20) / (2 * TILE_BYTES);   // tiles of K and V from which on they pass by the last-level cache
 constexpr long long COMBINE_FEW = 2048;          // rows of a launch up to which a workgroup joins one row's parts
 
 // rows of K and V that no token stands for (beyond the sequence's end, on an unmapped page) are read from here
@@ -101,16 +101,34 @@ __device__ __forceinline__ Span span_of(const NewArgs& a, int len, int p_lo, int
 // Which part of which list a workgroup takes.  A list is a (row block, KV head) of a sequence; a sequence's lists are cut
 // into the same number of chunks.
 struct Item {
-  int b, rb, h, chunk, chunks, slot;
+  int b, n, len, off;                            // the sequence, as Seq
+  int rb, h, chunk, chunks, slot;
   uint32_t items;                                // of the launch, where one wave's lanes hold all sequences (no need to look for a next one)
 };
 
+// A sequence: its new tokens, length and first row, its lists and the tiles of the longest of them.
+struct Seq {
+  int n, len, off, lists, tiles;
+};
 template <int MODE, int M>
-__device__ __forceinline__ void lists_of(const NewArgs& a, int b, int* lists, int* tiles) {
-  const int n = seq_new(a, b), len = seq_len(a, b);
-  const int blocks = (n * a.G + M - 1) / M;
-  *lists = blocks * a.Hkv;
-  *tiles = blocks == 0 ? 0 : max(1, span_of<MODE>(a, len, len - min(n, M / a.G), len - 1).tiles);
+__device__ __forceinline__ Seq seq_of(const NewArgs& a, int b) {
+  Seq s = {0, 0, 0, 0, 0};
+  if (b >= a.batch) return s;
+  s.off = a.offsets ? a.offsets[b] : b * a.max_new;
+  s.n = seq_new(a, b);
+  s.len = seq_len(a, b);
+  const int blocks = (s.n * a.G + M - 1) / M;
+  s.lists = blocks * a.Hkv;
+  s.tiles = blocks == 0 ? 0 : max(1, span_of<MODE>(a, s.len, s.len - min(s.n, M / a.G), s.len - 1).tiles);
+  return s;
+}
+
+// x / d for quotients below 2^20
+__device__ __forceinline__ uint32_t quotient(uint32_t x, uint32_t d) {
+  uint32_t q = (uint32_t)((float)x * __builtin_amdgcn_rcpf((float)d));
+  const int r = (int)(x - q * d);
+  q = r < 0 ? q - 1u : (uint32_t)r >= d ? q + 1u : q;
+  return q;
 }
 
 // Sum over the 64 lanes, for all of them.
@@ -129,17 +147,16 @@ __device__ __forceinline__ float wave_sum_f(float v) {
 // there are fewer than W r + lists items, and fewer than 2 W r of lists that are cut: what the workspace is sized for.
 // (Sums in fp32, a thousandth more than their errors added.)  Every workgroup does this before it knows its item, so in
 // few and short steps: with exact quotients by integer division it took 3 us of the 10 us that a single chat's call runs.
-// lists, tiles: of this lane's sequence where 64 lanes hold them all; *stream stays true where that many tiles are read.
+// *seq: this lane's sequence where 64 lanes hold them all; *stream stays true where that many tiles are read.
 template <int MODE, int M>
-__device__ __forceinline__ int plan_chunk(const NewArgs& a, int lane, int* lists, int* tiles, bool* stream) {
+__device__ __forceinline__ int plan_chunk(const NewArgs& a, int lane, Seq* seq, bool* stream) {
   constexpr float kJoin = 1.5f, kPart = 2e-4f * M;
   float total = 0.f, lists_all = 0.f, longest = 0.f;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    *lists = *tiles = 0;
-    if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, lists, tiles);
-    total += wave_sum_f((float)*lists * (float)*tiles);
-    lists_all += wave_sum_f((float)*lists);
-    longest = __builtin_fmaxf(longest, tw_wave_max_f((float)*tiles));
+    *seq = seq_of<MODE, M>(a, b0 + lane);
+    total += wave_sum_f((float)seq->lists * (float)seq->tiles);
+    lists_all += wave_sum_f((float)seq->lists);
+    longest = __builtin_fmaxf(longest, tw_wave_max_f((float)seq->tiles));
   }
   const float cus = (float)a.cus, W = 2.f * cus;
   *stream = *stream && total > (float)STREAM_TILES;
@@ -167,11 +184,8 @@ __device__ __forceinline__ int plan_chunk(const NewArgs& a, int lane, int* lists
       const float inv = __builtin_amdgcn_rcpf(c);
       float items = 0.f;
       for (int b0 = 0; b0 < a.batch; b0 += 64) {
-        if (a.batch > 64) {
-          *lists = *tiles = 0;
-          if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, lists, tiles);
-        }
-        items += wave_sum_f((float)*lists * __builtin_ceilf((float)*tiles * inv - 1e-4f));
+        if (a.batch > 64) *seq = seq_of<MODE, M>(a, b0 + lane);
+        items += wave_sum_f((float)seq->lists * __builtin_ceilf((float)seq->tiles * inv - 1e-4f));
       }
       const float cost = cost_of(items, c) + kJoin + items * kPart;
       if (cost < best) { best = cost; chunk = c; }
@@ -182,16 +196,13 @@ __device__ __forceinline__ int plan_chunk(const NewArgs& a, int lane, int* lists
 
 // Item `want` of a launch whose lists are cut into chunks of `chunk` tiles; false: there are fewer.
 template <int MODE, int M>
-__device__ __forceinline__ bool find_item(const NewArgs& a, int lane, int chunk, int lists, int tiles, uint32_t want, Item* it) {
+__device__ __forceinline__ bool find_item(const NewArgs& a, int lane, int chunk, Seq seq, uint32_t want, Item* it) {
   uint32_t items = 0, slots = 0;
   bool found = false;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    if (a.batch > 64) {
-      lists = tiles = 0;
-      if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, &lists, &tiles);
-    }
-    const int chunks = (tiles + chunk - 1) / chunk;
-    const uint32_t mine = (uint32_t)(lists * chunks), part = chunks > 1 ? mine : 0u;
+    if (a.batch > 64) seq = seq_of<MODE, M>(a, b0 + lane);
+    const int chunks = (int)quotient((uint32_t)(seq.tiles + chunk - 1), (uint32_t)chunk);
+    const uint32_t mine = (uint32_t)(seq.lists * chunks), part = chunks > 1 ? mine : 0u;
     const uint32_t ie = tw_wave_scan_u32(mine), se = tw_wave_scan_u32(part);
     if (want == 0 && threadIdx.x < 64 && b0 + lane < a.batch) {         // for the combine kernel
       a.ws_plan[2 * (b0 + lane)] = chunks;
@@ -203,11 +214,14 @@ __device__ __forceinline__ bool find_item(const NewArgs& a, int lane, int chunk,
       const uint32_t before = items + (uint32_t)__builtin_amdgcn_readlane((int)(ie - mine), l);
       const uint32_t k = want - before;          // ((chunk * blocks) + block) * Hkv + head: blocks of the same rows' chunk on one XCD
       it->b = b0 + l;
+      it->n = __builtin_amdgcn_readlane(seq.n, l);
+      it->len = __builtin_amdgcn_readlane(seq.len, l);
+      it->off = __builtin_amdgcn_readlane(seq.off, l);
       it->chunks = __builtin_amdgcn_readlane(chunks, l);
-      const uint32_t all = (uint32_t)__builtin_amdgcn_readlane(lists, l);
-      it->chunk = (int)(k / all);
+      const uint32_t all = (uint32_t)__builtin_amdgcn_readlane(seq.lists, l);
+      it->chunk = (int)quotient(k, all);
       const uint32_t rest = k - (uint32_t)it->chunk * all;
-      it->rb = (int)(rest / (uint32_t)a.Hkv);
+      it->rb = (int)quotient(rest, (uint32_t)a.Hkv);
       it->h = (int)(rest - (uint32_t)it->rb * (uint32_t)a.Hkv);
       it->slot = (int)(slots + (uint32_t)__builtin_amdgcn_readlane((int)(se - part), l) + k);
       found = true;
@@ -230,7 +244,10 @@ __device__ __forceinline__ bool whole_item(const NewArgs& a, Item* it) {
   it->rb = a.rb_max - 1 - (int)(i % (unsigned)a.rb_max);
   it->b = (int)(i / (unsigned)a.rb_max);
   it->chunk = 0; it->chunks = 1; it->slot = 0;
-  return it->rb * M < seq_new(a, it->b) * a.G;
+  it->n = seq_new(a, it->b);
+  it->len = seq_len(a, it->b);
+  it->off = a.offsets ? a.offsets[it->b] : it->b * a.max_new;
+  return it->rb * M < it->n * a.G;
 }
 
 // The 16 rows of a page's K and V for one head, 16 bytes per lane.  HINT 2: non-temporal.
@@ -251,8 +268,7 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
   constexpr int NW = WR * WT, M = 32 * WR, MT = 2 / WT, PPW = 4 / NW;
   const int wr = wave / WT, wt = wave % WT, half = lane >> 5;
   const int b = __builtin_amdgcn_readfirstlane(it.b), rb = __builtin_amdgcn_readfirstlane(it.rb), h = __builtin_amdgcn_readfirstlane(it.h);
-  const int n = __builtin_amdgcn_readfirstlane(seq_new(a, b)), len = __builtin_amdgcn_readfirstlane(seq_len(a, b));
-  const int off = __builtin_amdgcn_readfirstlane(a.offsets ? a.offsets[b] : b * a.max_new);
+  const int n = __builtin_amdgcn_readfirstlane(it.n), len = __builtin_amdgcn_readfirstlane(it.len), off = __builtin_amdgcn_readfirstlane(it.off);
   const int ctx = len - n;                       // position of new token 0 (negative: a draft longer than the sequence)
 
   // this lane's row; rows beyond the last repeat it and are not stored
@@ -565,28 +581,28 @@ __global__ __launch_bounds__(64 * WR * WT, WR * WT >= 4 ? 2 : 1) void new_tokens
   __shared__ __align__(1024) unsigned char buf1[2 * TILE_BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   Item it;
-  // K and V that one workgroup alone reads and that are more than half of the last-level cache (256 MB) together pass by it: non-temporal
+  // K and V that one workgroup alone reads and that are more than 96 MB together (the last-level cache holds 256) pass by it: non-temporal
   // loads, tree of 16 over 4 x 8192 tokens of 32 KV heads 104 -> 91 us (5.9 TB/s), 64 tokens under windows of 4096 156 -> 139 (6.1).
-  // Less would still lie there for the next call on the same cache (60 MB over and over 20.5 us, non-temporal 24.6), and row
-  // blocks that share their rows read them from the caches (two prompts of 8192 tokens 806 us, 894).
+  // Less would still lie there for the next call on the same cache (calls on three caches in turn: of 128 MB 40.2 us, non-temporal
+  // 35.6, of 73 MB 23.4 and 24.1, of 60 MB 20.5 and 24.6), and row blocks that share their rows read them from the caches (two prompts
+  // of 8192 tokens 806 us, 894).
   bool stream = a.stream != 0;
   if (!SPLIT) {
     if (stream) {                                // as the lists really are
       float total = 0.f;
       for (int b0 = 0; b0 < a.batch; b0 += 64) {
-        int lists = 0, tiles = 0;
-        if (b0 + lane < a.batch) lists_of<MODE, M>(a, b0 + lane, &lists, &tiles);
-        total += wave_sum_f((float)lists * (float)tiles);
+        const Seq q = seq_of<MODE, M>(a, b0 + lane);
+        total += wave_sum_f((float)q.lists * (float)q.tiles);
       }
       stream = total > (float)STREAM_TILES;
     }
     if (whole_item<M>(a, &it)) attend_item<MODE, WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave, stream);
     return;
   }
-  int lists, tiles;
-  const int chunk = plan_chunk<MODE, M>(a, lane, &lists, &tiles, &stream);
+  Seq seq;
+  const int chunk = plan_chunk<MODE, M>(a, lane, &seq, &stream);
   uint32_t want = blockIdx.x;
-  while (find_item<MODE, M>(a, lane, chunk, lists, tiles, want, &it)) {
+  while (find_item<MODE, M>(a, lane, chunk, seq, want, &it)) {
     attend_item<MODE, WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave, stream);
     want += gridDim.x;
     if (want >= it.items) break;

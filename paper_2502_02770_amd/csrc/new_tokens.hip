@@ -82,19 +82,28 @@ __device__ __forceinline__ int seq_new(const NewArgs& a, int b) {
   return a.n_new ? max(0, min(a.n_new[b], a.max_new)) : a.max_new;
 }
 
-// The tiles that rows of tokens at positions p_lo .. p_hi see: `sink` tiles from the start, then those from `first` on.
+// The pages that rows of tokens at positions p_lo .. p_hi see: `sink` pages from the start, then those from `first` on; four of
+// this list to a tile, so that a few sinks and a window that begins inside 64 tokens cost no tile of their own: five prompts of 882
+// tokens, a window of 51 and one sink 35.1 us with tiles at multiples of 64, 32.3 so.  Where few tiles are saved, working out the
+// places costs more than that: one token, a window of 1024 and 4 sinks 10.5 and 10.8 us.
 struct Span {
-  int sink, first, tiles;
-  __device__ __forceinline__ int tile(int u) const { return u < sink ? u : first + (u - sink); }
+  int sink, first, pages, tiles;
+  int both, behind, shift;                       // the tile with pages of both parts, the first one of the second; positions between the parts
+  __device__ __forceinline__ int page(int v) const { return v < sink ? v : first + (v - sink); }
+  __device__ __forceinline__ int start(int u) const { return u * TILE + (u >= behind ? shift : 0); }   // position of tile u's first page
 };
 template <int MODE>
 __device__ __forceinline__ Span span_of(const NewArgs& a, int len, int p_lo, int p_hi) {
   Span s;
   const int end = MODE == MODE_TREE ? len : min(len, p_hi + 1);
-  if (end <= 0) { s.sink = s.first = s.tiles = 0; return s; }
-  s.first = MODE == MODE_TREE ? 0 : max(0, p_lo - a.window + 1) / TILE;
-  s.sink = MODE == MODE_TREE ? 0 : min((int)(((unsigned)a.sinks + TILE - 1) / TILE), s.first);
-  s.tiles = s.sink + (end - 1) / TILE - s.first + 1;
+  if (end <= 0) { s.sink = s.first = s.pages = s.tiles = s.behind = s.shift = 0; s.both = -1; return s; }
+  s.first = MODE == MODE_TREE ? 0 : max(0, p_lo - a.window + 1) / TW_PAGE;
+  s.sink = MODE == MODE_TREE ? 0 : min((int)(((unsigned)a.sinks + TW_PAGE - 1) / TW_PAGE), s.first);
+  s.pages = s.sink + (end - 1) / TW_PAGE - s.first + 1;
+  s.tiles = (s.pages + 3) / 4;
+  s.behind = (s.sink + 3) / 4;
+  s.both = s.sink & 3 && s.sink < s.first ? s.sink / 4 : -1;
+  s.shift = (s.first - s.sink) * TW_PAGE;
   return s;
 }
 
@@ -315,12 +324,14 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
   int mine[PPW];                                 // the pages that this wave loads
   unsigned long long mapped[4];                  // per page of a tile: the tiles (bits) where it is mapped
   auto refill = [&](int u) {
-    const int ul = min(u + lane, u1 - 1), pg0 = sp.tile(ul) * (TILE / TW_PAGE);
+    const int v0 = 4 * min(u + lane, u1 - 1);
     int id[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) id[j] = table[min(pg0 + j, a.max_pages - 1)];
+    for (int j = 0; j < 4; ++j) id[j] = table[min(sp.page(v0 + j), a.max_pages - 1)];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) mapped[j] = __ballot((unsigned)id[j] < a.pool_pages && (pg0 + j) * TW_PAGE < len);
+    for (int j = 0; j < 4; ++j) {
+      mapped[j] = __ballot(v0 + j < sp.pages && (unsigned)id[j] < a.pool_pages);
+    }
 #pragma unroll
     for (int p = 0; p < PPW; ++p) {
       const int j = wave * PPW + p;
@@ -330,12 +341,13 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
   const long long head_off = (long long)h * TW_PAGE * 256, page_stride = (long long)a.Hkv * TW_PAGE * 256;
   int base = 0;                                  // first tile of the page ids held
   auto issue = [&](unsigned char* buf, int u) {
-    const int k = u - base, t0 = sp.tile(u) * TILE;
+    const int k = u - base, t0 = sp.start(u);
 #pragma unroll
     for (int p = 0; p < PPW; ++p) {
       const int pg = wave * PPW + p;
       const int id = __builtin_amdgcn_readlane(mine[p], k);
-      const int left = (unsigned)id < a.pool_pages ? len - (t0 + pg * TW_PAGE) : 0;    // rows of the page that are tokens
+      const int gap = MODE == MODE_WINDOW && ((u == sp.both) & (4 * u + pg >= sp.sink)) ? sp.shift : 0;
+      const int left = (unsigned)id < a.pool_pages ? len - (t0 + pg * TW_PAGE + gap) : 0;    // rows of the page that are tokens
       unsigned char* dst = buf + pg * 4096;
       const char* kp = a.k_pool + (long long)id * page_stride + head_off;
       const char* vp = a.v_pool + (long long)id * page_stride + head_off;
@@ -367,7 +379,7 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
   struct Words { uint32_t w[3]; };
   auto mask_words = [&](int u) -> Words {
     Words x = {{0u, 0u, 0u}};
-    const int j0 = sp.tile(u) * TILE - ctx;      // draft token of the tile's first position
+    const int j0 = u * TILE - ctx;       // draft token of the tile's first position
     if (MODE == MODE_TREE && j0 > -TILE) {
       const uint32_t* mrow = a.mask + (long long)(off + tok) * a.mask_words;
       const int w0 = j0 >= 0 ? j0 >> 5 : 0;
@@ -386,15 +398,16 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
     __syncthreads();
   };
   auto compute = [&](const unsigned char* buf, int u, unsigned held, const Words& x) {
-    const int t0 = sp.tile(u) * TILE;
-    bool all = held == 15u && t0 + TILE <= len;
-    if (MODE == MODE_TREE) {
-      all = all && t0 + TILE <= ctx;
-      if (idle_wave) return;
+    const int t0 = sp.start(u);
+    const bool in_a_row = MODE == MODE_TREE || u != sp.both;
+    bool none = idle_wave, all = (held == 15u) & (t0 + TILE <= len);     // does no row of the wave see the tile, does every row see all of it
+    if (MODE == MODE_TREE) {                     // (no short cuts in these: as branches they made 826 us of the prompts of 8192 tokens 838)
+      all = all & (t0 + TILE <= ctx);
     } else {
-      if (idle_wave || t0 > w_hi || (t0 + TILE - 1 <= w_lo - a.window && t0 >= a.sinks)) return;    // no row of the wave sees the tile
-      all = all && t0 + TILE - 1 <= w_lo && (t0 > w_hi - a.window || t0 + TILE <= a.sinks);
+      none = none | (in_a_row & ((t0 > w_hi) | ((t0 + TILE - 1 <= w_lo - a.window) & (t0 >= a.sinks))));
+      all = all & in_a_row & (t0 + TILE - 1 <= w_lo) & ((t0 > w_hi - a.window) | (t0 + TILE <= a.sinks));
     }
+    if (none) return;
     // K of the whole slice, then the products, each later operand's read behind a product; the first V operands come with
     // the last products, so that they wait for nothing behind the softmax
     tw_f32x16 s[MT];
@@ -446,7 +459,11 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
         }
         vis &= low_bits(len - t0);
       } else {
-        vis = low_bits(pos + 1 - t0) & (~low_bits(pos - a.window + 1 - t0) | low_bits(a.sinks - t0)) & low_bits(len - t0);
+        // (pos < len.)  In the tile in which the sinks' pages end, the first `lead` positions are those, and the others follow the
+        // window's first page as if they had begun at t1
+        const int lead = in_a_row ? 0 : (sp.sink - 4 * u) * TW_PAGE, t1 = in_a_row ? t0 : sp.first * TW_PAGE - lead;
+        vis = low_bits(pos + 1 - t1) & (~low_bits(pos - a.window + 1 - t1) | low_bits(a.sinks - t1));
+        if (!in_a_row) vis = (vis & ~low_bits(lead)) | (low_bits(min(a.sinks, pos + 1) - t0) & low_bits(lead));
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -574,7 +591,7 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
 }
 
 // (Bounds of 256 threads also where there are 128: told that LDS leaves one wave to a SIMD, the compiler keeps the accumulators apart from
-// the registers that vector instructions reach, and moves them to and fro for every rescaling: 43 lists of 7 tiles 10.2 us, 8.9 without.)
+// the registers that vector instructions reach, and moves them to and fro for every rescaling: 40 lists of up to 7 tiles 10.2 us, 8.9 without.)
 // SPLIT: resident workgroups stride over the items (workgroups beyond those would wait for a slot to find out that there is
 // nothing left for them); otherwise a workgroup per list.
 template <int MODE, int WR, int WT, bool SPLIT>
@@ -684,7 +701,8 @@ int launch_new(NewArgs a, hipStream_t s) {
   constexpr int M = 32 * WR;
   const long long lists = (long long)a.rb_max * a.batch * a.Hkv;
   long long longest = ((long long)a.max_pages * TW_PAGE + TILE - 1) / TILE;      // tiles that a list can have
-  if (MODE == MODE_WINDOW) longest = min(longest, ((long long)a.sinks + TILE - 1) / TILE + ((long long)a.window + M / a.G + TILE - 2) / TILE + 1);
+  if (MODE == MODE_WINDOW)
+    longest = min(longest, (((long long)a.sinks + TW_PAGE - 1) / TW_PAGE + ((long long)a.window + M / a.G + TW_PAGE - 2) / TW_PAGE + 1 + 3) / 4);
   a.stream = a.rb_max == 1 && lists * longest > STREAM_TILES;
   tw_prof_before(TW_K_NEW_TOKENS, s);
   if (!cut_lists(MODE == MODE_WINDOW, a.rb_max, lists, longest)) {

@@ -289,6 +289,16 @@ def test_windows_of_whole_prompts(hq, hkv, tokens, window, sinks):
     run_window(Cache(lens, hq, hkv, seed=3), lens, tokens, window, sinks, seed=5)
 
 
+@pytest.mark.parametrize("hq,hkv,new", [(8, 8, 1), (32, 8, 5), (16, 2, 30), (8, 4, 60)])
+@pytest.mark.parametrize("sinks", [1, 16, 17, 40, 63, 100])
+def test_pages_of_sinks_and_pages_of_the_window_in_one_tile(hq, hkv, new, sinks):
+    """The sinks' pages end inside a tile and the window begins on any page, next to them or far behind."""
+    lens = [400, 129, 144, 1000, 161, 97, 15, 257, 64]
+    c = Cache(lens, hq, hkv, seed=sinks)
+    for window in (1, 15, 30, 64, 110):
+        run_window(c, [min(n, new) for n in lens], new, window, sinks, seed=window)
+
+
 def test_a_window_over_freed_pages():
     """Pages between the sinks and the window have been given back."""
     c = Cache([5000], 8, 2, seed=12)

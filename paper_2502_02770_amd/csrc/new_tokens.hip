@@ -26,7 +26,7 @@
 // 1.08 GB in 208 us (5.2 TB/s; a large copy reads and writes 4.9).  128 rows (4 waves of 32 rows, all tokens each): a wave's tile
 // is 32 matrix instructions of 32 cycles, 16 of which keep the SIMD from issuing vector instructions, and 149 vector
 // instructions of 4 cycles (8 for the 32 exponentials): 1024 cycles of the matrix unit against 1236 of issue.  Two prompts
-// of 8192 tokens under a window of 4096: 811 us, 1.02 PFLOP/s of the pairs that are visible; an 8192^3 library product 1.21.
+// of 8192 tokens under a window of 4096: 826 us, 1.00 PFLOP/s of the pairs that are visible; an 8192^3 library product 1.21.
 #include "tw_common.h"
 
 namespace {
@@ -686,10 +686,12 @@ int rows_per_block(long long rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 
 // Lists that cannot be long are not cut, which saves the launch that joins the parts and their way through memory: up to 6 tiles,
 // one more for every 32 lists, at most 32.  Few lists run no faster whole than cut from there on; many would leave CUs idle
 // only where few of them are as long as the longest may be.  us, cut / whole, by tiles of all lists:
-//   32 rows    8 lists  4: 10.9 /  8.3  6: 10.9 / 10.2  8: 10.9 / 12.2     160 lists   8: 18.7 / 15.0  16: 25.5 / 26.1  24: 36.2 / 44.0
-//   64         8        6: 11.1 /  9.5  8: 11.2 / 10.9 12: 11.4 / 14.1     160        12: 23.9 / 19.1  16: 28.3 / 24.8  24: 39.6 / 41.9
-//   128        8        6: 12.6 / 11.6  8: 12.8 / 13.9                     160        12: 35.4 / 22.2  16: 42.0 / 31.2  24: 50.5 / 48.5
-//   32       512       16: 51.7 / 51.5 24: 79.1 / 73.4 32: 100.6 / 94.8
+//   32 rows    8 lists  4: 10.1 /  7.3  6: 10.2 /  8.9  8: 10.2 / 10.5     160 lists   8: 18.0 / 13.3  16: 23.3 / 21.8  26: 30.9 / 42.9
+//   64        32        6: 13.4 / 10.4  8: 13.4 / 11.6 12: 14.4 / 17.6     160        12: 24.1 / 19.6  16: 29.1 / 25.1  26: 37.0 / 44.3
+//   128        8        6: 12.4 / 11.7  8: 12.6 / 14.0                     160        12: 27.3 / 22.1  16: 36.3 / 31.2  26: 55.3 / 49.9
+//   32       512       16: 47.2 / 43.6 24: 66.7 / 63.0 32: 85.2 / 81.9
+// and with ragged lengths up to that, for which more would be too many:
+//   32       160        8: 10.3 / 10.8 12: 11.0 / 12.5 16: 13.7 / 18.2     128 rows   12: 14.8 / 14.9  16: 16.9 / 22.4  26: 25.5 / 34.6
 // Nor are the row blocks of chunks and prompts under a window that fill the chip by themselves: their lists are alike.
 bool cut_lists(bool window, int blocks, long long lists, long long longest) {
   if (longest <= min(32ll, 6 + lists / 32)) return false;

@@ -439,7 +439,8 @@ int twilight_window_attention(const twilight_kv_t* kv, const void* q, const int3
  * positions seq_lens[b] .. seq_lens[b] + n_new[b] - 1 gets a page (seq_lens
  * not yet advanced; beyond the row's max_pages_per_seq nothing happens).
  *   n_new          i32 [batch], clamped to [0, max_new]
- *   max_new        host: upper bound of n_new[] (sizes the workspace)
+ *   max_new        host: upper bound of n_new[] (sizes the workspace);
+ *                  batch * min(max_pages_per_seq, max_new / 16 + 2) < 2^31
  *   ws             >= twilight_workspace_bytes(TW_WS_PAGES, kv, max_new, 0)
  *
  * twilight_pages_free: logical pages first_page[b] .. end_page[b] - 1 of every

@@ -2,6 +2,7 @@
 // pools, bits only).  The state of the pool is one count per page; a page is free when its count is 0, and pages are
 // handed out from the lowest free one up in the order of the requests.  Counts change by integer atomics, whose order
 // does not matter, and the order of handing out is a prefix sum, so tables and counts never depend on timing.
+#include <algorithm>
 #include "tw_common.h"
 
 namespace {
@@ -438,17 +439,21 @@ PagesArgs pages_args(const twilight_kv_t* kv, const TwDims& d, int32_t* ref, uin
   a.batch = d.batch; a.max_pages = d.max_pages; a.pool_pages = (unsigned)d.pool_pages;
   return a;
 }
-unsigned row_blocks(int max_pages) { return (unsigned)min((max_pages + 255) / 256, 64); }
+unsigned row_blocks(int max_pages) { return (unsigned)std::min((max_pages + 255) / 256, 64); }
 
 size_t take_rows_bytes(long long rows) { return align256p((size_t)rows * 4); }
 
 }  // namespace
 
+// entries that a reservation of max_new tokens per row looks at; counted in 32 bits
+static long long reserve_entries(const TwDims& d, int max_new) {
+  return d.batch * std::min((long long)d.max_pages, max_new > 0 ? ((long long)max_new + TW_PAGE - 1) / TW_PAGE + 1 : 0ll);
+}
+
 size_t tw_pages_workspace(const TwDims& d, int max_new, int new_batch) {
   if (max_new < 0 || new_batch < 0 || new_batch > 65535) return 0;
   const long long rows = d.batch > new_batch ? d.batch : new_batch;
-  const long long pages = min((long long)d.max_pages, max_new ? (max_new + TW_PAGE - 1ll) / TW_PAGE + 1 : 0ll);
-  const long long most = min(max((long long)d.batch * pages, (long long)new_batch), d.pool_pages);
+  const long long most = std::min<long long>(std::max(reserve_entries(d, max_new), (long long)new_batch), d.pool_pages);
   return take_rows_bytes(rows) + align256p((size_t)most * 4);
 }
 
@@ -456,7 +461,7 @@ extern "C" int twilight_pages_reserve(const twilight_kv_t* kv, const int32_t* n_
                                       uint32_t* status, void* ws, size_t ws_bytes, void* stream) {
   TwDims d;
   if (int e = check_pages(kv, &d)) return e;
-  if (!n_new || max_new <= 0 || !ref_count || !status) return TW_EINVAL;
+  if (!n_new || max_new <= 0 || !ref_count || !status || reserve_entries(d, max_new) >= (1ll << 31)) return TW_EINVAL;
   if (!ws || ws_bytes < tw_pages_workspace(d, max_new, 0)) return TW_EWORKSPACE;
   hipStream_t s = (hipStream_t)stream;
   PagesArgs a = pages_args(kv, d, ref_count, status);
@@ -522,7 +527,7 @@ extern "C" int twilight_pages_copy(const twilight_kv_t* kv, const int32_t* copy_
   RowsArgs a = rows_args(kv, d);
   a.src = copy_src; a.dst = copy_dst; a.n_copy = n_copy;
   tw_prof_before(TW_K_PAGES_COPY, s);
-  TW_LAUNCH(pages_copy_kernel, dim3((unsigned)min((long long)n_copy * d.Hkv, 1ll << 20)), dim3(256), 0, s, a);
+  TW_LAUNCH(pages_copy_kernel, dim3((unsigned)std::min((long long)n_copy * d.Hkv, 1ll << 20)), dim3(256), 0, s, a);
   return tw_prof_after(s);
 }
 
@@ -535,7 +540,7 @@ extern "C" int twilight_tokens_compact(const twilight_kv_t* kv, const int32_t* k
   RowsArgs a = rows_args(kv, d);
   a.table = kv->page_table; a.to = dst_table; a.seq_lens = kv->seq_lens;
   a.keep = keep_idx; a.count = keep_count; a.start = dst_start; a.stride = keep_stride;
-  const long long most = min((long long)keep_stride, (long long)d.max_pages * TW_PAGE) + TW_PAGE - 1;   // positions from a page's start on
+  const long long most = std::min((long long)keep_stride, (long long)d.max_pages * TW_PAGE) + TW_PAGE - 1;   // positions from a page's start on
   const bool in_place = !dst_table || dst_table == kv->page_table;
   tw_prof_before(TW_K_COMPACT, s);
   if (!in_place) TW_LAUNCH((compact_kernel<false, 4>), dim3((unsigned)((most + 63) / 64), (unsigned)d.Hkv, (unsigned)d.batch), dim3(256), 0, s, a);

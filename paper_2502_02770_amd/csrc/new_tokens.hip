@@ -27,6 +27,7 @@
 // is 32 matrix instructions of 32 cycles, 16 of which keep the SIMD from issuing vector instructions, and 149 vector
 // instructions of 4 cycles (8 for the 32 exponentials): 1024 cycles of the matrix unit against 1236 of issue.  Two prompts
 // of 8192 tokens under a window of 4096: 826 us, 1.00 PFLOP/s of the pairs that are visible; an 8192^3 library product 1.21.
+#include <algorithm>
 #include "tw_common.h"
 
 namespace {
@@ -694,7 +695,7 @@ int rows_per_block(long long rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 
 //   32       160        8: 10.3 / 10.8 12: 11.0 / 12.5 16: 13.7 / 18.2     128 rows   12: 14.8 / 14.9  16: 16.9 / 22.4  26: 25.5 / 34.6
 // Nor are the row blocks of chunks and prompts under a window that fill the chip by themselves: their lists are alike.
 bool cut_lists(bool window, int blocks, long long lists, long long longest) {
-  if (longest <= min(32ll, 6 + lists / 32)) return false;
+  if (longest <= std::min(32ll, 6 + lists / 32)) return false;
   return !(window && blocks >= 8 && lists >= 2ll * tw_num_cus());
 }
 
@@ -704,7 +705,7 @@ int launch_new(NewArgs a, hipStream_t s) {
   const long long lists = (long long)a.rb_max * a.batch * a.Hkv;
   long long longest = ((long long)a.max_pages * TW_PAGE + TILE - 1) / TILE;      // tiles that a list can have
   if (MODE == MODE_WINDOW)
-    longest = min(longest, (((long long)a.sinks + TW_PAGE - 1) / TW_PAGE + ((long long)a.window + M / a.G + TW_PAGE - 2) / TW_PAGE + 1 + 3) / 4);
+    longest = std::min(longest, (((long long)a.sinks + TW_PAGE - 1) / TW_PAGE + ((long long)a.window + M / a.G + TW_PAGE - 2) / TW_PAGE + 1 + 3) / 4);
   a.stream = a.rb_max == 1 && lists * longest > STREAM_TILES;
   tw_prof_before(TW_K_NEW_TOKENS, s);
   if (!cut_lists(MODE == MODE_WINDOW, a.rb_max, lists, longest)) {
@@ -713,7 +714,7 @@ int launch_new(NewArgs a, hipStream_t s) {
   }
   // resident workgroups (64 KiB of LDS each, two to a CU), no more than the lists could make items
   const long long most = lists * ((longest + PLAN_MIN_TILES - 1) / PLAN_MIN_TILES);
-  TW_LAUNCH((new_tokens_kernel<MODE, WR, WT, true>), dim3((unsigned)min(most, 2ll * a.cus)), dim3(64 * WR * WT), 0, s, a);
+  TW_LAUNCH((new_tokens_kernel<MODE, WR, WT, true>), dim3((unsigned)std::min(most, 2ll * a.cus)), dim3(64 * WR * WT), 0, s, a);
   if (int e = tw_prof_after(s)) return e;
   tw_prof_before(TW_K_NEW_COMBINE, s);
   const long long rows = (long long)a.max_new * a.Hq;

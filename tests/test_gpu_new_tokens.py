@@ -299,6 +299,12 @@ def test_pages_of_sinks_and_pages_of_the_window_in_one_tile(hq, hkv, new, sinks)
         run_window(c, [min(n, new) for n in lens], new, window, sinks, seed=window)
 
 
+def test_a_table_with_room_for_more_work_than_32_bits_count():
+    """Row blocks x tiles that the arguments allow are 2^33; the sequences are short."""
+    c = Cache([200, 0, 77, 1000], 64, 8, seed=3, max_pages=1 << 24)
+    run_tree(c, [3, 0, 20, 9], 1024, seed=5)
+
+
 def test_a_window_over_freed_pages():
     """Pages between the sinks and the window have been given back."""
     c = Cache([5000], 8, 2, seed=12)

@@ -177,6 +177,27 @@ def test_copied_pages(bits, hkv):
         assert torch.equal(getattr(c, n).view(torch.uint8), before[n].view(torch.uint8)), n
 
 
+def test_more_copies_than_32_bits_count():
+    """2^31 (pair, KV head) items, all but two of them passed over."""
+    c = cache_of([[0]], [1], 5, 8, 8)
+    src = torch.full((1 << 28,), -1, dtype=torch.int32, device="cuda")
+    dst = src.clone()
+    src[[0, -1]], dst[[0, -1]] = i32([3, 1]), i32([0, 4])
+    before = {n: getattr(c, n).clone() for n in POOLS}
+    c.copy_pages(src, dst)
+    for n in POOLS:
+        before[n][0], before[n][4] = before[n][3], before[n][1]
+        assert torch.equal(getattr(c, n).view(torch.uint8), before[n].view(torch.uint8)), n
+
+
+def test_a_reservation_of_any_number_is_clipped_to_the_row():
+    c = cache_of([[-1] * 6, [-1] * 6], [0, 17], 20)
+    import paper_2502_02770_amd as T
+    pp = T.PagePool(c)
+    pp.reserve(i32([2**31 - 1, 2**31 - 1]), 2**31 - 1)
+    assert c.page_table.tolist() == [[0, 1, 2, 3, 4, 5], [-1, 6, 7, 8, 9, 10]] and int(pp.status) == 0
+
+
 def compact_model(c, keep, count, start, to):
     """-> pools after, and the bounds' pages that are taken again {(page): rows valid}"""
     p = {n: getattr(c, n).clone().cpu() for n in POOLS}

@@ -58,10 +58,13 @@ class PagedKV:
 
     def copy_pages(self, src, dst):
         """twilight_pages_copy: whole pages src[i] -> dst[i] of this layer; negative entries are passed over."""
+        assert src.shape == dst.shape, "a destination per source"
         B.twilight_pages_copy(self.kv, src, dst, src.numel())
 
     def compact(self, keep_idx, keep_count, dst_start, dst_table=None):
         """twilight_tokens_compact; does not change seq_lens."""
+        assert keep_idx.dim() == 2 and keep_idx.shape[0] == keep_count.numel() == dst_start.numel() == self.batch, "a row per sequence"
+        assert dst_table is None or dst_table.shape == self.page_table.shape, "a destination table like the cache's"
         B.twilight_tokens_compact(self.kv, keep_idx, keep_count, keep_idx.shape[1], dst_start, dst_table)
 
 
@@ -91,10 +94,12 @@ class PagePool:
 
     def reserve(self, n_new, max_new):
         """Pages for the next n_new[b] positions of every sequence (seq_lens not yet advanced)."""
+        assert n_new.numel() == self.cache.batch, "a count per sequence"
         B.twilight_pages_reserve(self.cache.kv, n_new, max_new, self.ref_count, self.status, self._workspace(max_new, 0))
 
     def free(self, first_page, end_page):
         """Logical pages first_page[b] .. end_page[b] - 1 of every row given back."""
+        assert first_page.numel() == end_page.numel() == self.cache.batch, "a range per sequence"
         B.twilight_pages_free(self.cache.kv, first_page, end_page, self.ref_count, self.status)
 
     def free_behind(self, window, num_sinks):
@@ -124,13 +129,20 @@ class NewTokens:
         self.lse = torch.zeros(rows, c.Hq, dtype=torch.float32, device=c.device) if with_lse else None
         self.ws = torch.empty(B.twilight_workspace_bytes(B.TW_WS_NEW_TOKENS, c.kv, self.max_new), dtype=torch.uint8, device=c.device)
 
+    def _check(self, q, n_new):
+        assert q.shape == self.out.shape, "q [batch * max_new, heads, 128]"
+        assert n_new is None or n_new.numel() == self.cache.batch, "a count per sequence"
+
     def tree(self, q, tree_mask, n_new=None):
         """A drafted tree per sequence; tree_mask i32 [rows, words] (tree_mask_of_parents)."""
+        self._check(q, n_new)
+        assert tree_mask.dim() == 2 and tree_mask.shape[0] == q.shape[0], "a mask row per row of q"
         B.twilight_tree_attention(self.cache.kv, q, n_new, None, self.max_new, tree_mask, tree_mask.shape[1], self.out, self.lse, self.ws)
         return self.out
 
     def window(self, q, window, num_sinks=0, n_new=None):
         """Consecutive tokens under a sliding window with sinks."""
+        self._check(q, n_new)
         B.twilight_window_attention(self.cache.kv, q, n_new, None, self.max_new, window, num_sinks, self.out, self.lse, self.ws)
         return self.out
 

@@ -98,6 +98,41 @@ def test_page_operators_refuse(T):
     assert L.twilight_pages_free(ref(no_table), ONE, ONE, ONE, ONE, None) == -1
 
 
+def test_more_page_requests_than_are_counted_in_32_bits(T):
+    L, kv = T.binding.lib(), _kv(T, batch=256, max_pages=1 << 24)
+    assert L.twilight_pages_reserve(ctypes.byref(kv), ONE, 2**31 - 1, ONE, ONE, ONE, PLENTY, None) == -1
+    kv = _kv(T, batch=128, max_pages=1 << 24)
+    assert L.twilight_pages_reserve(ctypes.byref(kv), ONE, 2**31 - 1, ONE, ONE, ONE, PLENTY, None) == -1
+
+
+def test_workspace_of_a_bound_near_the_largest_int(T):
+    """max_new + 15 does not wrap: every page of the pool at most."""
+    kv = _kv(T)
+    assert 64 * 4 <= T.twilight_workspace_bytes(T.TW_WS_PAGES, kv, 2**31 - 1, 0) <= 4096
+    assert T.twilight_workspace_bytes(T.TW_WS_PAGES, kv, 2**31 - 1, 0) == T.twilight_workspace_bytes(T.TW_WS_PAGES, kv, 10**6, 0)
+
+
+def test_shapes_that_do_not_fit_the_batch_are_refused(T):
+    """Before anything reaches the GPU: lists, queries and masks with another number of rows than the cache has."""
+    i32 = lambda *n: torch.zeros(*n, dtype=torch.int32)
+    c = object.__new__(T.PagedKV)
+    c.batch, c.Hq, c.kv, c.page_table, c.device = 3, 8, None, i32(3, 5), "cpu"
+    p = object.__new__(T.PagePool)
+    p.cache = c
+    st = object.__new__(T.NewTokens)
+    st.cache, st.max_new, st.out = c, 4, torch.zeros(12, 8, 128, dtype=torch.bfloat16)
+    q = lambda rows, heads=8: torch.zeros(rows, heads, 128, dtype=torch.bfloat16)
+    for call in (lambda: c.copy_pages(i32(4), i32(3)),
+                 lambda: c.compact(i32(2, 6), i32(3), i32(3)), lambda: c.compact(i32(3, 6), i32(2), i32(3)), lambda: c.compact(i32(3, 6), i32(3), i32(4)),
+                 lambda: c.compact(i32(18), i32(3), i32(3)), lambda: c.compact(i32(3, 6), i32(3), i32(3), i32(3, 4)),
+                 lambda: p.reserve(i32(2), 4), lambda: p.free(i32(3), i32(2)), lambda: p.free(i32(2), i32(2)),
+                 lambda: st.window(q(3), 64), lambda: st.window(q(12, 4), 64), lambda: st.window(q(12), 64, n_new=i32(2)),
+                 lambda: st.tree(q(3), i32(3, 1)), lambda: st.tree(q(12), i32(3, 1)), lambda: st.tree(q(12), i32(12)),
+                 lambda: st.tree(q(12), i32(12, 1), n_new=i32(4))):
+        with pytest.raises(AssertionError, match="per|batch|like"):
+            call()
+
+
 def test_workspace_sizes_of_the_new_operators(T):
     kv = _kv(T)
     assert T.twilight_workspace_bytes(T.TW_WS_NEW_TOKENS, kv, 0) == T.twilight_workspace_bytes(T.TW_WS_NEW_TOKENS, kv, (1 << 20) + 1) == 0

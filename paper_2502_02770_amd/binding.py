@@ -253,7 +253,7 @@ def twilight_tree_attention(kv, q, n_new, new_offsets, max_new, tree_mask, mask_
 
 def twilight_window_attention(kv, q, n_new, new_offsets, max_new, window, num_sinks, out, lse, ws):
     _check(lib().twilight_window_attention(ctypes.byref(kv), _rows(q), _ints(n_new), _ints(new_offsets), int(max_new),
-                                           int(window), int(num_sinks), _rows(out), _sums(lse),
+                                           min(int(window), 2**31 - 1), min(int(num_sinks), 2**31 - 1), _rows(out), _sums(lse),
                                            _ptr(ws), ws.numel() * ws.element_size(), _stream_of(q)))
 
 

@@ -305,6 +305,11 @@ def test_a_table_with_room_for_more_work_than_32_bits_count():
     run_tree(c, [3, 0, 20, 9], 1024, seed=5)
 
 
+@pytest.mark.parametrize("window,sinks", [(2**32 + 5, 0), (2**63 - 1, 3), (5, 2**32 + 1)])
+def test_windows_and_sinks_beyond_32_bits_are_no_limit(window, sinks):
+    run_window(Cache([300, 40], 8, 2, seed=6), [7, 40], 40, window, sinks)
+
+
 def test_a_window_over_freed_pages():
     """Pages between the sinks and the window have been given back."""
     c = Cache([5000], 8, 2, seed=12)

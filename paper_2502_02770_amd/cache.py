@@ -104,8 +104,7 @@ class PagePool:
 
     def free_behind(self, window, num_sinks):
         """The pages given back that neither the sinks nor the window of the next token reaches (twilight_window_attention)."""
-        lens = self.cache.seq_lens
-        self.free(torch.full_like(lens, -(-num_sinks // 16)), torch.clamp((lens + 1 - window) // 16, min=0))
+        self.free(*pages_behind(self.cache.seq_lens, window, num_sinks))
 
     def fork(self, parent):
         """-> (new_table, new_lens, copy_src, copy_dst) of the batch whose row i continues row parent[i]; every layer then
@@ -116,6 +115,16 @@ class PagePool:
         src, dst = torch.empty(n, **i32), torch.empty(n, **i32)
         B.twilight_pages_fork(c.kv, parent, n, table, lens, self.ref_count, src, dst, self.status, self._workspace(0, n))
         return table, lens, src, dst
+
+
+def pages_behind(seq_lens, window, num_sinks):
+    """-> (first, end) i32 [batch]: the logical pages of every sequence that lie between the sinks and the window of the next
+    token, which stands at position seq_lens[b].  Windows and sinks of any size, as NewTokens.window takes them."""
+    assert window >= 1 and num_sinks >= 0, "a window of one token at least, and no fewer than no sinks"
+    window, num_sinks = min(int(window), 2**31 - 1), min(int(num_sinks), 2**31 - 1)
+    # (differences of two numbers that are not negative stay in 32 bits)
+    behind = torch.clamp(torch.clamp(seq_lens, min=0) - (window - 1), min=0)
+    return torch.full_like(seq_lens, -(-num_sinks // 16)), behind // 16
 
 
 class NewTokens:

@@ -1,0 +1,44 @@
+"""Arguments at the ends of their ranges for the operators on new tokens and on the cache's pages: what needs no GPU."""
+import numpy as np
+import pytest
+import torch
+
+
+@pytest.mark.parametrize("window", [1, 2, 16, 17, 40, 1000, 2**31 - 1, 2**31, 2**32, 2**32 + 5, 2**40, 2**63 - 1])
+@pytest.mark.parametrize("sinks", [0, 1, 16, 33, 2**31 - 1, 2**32 + 1, 2**36])
+def test_pages_behind_a_window(window, sinks):
+    """Exactly the pages none of whose tokens the next token sees; the entry's definition, one page at a time."""
+    from paper_2502_02770_amd.cache import pages_behind
+    lens = [0, 1, 15, 16, 64, 100, 1000, 5000]
+    first, end = pages_behind(torch.tensor(lens, dtype=torch.int32), window, sinks)
+    assert first.dtype == end.dtype == torch.int32 and (first >= 0).all() and (end >= 0).all()
+    for n, lo, hi in zip(lens, first.tolist(), end.tolist()):
+        unseen = {p for p in range(n // 16) if all(n - t >= window and t >= sinks for t in range(16 * p, 16 * p + 16))}
+        assert set(range(lo, hi)) == unseen, n
+
+
+@pytest.mark.parametrize("window", [2**31 - 1, 2**32, 2**40, 2**63 - 1])
+def test_nothing_is_given_back_behind_a_window_without_limit(window):
+    import paper_2502_02770_amd as T
+    p = object.__new__(T.PagePool)
+    p.cache = object.__new__(T.PagedKV)
+    p.cache.seq_lens, p.cache.batch, given = torch.tensor([1000, 64], dtype=torch.int32), 2, []
+    p.free = lambda first, end: given.append((first.tolist(), end.tolist()))
+    p.free_behind(window, 4)
+    p.free_behind(40, 2**36)                                       # sinks without limit
+    for first, end in given:
+        assert all(hi <= lo for lo, hi in zip(first, end)), (first, end)
+
+
+def test_lengths_outside_a_row_give_back_nothing_by_a_wrap():
+    from paper_2502_02770_amd.cache import pages_behind
+    lens = torch.tensor([-5, -2**31, 2**31 - 1], dtype=torch.int32)
+    assert pages_behind(lens, 2**63 - 1, 0)[1].tolist() == [0, 0, 0]
+    assert pages_behind(lens, 1, 0)[1].tolist() == [0, 0, (2**31 - 1) // 16]
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (-1, 0), (-2**40, 0), (5, -1), (5, -2**33)])
+def test_windows_and_sinks_that_attention_refuses(window, sinks):
+    from paper_2502_02770_amd.cache import pages_behind
+    with pytest.raises(AssertionError, match="window"):
+        pages_behind(torch.tensor([100], dtype=torch.int32), window, sinks)

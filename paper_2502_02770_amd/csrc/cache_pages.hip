@@ -43,7 +43,7 @@ __device__ __forceinline__ int row_len(const PagesArgs& a, int b) {
 // Every entry of the range loses its page.  Bound by the atomics' trips to memory; one thread per entry, all rows at once.
 __global__ __launch_bounds__(256) void pages_free_kernel(PagesArgs a) {
   const int b = blockIdx.y;
-  const int lo = max(a.first[b], 0), hi = min(a.end[b], a.max_pages);
+  const int lo = min(max(a.first[b], 0), a.max_pages), hi = min(a.end[b], a.max_pages);   // (both: what is added to lo stays in 32 bits)
   for (int p = lo + (int)(blockIdx.x * 256 + threadIdx.x); p < hi; p += (int)gridDim.x * 256) {
     int32_t* e = a.table + (long long)b * a.max_pages + p;
     const int id = *e;

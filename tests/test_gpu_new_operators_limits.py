@@ -18,3 +18,24 @@ def test_windows_and_sinks_without_limit_keep_every_page(window, sinks):
     table, count = c.page_table.clone(), p.ref_count.clone()
     p.free_behind(window, sinks)
     assert torch.equal(c.page_table, table) and torch.equal(p.ref_count, count) and int(p.status) == 0
+
+
+@pytest.mark.parametrize("max_pages", [1, 7, 300, 20000])
+def test_ranges_of_pages_far_outside_the_row(max_pages):
+    """First and last pages of any 32-bit value: what lies in the row is given back, nothing else is touched."""
+    import paper_2502_02770_amd as T
+    most, least = 2**31 - 1, -2**31
+    ranges = [(most, 0), (most, most), (least, least), (most, least), (least, 0), (max_pages, most), (most - 5, most), (max_pages + 1, 0),
+              (0, least), (least, 2), (max_pages - 1, most), (0, 0)]
+    n = len(ranges)
+    # rows of others on both sides of every row: the whole table is checked
+    table = np.arange(n * max_pages, dtype=np.int32).reshape(n, max_pages)
+    c = cache_of(table, [0] * n, n * max_pages, 1, 1, fill=False)
+    p = T.PagePool(c)
+    p.free(i32([r[0] for r in ranges]), i32([r[1] for r in ranges]))
+    for b, (lo, hi) in enumerate(ranges):
+        table[b, max(lo, 0):max(0, min(hi, max_pages))] = -1
+    assert np.array_equal(c.page_table.cpu().numpy(), table) and int(p.status) == 0
+    count = np.ones(n * max_pages, dtype=np.int32)
+    count[np.setdiff1d(np.arange(n * max_pages), table[table >= 0])] = 0
+    assert np.array_equal(p.ref_count.cpu().numpy(), count)

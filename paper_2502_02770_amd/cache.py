@@ -157,12 +157,13 @@ class NewTokens:
 
 
 def tree_mask_of_parents(parents):
-    """Mask words [..., ceil(n / 32)] (i32) of drafted trees from their parents [..., n] (before their children; -1: the last
-    cached token): every token sees its ancestors and itself."""
+    """Mask words [..., ceil(n / 32)] (i32) of drafted trees from their parents [..., n] (before their children; -1, or whatever
+    else is no token before the child: the last cached token): every token sees its ancestors and itself."""
     n = parents.shape[-1]
     see = torch.zeros(*parents.shape, -(-n // 32) * 32, dtype=torch.bool, device=parents.device)
     for j in range(n):
         up = parents[..., j].long()
+        up = torch.where(up < j, up, torch.full_like(up, -1))
         row = torch.take_along_dim(see, up.clamp(min=0)[..., None, None], dim=-2).squeeze(-2) & (up >= 0)[..., None]
         row[..., j] = True
         see[..., j, :] = row

@@ -42,3 +42,28 @@ def test_windows_and_sinks_that_attention_refuses(window, sinks):
     from paper_2502_02770_amd.cache import pages_behind
     with pytest.raises(AssertionError, match="window"):
         pages_behind(torch.tensor([100], dtype=torch.int32), window, sinks)
+
+
+def ancestors(parents):
+    """Bits of a tree's masks, one token and one step towards the root at a time."""
+    see = np.zeros((len(parents), -(-len(parents) // 32) * 32), dtype=bool)
+    for j in range(len(parents)):
+        k = j
+        while True:
+            see[j, k] = True
+            up = int(parents[k])
+            if not 0 <= up < k:
+                break
+            k = up
+    return np.packbits(see, axis=1, bitorder="little").view(np.int32)
+
+
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+def test_parents_that_are_no_earlier_token_stand_for_the_cache(dtype):
+    """Beyond the draft, the token itself or a later one, negative: nothing outside the masks is read."""
+    from paper_2502_02770_amd.cache import tree_mask_of_parents
+    top = torch.iinfo(dtype).max
+    p = torch.tensor([[0, 0, 5, 9, 40, 3], [-7, top, -top, 1, 3, 4], [3, 2, 2, 2, 6, 33]], dtype=dtype)
+    got = tree_mask_of_parents(p).numpy()
+    for b in range(3):
+        assert np.array_equal(got[b], ancestors(p[b].tolist())), b

@@ -39,3 +39,22 @@ def test_ranges_of_pages_far_outside_the_row(max_pages):
     count = np.ones(n * max_pages, dtype=np.int32)
     count[np.setdiff1d(np.arange(n * max_pages), table[table >= 0])] = 0
     assert np.array_equal(p.ref_count.cpu().numpy(), count)
+
+
+def test_masks_on_the_device_and_in_a_graph():
+    from paper_2502_02770_amd.cache import tree_mask_of_parents
+    rng = np.random.default_rng(0)
+    ps = [i32(np.floor(rng.random((5, 130)) * (np.arange(130) + 1)) - 1) for _ in range(2)]
+    ps[1][2, 7:40] = 2**31 - 1                                     # no tokens of the draft
+    want = [tree_mask_of_parents(p.cpu()).cuda() for p in ps]
+    at = ps[0].clone()
+    assert torch.equal(tree_mask_of_parents(at), want[0])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = tree_mask_of_parents(at)
+    for turn in range(4):
+        at.copy_(ps[turn % 2])
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want[turn % 2])

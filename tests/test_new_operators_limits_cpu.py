@@ -67,3 +67,33 @@ def test_parents_that_are_no_earlier_token_stand_for_the_cache(dtype):
     got = tree_mask_of_parents(p).numpy()
     for b in range(3):
         assert np.array_equal(got[b], ancestors(p[b].tolist())), b
+
+
+@pytest.mark.parametrize("shape", [(0,), (1,), (2, 0), (2,), (1, 33), (3, 2, 64), (2, 200), (1024,)])
+@pytest.mark.parametrize("kind", ["any", "chain", "star"])
+def test_masks_of_trees_of_any_depth(shape, kind):
+    from paper_2502_02770_amd.cache import tree_mask_of_parents
+    n, rng = shape[-1], np.random.default_rng(shape[-1])
+    p = np.broadcast_to(np.arange(n) - 1, shape) if kind == "chain" else np.zeros(shape) if kind == "star" else (
+        np.floor(rng.random(shape) * (np.arange(n) + 1)) - 1)
+    got = tree_mask_of_parents(torch.from_numpy(p.astype(np.int32)))
+    assert got.shape == (*shape, -(-n // 32)) and got.dtype == torch.int32 and got.is_contiguous()
+    for tree, words in zip(p.reshape(-1, n), got.reshape(-1, n, got.shape[-1]).numpy()) if n else ():
+        assert np.array_equal(words, ancestors(tree))
+
+
+def test_masks_take_steps_of_the_logarithm_of_the_draft():
+    """A draft of 128 tokens: operations of torch, each a launch of some microseconds ahead of the attention."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+    from paper_2502_02770_amd.cache import tree_mask_of_parents
+
+    class Count(TorchDispatchMode):
+        n = 0
+
+        def __torch_dispatch__(self, f, types, args=(), kwargs=None):
+            Count.n += 1
+            return f(*args, **(kwargs or {}))
+
+    with Count():
+        tree_mask_of_parents(torch.arange(-1, 127, dtype=torch.int32).expand(4, 128))
+    assert Count.n <= 30 + 10 * 7, Count.n                         # per step two look-ups of a few operations each and a union

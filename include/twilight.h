@@ -388,7 +388,8 @@ int twilight_sparse_decode_per_head(const twilight_kv_t* kv, const void* q, cons
  *                  num_kv_heads < 2^24
  *   out            bf16 [rows][num_q_heads][128], not overlapping q; rows of no
  *                  token are left
- *   lse            fp32 [rows][num_q_heads] or NULL, as twilight_sparse_decode
+ *   lse            fp32 [rows][num_q_heads] or NULL: natural-log log-sum-exp of
+ *                  the scaled logits (-inf: nothing seen; NaN where out is)
  *   ws             >= twilight_workspace_bytes(TW_WS_NEW_TOKENS, kv, max_new, 0),
  *                  for one call at a time
  * q, out, ws and the pools are 16-byte aligned (TW_EINVAL).  The rows of V of

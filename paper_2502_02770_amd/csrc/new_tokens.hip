@@ -260,6 +260,9 @@ __device__ __forceinline__ bool whole_item(const NewArgs& a, Item* it) {
   return it->rb * M < it->n * a.G;
 }
 
+// log-sum-exp of a row; -inf where it saw nothing (l = 0 and no NaN: a row with one has to show it)
+__device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * kLn2n; }
+
 // The 16 rows of a page's K and V for one head, 16 bytes per lane.  HINT 2: non-temporal.
 template <int HINT>
 __device__ __forceinline__ void page_to_lds(const char* kp, const char* vp, unsigned k_off, unsigned v_off, unsigned char* dst) {
@@ -568,7 +571,7 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
   }
   if (!live) return;
   if (!SPLIT || it.chunks == 1) {
-    const float inv = l > 0.f ? 1.0f / l : 0.f;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
     uint2* orow = a.out + qrow * 32;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -579,7 +582,7 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
         for (int i = 0; i < 4; ++i) w.e[i] = (__bf16)(o[d][4 * k + i] * inv);
         orow[8 * d + 2 * k + half] = w.v;
       }
-    if (a.lse && half == 0) a.lse[qrow] = l > 0.f ? (m + __log2f(l)) * kLn2n : -__builtin_inff();
+    if (a.lse && half == 0) a.lse[qrow] = row_lse(m, l);
     return;
   }
   const long long prow = (long long)it.slot * M + wr * 32 + (lane & 31);
@@ -674,11 +677,11 @@ __global__ __launch_bounds__(256) void new_tokens_combine_kernel(NewArgs a) {
   }
   if (!live || (lane >> 5)) return;
   const long long qrow = (long long)((a.offsets ? a.offsets[b] : b * a.max_new) + tok) * a.Hq + head;
-  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
   union { __bf16 e[4]; uint2 v; } w;
   w.e[0] = (__bf16)(o.x * inv); w.e[1] = (__bf16)(o.y * inv); w.e[2] = (__bf16)(o.z * inv); w.e[3] = (__bf16)(o.w * inv);
   a.out[qrow * 32 + dl] = w.v;
-  if (a.lse && lane == 0) a.lse[qrow] = l > 0.f ? (m + __log2f(l)) * kLn2n : -__builtin_inff();
+  if (a.lse && lane == 0) a.lse[qrow] = row_lse(m, l);
 }
 
 // ---------------------------------------------------------------- host side

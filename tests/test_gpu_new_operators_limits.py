@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+from tests.test_gpu_new_tokens import Cache, queries, run_tree, run_window, sent, workspace
 from tests.test_gpu_pages import cache_of, i32
 
 pytestmark = pytest.mark.gpu
@@ -58,3 +59,24 @@ def test_masks_on_the_device_and_in_a_graph():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, want[turn % 2])
+
+
+@pytest.mark.parametrize("hq,hkv", [(8, 8), (16, 2)])
+@pytest.mark.parametrize("n,new", [(70, 1), (70, 9), (3000, 1), (3000, 9), (3000, 40)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_rows_that_are_not_finite_show_it_in_lse_too(n, new, hq, hkv, bad):
+    """-inf stands for rows that see nothing; lists taken whole and cut ones."""
+    import paper_2502_02770_amd as T
+    c = Cache([n], hq, hkv, seed=n)
+    q = queries(new, hq, 1)
+    q[new // 2, 3] = bad                                           # inf: scores of either infinity
+    mask = np.full((new, -(-new // 32)), -1, dtype=np.int32)
+    calls = (lambda o, l: T.twilight_window_attention(c.kv, q, None, None, new, 2**31 - 1, 0, o, l, workspace(c.kv, new)),
+             lambda o, l: T.twilight_tree_attention(c.kv, q, None, None, new, i32(mask), mask.shape[1], o, l, workspace(c.kv, new)))
+    for call in calls:
+        out, lse = sent(q, hq)
+        call(out, lse)
+        mine = torch.zeros(new, hq, dtype=torch.bool, device="cuda")
+        mine[new // 2, 3] = True
+        assert torch.isnan(out[mine]).all() and torch.isnan(lse[mine]).all()
+        assert torch.isfinite(out[~mine]).all() and torch.isfinite(lse[~mine]).all()

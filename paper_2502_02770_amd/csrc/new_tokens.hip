@@ -40,7 +40,8 @@ typedef float tw_f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kScaleLog2 = 0.08838834764831845f * 1.4426950408889634f;   // log2(e) / sqrt(128)
 constexpr float kLn2n = 0.6931471805599453f;
-constexpr float kLow = -1e30f;                   // running maximum before any visible token: exp2(-inf - kLow) = 0
+constexpr float kLow = -3.4028234663852886e38f;  // running maximum before any visible token, the lowest number: exp2(-inf - kLow) = 0
+constexpr float kFar = 1073741824.f;             // from an |m| of 2^30 on, a row's scores are told apart by their own steps, 64 and more
 constexpr float kGrowth = 8.f;                   // by how much (in powers of 2) a row's scores may exceed its m before m follows
 constexpr int TILE = 64, TILE_BYTES = TILE * 256;
 enum { MODE_TREE = 0, MODE_WINDOW = 1 };
@@ -212,7 +213,8 @@ __device__ __forceinline__ bool find_item(const NewArgs& a, int lane, int chunk,
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     if (a.batch > 64) seq = seq_of<MODE, M>(a, b0 + lane);
     const int chunks = (int)quotient((uint32_t)(seq.tiles + chunk - 1), (uint32_t)chunk);
-    const uint32_t mine = (uint32_t)(seq.lists * chunks), part = chunks > 1 ? mine : 0u;
+    const int lists = (seq.n * a.G + M - 1) / M * a.Hkv;             // (again, as it would be a register of the whole walk)
+    const uint32_t mine = (uint32_t)(lists * chunks), part = chunks > 1 ? mine : 0u;
     const uint32_t ie = tw_wave_scan_u32(mine), se = tw_wave_scan_u32(part);
     if (want == 0 && threadIdx.x < 64 && b0 + lane < a.batch) {         // for the combine kernel
       a.ws_plan[2 * (b0 + lane)] = chunks;
@@ -228,7 +230,7 @@ __device__ __forceinline__ bool find_item(const NewArgs& a, int lane, int chunk,
       it->len = __builtin_amdgcn_readlane(seq.len, l);
       it->off = __builtin_amdgcn_readlane(seq.off, l);
       it->chunks = __builtin_amdgcn_readlane(chunks, l);
-      const uint32_t all = (uint32_t)__builtin_amdgcn_readlane(seq.lists, l);
+      const uint32_t all = (uint32_t)__builtin_amdgcn_readlane(lists, l);
       it->chunk = (int)quotient(k, all);
       const uint32_t rest = k - (uint32_t)it->chunk * all;
       it->rb = (int)quotient(rest, (uint32_t)a.Hkv);
@@ -377,6 +379,11 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
   float m = kLow, l = 0.f;                       // m: of the whole row; l: of this lane's tokens
+  // A weight is exp2(fma(score, c, -m)) with c = log2(e)/sqrt(128).  The fma keeps what rounding took off m = score * c of the
+  // largest score, 2^-24 of it: from 2^30 on, where that leaves an exponent's range, m is kept with c = 1/4, which rounds nothing
+  // (and scores that differ at all differ by 64 powers of two).  Then |m| is more than 2^30 whatever the score, which tells.
+  auto scale_of = [](float m) -> float { return __builtin_fabsf(m) < kFar ? kScaleLog2 : 0.25f; };
+  auto m_log2 = [&]() -> float { return __builtin_fabsf(m) < kFar ? m : m * kScaleLog2 * 4.f; };
 
   // the mask words of this lane's row that a tile's positions stand in, asked for ahead of the next tile's rows, so that they
   // are not waited for behind those
@@ -492,22 +499,23 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
     }
-    const float mn = fmaxf(m, mx * kScaleLog2);
-    if (__any(mn > m + kGrowth)) {
-      const float al = __builtin_amdgcn_exp2f(m - mn);
+    float c = scale_of(m);
+    if (__any(mx * c > m + kGrowth)) {
+      const float was = m_log2(), mn = fmaxf(was, mx * kScaleLog2), al = __builtin_amdgcn_exp2f(was - mn);
       l *= al;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= al;
-      m = mn;
+      if (mn > was) m = __builtin_fabsf(mn) < kFar ? mn : mx * 0.25f;
+      c = scale_of(m);
     }
     tw_bf16x8 p[2 * MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][r], kScaleLog2, -m));
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][r], c, -m));
         l += w;
         p[2 * mt + r / 8][r % 8] = (__bf16)w;
       }
@@ -542,6 +550,7 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
   }
 
   // ---- the waves' states of the same rows merged
+  m = m_log2();
   {
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
@@ -624,7 +633,7 @@ __global__ __launch_bounds__(256, 2) void new_tokens_kernel(NewArgs a) {
     return;
   }
   Seq seq;
-  const int chunk = plan_chunk<MODE, M>(a, lane, &seq, &stream);
+  const int chunk = __builtin_amdgcn_readfirstlane(plan_chunk<MODE, M>(a, lane, &seq, &stream));
   uint32_t want = blockIdx.x;
   while (find_item<MODE, M>(a, lane, chunk, seq, want, &it)) {
     attend_item<MODE, WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave, stream);

@@ -80,3 +80,81 @@ def test_rows_that_are_not_finite_show_it_in_lse_too(n, new, hq, hkv, bad):
         mine[new // 2, 3] = True
         assert torch.isnan(out[mine]).all() and torch.isnan(lse[mine]).all()
         assert torch.isfinite(out[~mine]).all() and torch.isfinite(lse[~mine]).all()
+
+
+@pytest.mark.parametrize("new", [1, 9, 40])
+@pytest.mark.parametrize("n,size", [(70, 2.0**50), (3000, 2.0**50), (3000, 2.0**57), (3000, -2.0**57), (70, 2.0**62)])
+def test_scores_far_below_and_above(n, size, new):
+    """All scores of a row alike and up to 2^123 from 0, exactly: q and K are powers of two.  The weights are 1 / visible, the
+    output the mean of V."""
+    import paper_2502_02770_amd as T
+    c = Cache([n], 8, 2, seed=n)
+    pages = c.table[0, :-(-n // 16)].long()
+    k = torch.full((len(pages) * 16, 2, 128), -2.0**57, dtype=torch.bfloat16, device="cuda")
+    k[n:] = math.nan
+    c.k[pages] = k.view(-1, 16, 2, 128).transpose(1, 2)
+    q = torch.full((new, 8, 128), size, device="cuda").to(torch.bfloat16)
+    if abs(size) == 2.0**62:                                       # one dim decides: 2^119
+        q[..., 1:] = 0
+    score = -float(q[0, 0].double().sum()) * 2.0**57 / math.sqrt(128)
+    assert 1e30 < abs(score) < 1e38
+    ref = Cache([n], 8, 2, seed=n)                                 # (V again)
+    v = ref.logical[0][1].double()
+    mask = np.full((new, -(-new // 32)), -1, dtype=np.int32)
+    out, lse = sent(q, 8)
+    calls = ((lambda: T.twilight_window_attention(c.kv, q, None, None, new, 2**31 - 1, 0, out, lse, workspace(c.kv, new)), True),
+             (lambda: T.twilight_tree_attention(c.kv, q, None, None, new, i32(mask), mask.shape[1], out, lse, workspace(c.kv, new)), False))
+    for call, causal in calls:
+        call()
+        for i in range(new):
+            seen = v[:n - new + i + 1] if causal else v
+            want, mean = seen.mean(0).repeat_interleave(4, 0), seen.abs().mean(0).repeat_interleave(4, 0)
+            # equal weights: the output's rounding and that of a weight, and the sums in fp32
+            assert ((out[i].double() - want).abs() <= 2.0**-8 * want.abs() + (2.0**-8 + (n + 300) * 2.0**-24) * mean).all(), i
+            # (a score that far out takes the logarithm's part up: three products' steps in fp32)
+            assert ((lse[i].double() - score).abs() <= 4 * 2.0**-24 * abs(score)).all(), i
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("size", [2.0**10, 2.0**30, 2.0**34, 2.0**36, 2.0**90])
+@pytest.mark.parametrize("n,new", [(70, 9), (3000, 5), (3000, 40)])
+def test_ordinary_scores_among_ones_far_away(n, new, size, sign):
+    """Some tokens' scores are `size` (or twice it) above or below the others, and q.K before scaling exact there: one dim alone
+    makes them.  A far one above takes the row to itself; one below counts where nothing else is seen."""
+    import paper_2502_02770_amd as T
+    c = Cache([n], 8, 2, seed=n)
+    pages = c.table[0, :-(-n // 16)].long()
+    k, v = (x.clone() for x in c.logical[0])
+    rng = np.random.default_rng(n)
+    far = np.zeros(n)
+    pick = rng.permutation(n)[:max(3, n // 9)]
+    far[pick] = rng.choice([1.0, 2.0], len(pick))
+    if sign < 0:
+        far[:n - new + 3] = 1.0                                    # the first rows see nothing else
+    k[:, :, 0] = torch.from_numpy(far).cuda()[:, None].to(torch.bfloat16) * (sign * 2.0**8)
+    far = torch.from_numpy(far).cuda()
+    k[far > 0, :, 1:] = 0
+    full = torch.full((len(pages) * 16, 2, 128), math.nan, dtype=torch.bfloat16, device="cuda")
+    full[:n] = k
+    c.k[pages] = full.view(-1, 16, 2, 128).transpose(1, 2)
+    q = queries(new, 8, 1)
+    q[..., 0] = size * 2.0**-8
+    out, lse = sent(q, 8)
+    T.twilight_window_attention(c.kv, q, None, None, new, 2**31 - 1, 0, out, lse, workspace(c.kv, new))
+    for i in range(new):
+        m = n - new + i + 1
+        for h in range(8):
+            kk, vv, qq = k[:m, h // 4].double(), v[:m, h // 4].double(), q[i, h].double()
+            x = (kk @ qq) / math.sqrt(128)
+            l, w = torch.logsumexp(x, 0), torch.softmax(x, 0)      # (l has no digits left for the sum of the weights at 2^90)
+            # as the definition's test of ordinary scores: products summed in fp32, one fma, exp2; the far ones are exact products
+            mag = ((kk[:, 1:].abs() @ qq[1:].abs()) / math.sqrt(128)).max()
+            e = 130 * 2.0**-24 * mag + 8 * 2.0**-24 * (mag + 1)
+            if size < 2.0**32:                                     # the exponent's own rounding, where both kinds can meet
+                e = e + 2.0**-23 * x.abs().max().clamp(max=200.0)
+            want, mean = w @ vv, w @ vv.abs()
+            # (weights below 2^-126 are 0 in fp32, counted from an m that is up to 2^8 behind: where V of the others is 0 they decide)
+            bound = 2.0**-8 * want.abs() + (2.0**-8 + 2 * e + (m + 300) * 2.0**-24) * mean + 2.0**-117 * vv.abs().sum(0)
+            worst = ((out[i, h].double() - want).abs() - bound).max().item()
+            assert worst <= 0, (i, h, worst)
+            assert (lse[i, h].double() - l).abs() <= e + (m + 300) * 2.0**-24 + 2.0**-21 * (1 + l.abs()), (i, h)

@@ -122,6 +122,18 @@ def _sums(t):
     return t.data_ptr()
 
 
+def _count(x):
+    """A number for an i32 argument, where ctypes would drop the bits beyond."""
+    x = int(x)
+    assert -2**31 <= x < 2**31, "numbers of 32 bits required"
+    return x
+
+
+def _limit(x):
+    """The same for a bound: beyond 32 bits there is none."""
+    return _count(min(int(x), 2**31 - 1))
+
+
 def _stream_of(t):
     """The current stream, on which the call runs: of the tensors' device."""
     d = torch._C._cuda_getDevice()
@@ -246,19 +258,19 @@ def twilight_sparse_decode_per_head(kv, q, kept_count, kept_idx, kept_stride, ou
 
 
 def twilight_tree_attention(kv, q, n_new, new_offsets, max_new, tree_mask, mask_words, out, lse, ws):
-    _check(lib().twilight_tree_attention(ctypes.byref(kv), _rows(q), _ints(n_new), _ints(new_offsets), int(max_new),
-                                         _ints(tree_mask), int(mask_words), _rows(out), _sums(lse),
+    _check(lib().twilight_tree_attention(ctypes.byref(kv), _rows(q), _ints(n_new), _ints(new_offsets), _count(max_new),
+                                         _ints(tree_mask), _count(mask_words), _rows(out), _sums(lse),
                                          _ptr(ws), ws.numel() * ws.element_size(), _stream_of(q)))
 
 
 def twilight_window_attention(kv, q, n_new, new_offsets, max_new, window, num_sinks, out, lse, ws):
-    _check(lib().twilight_window_attention(ctypes.byref(kv), _rows(q), _ints(n_new), _ints(new_offsets), int(max_new),
-                                           min(int(window), 2**31 - 1), min(int(num_sinks), 2**31 - 1), _rows(out), _sums(lse),
+    _check(lib().twilight_window_attention(ctypes.byref(kv), _rows(q), _ints(n_new), _ints(new_offsets), _count(max_new),
+                                           _limit(window), _limit(num_sinks), _rows(out), _sums(lse),
                                            _ptr(ws), ws.numel() * ws.element_size(), _stream_of(q)))
 
 
 def twilight_pages_reserve(kv, n_new, max_new, ref_count, status, ws):
-    _check(lib().twilight_pages_reserve(ctypes.byref(kv), _ints(n_new), int(max_new), _ints(ref_count), _ints(status),
+    _check(lib().twilight_pages_reserve(ctypes.byref(kv), _ints(n_new), _count(max_new), _ints(ref_count), _ints(status),
                                         _ptr(ws), ws.numel() * ws.element_size(), _stream_of(ref_count)))
 
 
@@ -268,18 +280,18 @@ def twilight_pages_free(kv, first_page, end_page, ref_count, status):
 
 
 def twilight_pages_fork(kv, parent, new_batch, new_table, new_lens, ref_count, copy_src, copy_dst, status, ws):
-    _check(lib().twilight_pages_fork(ctypes.byref(kv), _ints(parent), int(new_batch), _ints(new_table), _ints(new_lens),
+    _check(lib().twilight_pages_fork(ctypes.byref(kv), _ints(parent), _count(new_batch), _ints(new_table), _ints(new_lens),
                                      _ints(ref_count), _ints(copy_src), _ints(copy_dst), _ints(status), _ptr(ws),
                                      ws.numel() * ws.element_size(), _stream_of(ref_count)))
 
 
 def twilight_pages_copy(kv, copy_src, copy_dst, n_copy):
-    _check(lib().twilight_pages_copy(ctypes.byref(kv), _ints(copy_src), _ints(copy_dst), int(n_copy), _stream_of(copy_src)))
+    _check(lib().twilight_pages_copy(ctypes.byref(kv), _ints(copy_src), _ints(copy_dst), _count(n_copy), _stream_of(copy_src)))
 
 
 def twilight_tokens_compact(kv, keep_idx, keep_count, keep_stride, dst_start, dst_table):
     """dst_table None: in place."""
-    _check(lib().twilight_tokens_compact(ctypes.byref(kv), _ints(keep_idx), _ints(keep_count), int(keep_stride),
+    _check(lib().twilight_tokens_compact(ctypes.byref(kv), _ints(keep_idx), _ints(keep_count), _count(keep_stride),
                                          _ints(dst_start), _ints(dst_table), _stream_of(keep_idx)))
 
 

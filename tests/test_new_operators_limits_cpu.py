@@ -97,3 +97,46 @@ def test_masks_take_steps_of_the_logarithm_of_the_draft():
     with Count():
         tree_mask_of_parents(torch.arange(-1, 127, dtype=torch.int32).expand(4, 128))
     assert Count.n <= 30 + 10 * 7, Count.n                         # per step two look-ups of a few operations each and a union
+
+
+def _calls(B, n):
+    """Every call of the operators on new tokens and pages with n in one of its sizes."""
+    ws = torch.zeros(4)
+    kv = B.twilight_kv_t()
+    t = None
+    return {
+        "tree max_new": lambda: B.twilight_tree_attention(kv, t, t, t, n, t, 1, t, t, ws),
+        "tree mask_words": lambda: B.twilight_tree_attention(kv, t, t, t, 1, t, n, t, t, ws),
+        "window max_new": lambda: B.twilight_window_attention(kv, t, t, t, n, 1, 0, t, t, ws),
+        "reserve max_new": lambda: B.twilight_pages_reserve(kv, t, n, t, t, ws),
+        "fork new_batch": lambda: B.twilight_pages_fork(kv, t, n, t, t, t, t, t, t, ws),
+        "copy n_copy": lambda: B.twilight_pages_copy(kv, t, t, n),
+        "compact keep_stride": lambda: B.twilight_tokens_compact(kv, t, t, n, t, t),
+        "window": lambda: B.twilight_window_attention(kv, t, t, t, 1, n, 0, t, t, ws),
+        "sinks": lambda: B.twilight_window_attention(kv, t, t, t, 1, 1, n, t, t, ws),
+    }
+
+
+@pytest.mark.parametrize("n", [2**31, 2**32 + 4, 2**63 + 1, -2**31 - 1, -2**32 + 5, -2**40])
+def test_numbers_beyond_32_bits_are_never_cut_to_them(n, monkeypatch):
+    """They are refused; a window and a number of sinks above them are the largest there is, which limits nothing."""
+    from paper_2502_02770_amd import binding as B
+    seen = []
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *args: seen.append([a for a in args if isinstance(a, int)]) or 0
+
+    for f in ("_ints", "_rows", "_sums", "_ptr", "_stream_of"):
+        monkeypatch.setattr(B, f, lambda t: None)
+    monkeypatch.setattr(B, "lib", lambda: Lib())
+    for name, call in _calls(B, n).items():
+        if n > 0 and name in ("window", "sinks"):
+            call()
+            assert 2**31 - 1 in seen[-1], name
+        else:
+            with pytest.raises(AssertionError, match="32 bits"):
+                call()
+    for call in _calls(B, 7).values():
+        call()
+        assert 7 in seen[-1]

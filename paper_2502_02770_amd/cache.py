@@ -47,6 +47,7 @@ class PagedKV:
 
     def over(self, page_table, seq_lens):
         """A cache of another batch over the same pools (rows of a fork, a larger or smaller batch)."""
+        assert page_table.dim() == 2 and seq_lens.numel() == page_table.shape[0], "a length per row of the table"
         c = object.__new__(PagedKV)
         c.__dict__.update(self.__dict__)
         c.page_table = page_table.to(self.device, torch.int32).contiguous()
@@ -82,6 +83,7 @@ class PagePool:
 
     def over(self, cache):
         """The same pool for a cache of another batch (PagedKV.over): counts and status are shared."""
+        assert cache.num_pool_pages == self.ref_count.numel(), "a cache over pools like this one's"
         p = object.__new__(PagePool)
         p.cache, p.ref_count, p.status, p._ws = cache, self.ref_count, self.status, {}
         return p

@@ -140,3 +140,19 @@ def test_numbers_beyond_32_bits_are_never_cut_to_them(n, monkeypatch):
     for call in _calls(B, 7).values():
         call()
         assert 7 in seen[-1]
+
+
+def test_another_batch_that_does_not_fit_is_refused():
+    """Fewer lengths than rows, a table without rows, a pool of another size: the kernels would read past them."""
+    import paper_2502_02770_amd as T
+    i32 = lambda *n: torch.zeros(*n, dtype=torch.int32)
+    c, other = object.__new__(T.PagedKV), object.__new__(T.PagedKV)
+    c.device, c.num_pool_pages, other.num_pool_pages = torch.device("cpu"), 10, 11
+    p = object.__new__(T.PagePool)
+    p.cache, p.ref_count, p.status = c, i32(10), i32(1)
+    for table, lens in ((i32(4, 5), i32(3)), (i32(4, 5), i32(5)), (i32(20), i32(20)), (i32(2, 2, 5), i32(2))):
+        with pytest.raises(AssertionError, match="per row"):
+            c.over(table, lens)
+    with pytest.raises(AssertionError, match="like"):
+        p.over(other)
+    assert p.over(c).ref_count is p.ref_count

@@ -79,20 +79,28 @@ class PagePool:
         held = cache.page_table[(cache.page_table >= 0) & (cache.page_table < cache.num_pool_pages)].long()
         self.ref_count = torch.bincount(held, minlength=cache.num_pool_pages).to(torch.int32)
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
-        self._ws = {}
+        self._ws, self._room = [], (0, 0)
 
     def over(self, cache):
         """The same pool for a cache of another batch (PagedKV.over): counts and status are shared."""
         assert cache.num_pool_pages == self.ref_count.numel(), "a cache over pools like this one's"
         p = object.__new__(PagePool)
-        p.cache, p.ref_count, p.status, p._ws = cache, self.ref_count, self.status, {}
+        p.cache, p.ref_count, p.status, p._ws = cache, self.ref_count, self.status, []
+        p._room = (0, 0)
         return p
 
     def _workspace(self, max_new, new_batch):
-        if (max_new, new_batch) not in self._ws:
-            self._ws[max_new, new_batch] = torch.empty(B.twilight_workspace_bytes(B.TW_WS_PAGES, self.cache.kv, max_new, new_batch),
-                                                       dtype=torch.uint8, device=self.cache.device)
-        return self._ws[max_new, new_batch]
+        """One for all calls: its size grows with both arguments.  Outgrown ones are kept, as captured graphs may name them; each is
+        at least twice the one before, so that all together are no more than twice the largest."""
+        most = tuple(max(x, B._count(y)) for x, y in zip(self._room, (max_new, new_batch)))
+        if not self._ws or most != self._room:
+            n = B.twilight_workspace_bytes(B.TW_WS_PAGES, self.cache.kv, *most)
+            if n == 0:                           # (a size that the call refuses, too)
+                return torch.empty(0, dtype=torch.uint8, device=self.cache.device)
+            if not self._ws or n > self._ws[-1].numel():
+                self._ws.append(torch.empty(max(n, 2 * self._ws[-1].numel() if self._ws else 0), dtype=torch.uint8, device=self.cache.device))
+            self._room = most
+        return self._ws[-1]
 
     def reserve(self, n_new, max_new):
         """Pages for the next n_new[b] positions of every sequence (seq_lens not yet advanced)."""

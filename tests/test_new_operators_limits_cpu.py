@@ -156,3 +156,28 @@ def test_another_batch_that_does_not_fit_is_refused():
     with pytest.raises(AssertionError, match="like"):
         p.over(other)
     assert p.over(c).ref_count is p.ref_count
+
+
+def test_a_pool_keeps_one_workspace_for_calls_of_all_sizes():
+    """Every prompt's length is another max_new, every number of beams another new_batch: what is kept does not grow with them."""
+    import paper_2502_02770_amd as T
+    from tests.test_new_operators_cpu import _kv
+    p = object.__new__(T.PagePool)
+    p.cache = object.__new__(T.PagedKV)
+    p.cache.kv, p.cache.device = _kv(T, batch=64, max_pages=2048, pool=100000), "cpu"
+    p._ws, p._room, rng, given, largest = [], (0, 0), np.random.default_rng(0), [], 0
+    for _ in range(2000):
+        most, n = (int(rng.integers(1, 32768)), 0) if rng.random() < 0.6 else (0, int(rng.integers(1, 400)))
+        ws = p._workspace(most, n)
+        need = T.twilight_workspace_bytes(T.TW_WS_PAGES, p.cache.kv, most, n)
+        assert ws.numel() >= need > 0
+        given.append((ws.data_ptr(), ws.numel()))
+        largest = max(largest, need)
+    kept = p._ws if isinstance(p._ws, list) else list(p._ws.values())
+    assert sum(w.numel() for w in kept) <= 4 * largest
+    assert set(given) <= {(w.data_ptr(), w.numel()) for w in kept}            # none that was handed out has gone
+    with pytest.raises(AssertionError, match="32 bits"):
+        p._workspace(2**32 + 4, 0)
+    assert p._workspace(0, 70000).numel() == 0                     # refused by the call; the next one is not short of room
+    assert p._workspace(0, 500).numel() >= T.twilight_workspace_bytes(T.TW_WS_PAGES, p.cache.kv, 0, 500)
+    assert p._workspace(32767, 399).numel() >= T.twilight_workspace_bytes(T.TW_WS_PAGES, p.cache.kv, 32767, 0)

@@ -735,7 +735,14 @@ int launch_new(NewArgs a, hipStream_t s) {
   return tw_prof_after(s);
 }
 
-size_t part_slots() { return (size_t)tw_num_cus() * 4 * PLAN_ROUNDS; }          // parts that a plan can make
+// Parts that a plan can make: fewer than 2 W rounds (see plan_chunk), and of one row block per sequence and KV head no more than its
+// list has chunks of the shortest length (8 lists of 4096 tokens: 256 parts of 128 rows, 17 MB; all that fit the chip: 136 MB).
+size_t part_slots(const TwDims& d, long long rows) {
+  const long long most = (long long)tw_num_cus() * 4 * PLAN_ROUNDS;
+  if (rows > 128) return (size_t)most;
+  const long long tiles = ((long long)d.max_pages + 3) / 4, chunks = (tiles + PLAN_MIN_TILES - 1) / PLAN_MIN_TILES;
+  return (size_t)std::min(most, chunks * d.batch * d.Hkv);
+}
 
 size_t align256n(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -743,8 +750,9 @@ size_t align256n(size_t x) { return (x + 255) & ~(size_t)255; }
 
 size_t tw_new_tokens_workspace(const TwDims& d, int max_new) {
   if (max_new <= 0 || max_new > TW_MAX_NEW) return 0;
-  const int M = rows_per_block((long long)max_new * d.G);
-  const size_t slots = part_slots();
+  const long long rows = (long long)max_new * d.G;
+  const int M = rows_per_block(rows);
+  const size_t slots = part_slots(d, rows);
   return align256n((size_t)d.batch * 8) + align256n(slots * M * 8) + slots * M * 512;
 }
 
@@ -762,7 +770,7 @@ static int new_tokens_impl(const twilight_kv_t* kv, const void* q, const int32_t
   a.q = (const uint4*)q; a.k_pool = (const char*)kv->k_pool; a.v_pool = (const char*)kv->v_pool;
   a.page_table = kv->page_table; a.seq_lens = kv->seq_lens; a.n_new = n_new; a.offsets = new_offsets; a.mask = mask;
   a.out = (uint2*)out; a.lse = lse;
-  const size_t slots = part_slots();
+  const size_t slots = part_slots(d, (long long)max_new * d.G);
   a.ws_plan = (int32_t*)ws;
   a.ws_ml = (float2*)((char*)ws + align256n((size_t)d.batch * 8));
   a.ws_acc = (float*)((char*)a.ws_ml + align256n(slots * M * 8));

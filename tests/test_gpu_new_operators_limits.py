@@ -158,3 +158,31 @@ def test_ordinary_scores_among_ones_far_away(n, new, size, sign):
             worst = ((out[i, h].double() - want).abs() - bound).max().item()
             assert worst <= 0, (i, h, worst)
             assert (lse[i, h].double() - l).abs() <= e + (m + 300) * 2.0**-24 + 2.0**-21 * (1 + l.abs()), (i, h)
+
+
+@pytest.mark.parametrize("hq,hkv", [(8, 8), (16, 2)])
+@pytest.mark.parametrize("lens,new", [([3000], 1), ([3000], 9), ([9000, 5, 700], 16), ([700, 640, 640, 650], 3), ([513], 4), ([64 * 64], 8)])
+def test_parts_stay_inside_their_workspace(lens, new, hq, hkv):
+    """Workspaces of the size that is asked for, among bytes that have to stay; results as with a larger one."""
+    import paper_2502_02770_amd as T
+    c = Cache(lens, hq, hkv, seed=1)
+    many = [min(n, new) for n in lens]
+    off, rows = [sum(many[:b]) for b in range(len(lens))], sum(many)
+    q = queries(rows, hq, 2)
+    size = T.twilight_workspace_bytes(T.TW_WS_NEW_TOKENS, c.kv, new)
+    got = []
+    for room in (size, 1 << 27):
+        ws = torch.full((65536 + room + 65536,), 171, dtype=torch.uint8, device="cuda")
+        for window in (2**31 - 1, 600):
+            out, lse = sent(q, hq)
+            T.twilight_window_attention(c.kv, q, i32(many), i32(off), new, window, 5, out, lse, ws[65536:65536 + room])
+            got.append((room, out, lse))
+        mask = i32(np.full((rows, 1), -1))
+        out, lse = sent(q, hq)
+        T.twilight_tree_attention(c.kv, q, i32(many), i32(off), new, mask, 1, out, lse, ws[65536:65536 + room])
+        got.append((room, out, lse))
+        assert (ws[:65536] == 171).all() and (ws[65536 + room:] == 171).all()
+    for a, b in zip(got[:3], got[3:]):
+        assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2])
+    with pytest.raises(T.TwilightError):
+        T.twilight_window_attention(c.kv, q, i32(many), i32(off), new, 600, 5, out, lse, ws[:size - 1])

@@ -181,3 +181,23 @@ def test_a_pool_keeps_one_workspace_for_calls_of_all_sizes():
     assert p._workspace(0, 70000).numel() == 0                     # refused by the call; the next one is not short of room
     assert p._workspace(0, 500).numel() >= T.twilight_workspace_bytes(T.TW_WS_PAGES, p.cache.kv, 0, 500)
     assert p._workspace(32767, 399).numel() >= T.twilight_workspace_bytes(T.TW_WS_PAGES, p.cache.kv, 32767, 0)
+
+
+@pytest.mark.parametrize("hq,hkv", [(8, 8), (32, 8), (64, 8)])
+@pytest.mark.parametrize("new", [1, 4, 16, 128])
+def test_workspace_of_new_tokens_follows_the_lists(hq, hkv, new):
+    """A list of ceil(pages / 4) tiles has at most half as many parts (528 bytes a row of 32, 64 or 128); and never more than all
+    the chip's.  What does not fit a row block is sized for the chip."""
+    import paper_2502_02770_amd as T
+    from tests.test_new_operators_cpu import _kv
+    rows = new * hq // hkv
+    block = 32 if rows <= 32 else 64 if rows <= 64 else 128
+    size = lambda batch, pages: T.twilight_workspace_bytes(T.TW_WS_NEW_TOKENS, _kv(T, batch, hq, hkv, pages, 1 << 20), new)
+    chip = size(512, 1 << 16)
+    for batch, pages in ((1, 1), (1, 256), (2, 300), (3, 9)):
+        parts = batch * hkv * -(-(-(-pages // 4)) // 2)
+        if rows <= 128:
+            assert parts * block * 520 <= size(batch, pages) <= parts * block * 520 + 8 * batch + 512, (batch, pages)
+        else:
+            assert size(batch, pages) == size(1, 1)
+        assert size(batch, pages) <= chip

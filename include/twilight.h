@@ -372,8 +372,9 @@ int twilight_sparse_decode_per_head(const twilight_kv_t* kv, const void* q, cons
  * seq_lens counts them: with n = seq_lens[b] and N = n_new[b], new token i of
  * sequence b stands at position n - N + i.
  *   out = sum_t softmax_t(q.K_t / sqrt(128)) V_t over the visible t
- * bf16 in and out; scores, softmax statistics and sums in fp32, the weights
- * rounded to bf16 for their product with V.  A token that sees nothing has a
+ * bf16 in and out; scores, softmax statistics and sums in fp32.  For their
+ * product with V the weights have 16 bits where max_new x heads of a group is
+ * at most 64, and 8 (bf16) beyond: off by at most 2^-16 and 2^-8 of each.  A token that sees nothing has a
  * row of zeros and lse -inf.  Tokens on unmapped pages are seen by nobody;
  * whatever lies behind a sequence's end in its last page is not used.
  *

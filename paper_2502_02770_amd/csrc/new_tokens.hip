@@ -12,8 +12,11 @@
 // the other 16), so maximum, sum and rescaling are in-lane but for one exchange between the halves, and the lane's own P
 // values are its B operand of the second product as they stand: the order of the 16 tokens within a contraction step is
 // free as long as the V^T operand has the same (slot 8 * h + j of step k = token 16 k + 8 (j / 4) + 4 h + j % 4).
-// P is rounded to bf16 for the product (each weight by at most 2^-8 of itself, independently; the output is bf16 anyway);
-// scores, maxima, sums, accumulators and the parts of cut lists are fp32, and the sum is of the unrounded weights.  A weight
+// Scores, maxima, sums, accumulators and the parts of cut lists are fp32, and the sum is of the unrounded weights.  For its product P
+// is bf16: of up to 64 rows, which the memory bounds, a weight and what its rounding left (16 bits, 2^-16 of a weight at most), so
+// that a single token is as exact as in twilight_sparse_decode; of 128 rows the weight alone (2^-8 of it at most), as
+// the second product and the remainders cost 24 to 35 % there: 8 drafts of 32 over 32768 tokens 205 -> 255 us, two prompts of 8192
+// 815 -> 1102, against 64 single tokens 137 -> 140, a draft of 8 over 4096 13.1 -> 13.3.  A weight
 // may reach 2^8 before m follows (kGrowth): rescaling the accumulators for every new maximum, which some row of 32 has in most
 // tiles, took 54 of 211 vector instructions per tile (prompts of 8192 tokens: 852 us, 811 us without).
 //
@@ -510,14 +513,17 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
       if (mn > was) m = __builtin_fabsf(mn) < kFar ? mn : mx * 0.25f;
       c = scale_of(m);
     }
-    tw_bf16x8 p[2 * MT];
+    constexpr bool REST = WT == 2;
+    tw_bf16x8 p[2 * MT], rest[2 * MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][r], c, -m));
         l += w;
-        p[2 * mt + r / 8][r % 8] = (__bf16)w;
+        const __bf16 near = (__bf16)w;
+        p[2 * mt + r / 8][r % 8] = near;
+        if constexpr (REST) rest[2 * mt + r / 8][r % 8] = (__bf16)(w - (float)near);
       }
 #pragma unroll
     for (int ks = 2; ks < 2 * MT; ++ks) read_v(ks);
@@ -525,6 +531,11 @@ __device__ __forceinline__ void attend_item(const NewArgs& a, const Item& it, un
     for (int ks = 0; ks < 2 * MT; ++ks)
 #pragma unroll
       for (int d = 0; d < 4; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ks][d].v, p[ks], o[d], 0, 0, 0);
+    if constexpr (REST)                          // (behind the others: next to them they would wait for their accumulators)
+#pragma unroll
+      for (int ks = 0; ks < 2 * MT; ++ks)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ks][d].v, rest[ks], o[d], 0, 0, 0);
   };
 
   if (u0 < u1) {

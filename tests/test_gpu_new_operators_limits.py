@@ -186,3 +186,52 @@ def test_parts_stay_inside_their_workspace(lens, new, hq, hkv):
         assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2])
     with pytest.raises(T.TwilightError):
         T.twilight_window_attention(c.kv, q, i32(many), i32(off), new, 600, 5, out, lse, ws[:size - 1])
+
+
+def exact_rows(c, b, q, see):
+    """One sequence in float64 -> (out, bound) where a weight is off by 2^-16 of itself at most (bf16 and the bf16 of what that
+    left: 2^-8 of 2^-8), apart from its score's fp32 steps (as in test_gpu_new_tokens.reference), and the output by half a step."""
+    k, v = c.logical[b]
+    n, G = c.lens[b], c.hq // c.hkv
+    kk, vv = (x.double().repeat_interleave(G, 1).transpose(0, 1) for x in (k, v))                 # [Hq, n, 128]
+    qq = q.double().transpose(0, 1)
+    x = torch.stack([qq[h] @ kk[h].T for h in range(c.hq)]) / math.sqrt(128)
+    mag = torch.stack([qq[h].abs() @ kk[h].abs().T for h in range(c.hq)]) / math.sqrt(128)
+    mag = torch.where(see, mag, torch.zeros_like(mag)).amax(-1, keepdim=True)
+    w = torch.softmax(torch.where(see, x, torch.full_like(x, -math.inf)), -1)
+    out, spread = (torch.stack([w[h] @ f(vv[h]) for h in range(c.hq)]) for f in (lambda v: v, torch.abs))
+    e = 130 * 2.0**-24 * mag + 8 * 2.0**-24 * (mag + 1)
+    return out.transpose(0, 1), (2.0**-8 * out.abs() + (2.0**-16 + 2 * e + (n + 300) * 2.0**-24) * spread).transpose(0, 1)
+
+
+@pytest.mark.parametrize("hq,hkv", [(8, 8), (8, 4), (32, 8), (16, 2)])
+@pytest.mark.parametrize("lens", [[2], [5, 40, 700], [3000], [600] * 40])
+@pytest.mark.parametrize("rows", [0, 32, 64])
+def test_few_rows_carry_their_weights_in_16_bits(lens, rows, hq, hkv):
+    """Single tokens and as many as make 32 and 64 rows: no rounding but that of fp32 and the output's own shows."""
+    import paper_2502_02770_amd as T
+    new = max(1, rows * hkv // hq)
+    c = Cache(lens, hq, hkv, seed=len(lens))
+    many = [min(n, new) for n in lens]
+    off, total = [sum(many[:b]) for b in range(len(lens))], sum(many)
+    q = queries(total, hq, 3, spread=0.7)
+    rng = np.random.default_rng(1)
+    bits = rng.random((total, -(-new // 32) * 32)) < 0.5
+    mask = torch.from_numpy(np.packbits(bits, axis=1, bitorder="little").view(np.int32).copy()).cuda()
+    for window, sinks in ((2**31 - 1, 0), (2, 1), (300, 3), (None, None)):
+        out, lse = sent(q, hq)
+        if window:
+            T.twilight_window_attention(c.kv, q, i32(many), i32(off), new, window, sinks, out, lse, workspace(c.kv, new))
+        else:
+            T.twilight_tree_attention(c.kv, q, i32(many), i32(off), new, mask, mask.shape[1], out, lse, workspace(c.kv, new))
+        for b, (n, m) in enumerate(zip(lens, many)):
+            p, t = torch.arange(n - m, n, device="cuda")[:, None], torch.arange(n, device="cuda")
+            see = (t <= p) & ((p - t < (window or 1)) | (t < (sinks or 0)))
+            if not window:
+                see = (t < n - m).repeat(m, 1)
+                see[:, n - m:] = torch.from_numpy(bits[off[b]:off[b] + m, :m]).cuda()
+            some = see.any(1)
+            want, bound = exact_rows(c, b, q[off[b]:off[b] + m][some], see[some])
+            got = out[off[b]:off[b] + m][some].double()
+            worst = ((got - want).abs() - bound).max().item() if some.any() else 0
+            assert worst <= 0, (window, b, worst)

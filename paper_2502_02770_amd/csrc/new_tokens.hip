@@ -51,7 +51,7 @@ enum { MODE_TREE = 0, MODE_WINDOW = 1 };
 constexpr int PLAN_ROUNDS = 2;                   // items per resident workgroup at most, as planned
 constexpr int PLAN_MIN_TILES = 2;                // shortest chunk of a list
 constexpr int STREAM_TILES = (96 << 20) / (2 * TILE_BYTES);   // tiles of K and V from which on they pass by the last-level cache
-constexpr long long COMBINE_FEW = 2048;          // rows of a launch up to which a workgroup joins one row's parts
+constexpr long long COMBINE_FEW = 512;           // rows of a launch up to which a workgroup joins one row's parts
 
 // rows of K and V that no token stands for (beyond the sequence's end, on an unmapped page) are read from here
 __device__ const uint4 tw_zero_row[16] = {};
@@ -656,7 +656,10 @@ __global__ __launch_bounds__(256, 2) void new_tokens_kernel(NewArgs a) {
 
 // The parts of cut lists joined.  A row (new token, head) is folded by LANES half waves of 32 lanes x 4 dims: two (a wave; four
 // rows to a workgroup) where there are many rows, eight (a workgroup) where few rows have many parts each and the wait
-// for one part after the other is what counts: 256 rows of 32 parts 4.0 us with eight, 8.3 us with two.
+// for one part after the other is what counts: 256 rows of 32 parts 4.0 us with eight, 8.3 us with two.  Whole calls, two / eight:
+//   one sequence of 4096     rows  32: 11.9 / 11.0  256: 14.0 / 13.4   512: 15.7 / 15.4  1024: 16.6 / 16.9  4096: 28.3 / 29.8
+//   4 sequences of 8192      rows 512: 30.8 / 31.0 1024: 32.5 / 33.2  2048: 36.6 / 37.2  8192: 60 / 64     16384: 93 / 100
+//   16 sequences of 4096     rows 512: 49.2 / 49.5 2048: 49.5 / 50.8  8192: 57.5 / 61   16384: 70 / 77
 template <int M, int LANES>
 __global__ __launch_bounds__(256) void new_tokens_combine_kernel(NewArgs a) {
   constexpr int ROWS = 8 / LANES;

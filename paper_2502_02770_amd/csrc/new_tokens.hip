@@ -708,6 +708,12 @@ __global__ __launch_bounds__(256) void new_tokens_combine_kernel(NewArgs a) {
 }
 
 // ---------------------------------------------------------------- host side
+// Rows to a workgroup: as many as there are, up to 128, since another row block reads the same K and V again.  Fewer rows leave the
+// waves a half of the tile's tokens each, instead of rows that nobody has.  us with 32 / 64 / 128 to a workgroup, 8 KV heads:
+//   one sequence of 4096     16 rows 12.3 / 12.3 / 12.7   64 rows  15.5 /  15.3 /  14.5   128 rows  19.4 /  17.9 /  16.9
+//   8 sequences of 4096       4 rows 30.5 / 29.8 / 31.6   64 rows  41.3 /  36.6 /  36.8   128 rows  67.2 /  48.5 /  43.6
+//   8 sequences of 32768     32 rows  172 /  170 /  169   64 rows   262 /   180 /   173   128 rows   464 /   298 /   204
+// (what 64 lose against 128 is the weights' second product, which 128 leave out.)
 int rows_per_block(long long rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
 // Lists that cannot be long are not cut, which saves the launch that joins the parts and their way through memory: up to 6 tiles,
@@ -719,7 +725,13 @@ int rows_per_block(long long rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 
 //   32       512       16: 47.2 / 43.6 24: 66.7 / 63.0 32: 85.2 / 81.9
 // and with ragged lengths up to that, for which more would be too many:
 //   32       160        8: 10.3 / 10.8 12: 11.0 / 12.5 16: 13.7 / 18.2     128 rows   12: 14.8 / 14.9  16: 16.9 / 22.4  26: 25.5 / 34.6
-// Nor are the row blocks of chunks and prompts under a window that fill the chip by themselves: their lists are alike.
+// Nor are the row blocks of chunks and prompts under a window that fill the chip by themselves.  max_new decides, as the host knows no
+// n_new: right for sequences that are alike, and for ragged prompts, whose longest blocks the dispatcher starts first and evens
+// out; but a chunk's neighbours with one token have a workgroup walk each of their lists.  us, whole / cut:
+//   prompts  2 of 8192, window 4096: 840 / 954    1 of 8192, no window: 557 / 640    8 of 50 to 4000: 394 / 516    16 of 512: 72.6 / 72.5
+//   chunks   3 of 1499 over 9001, window 2047, 8 heads a group: 330 / 352    4 of 512 over 4096: 140 / 150    8 of 512 over 512 to 32768: 650 / 625
+//   mixed    512 and 3 single tokens over 32768: 815 / 361    512 and 31 over 8192: 531 / 260    2048 and 15 over 16384, window 4096: 254 / 270
+//            8192 and 63 over 8192: 1377 / 1767 (of which 1300 the launch that joins, over rows that are not there)
 bool cut_lists(bool window, int blocks, long long lists, long long longest) {
   if (longest <= std::min(32ll, 6 + lists / 32)) return false;
   return !(window && blocks >= 8 && lists >= 2ll * tw_num_cus());

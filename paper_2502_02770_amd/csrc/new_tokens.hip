@@ -725,16 +725,21 @@ int rows_per_block(long long rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 
 //   32       512       16: 47.2 / 43.6 24: 66.7 / 63.0 32: 85.2 / 81.9
 // and with ragged lengths up to that, for which more would be too many:
 //   32       160        8: 10.3 / 10.8 12: 11.0 / 12.5 16: 13.7 / 18.2     128 rows   12: 14.8 / 14.9  16: 16.9 / 22.4  26: 25.5 / 34.6
-// Nor are the row blocks of chunks and prompts under a window that fill the chip by themselves.  max_new decides, as the host knows no
-// n_new: right for sequences that are alike, and for ragged prompts, whose longest blocks the dispatcher starts first and evens
-// out; but a chunk's neighbours with one token have a workgroup walk each of their lists.  us, whole / cut:
+// Nor are the row blocks of chunks and prompts under a window that fill the chip by themselves: right for sequences that are alike,
+// and for ragged prompts, whose longest blocks the dispatcher starts first and evens out.  The host knows no n_new, though, and
+// beside a chunk single tokens have a workgroup walk each of their lists; so where n_new is given and a list can be of more tiles
+// than 192 for every turn of the chip, they are cut.  us, whole / cut:
 //   prompts  2 of 8192, window 4096: 840 / 954    1 of 8192, no window: 557 / 640    8 of 50 to 4000: 394 / 516    16 of 512: 72.6 / 72.5
 //   chunks   3 of 1499 over 9001, window 2047, 8 heads a group: 330 / 352    4 of 512 over 4096: 140 / 150    8 of 512 over 512 to 32768: 650 / 625
-//   mixed    512 and 3 single tokens over 32768: 815 / 361    512 and 31 over 8192: 531 / 260    2048 and 15 over 16384, window 4096: 254 / 270
-//            8192 and 63 over 8192: 1377 / 1767 (of which 1300 the launch that joins, over rows that are not there)
-bool cut_lists(bool window, int blocks, long long lists, long long longest) {
+//            4 of 512 over 32768: 1043 / 1074    2 of 1024 over 100000: 3195 / 3380
+//   mixed    512 and 3 single tokens over 32768: 815 / 361    512 and 31 over 8192 (16 tiles a turn): 531 / 260
+//            2048 and 15 over 16384, window 4096 (5): 254 / 270    8192 and 63 over 8192 (0.5): 1377 / 1767, with 900 for the launch that joins
+constexpr long long LONG_TURN = 192;
+bool cut_lists(bool window, bool counted, int blocks, long long lists, long long longest) {
   if (longest <= std::min(32ll, 6 + lists / 32)) return false;
-  return !(window && blocks >= 8 && lists >= 2ll * tw_num_cus());
+  const long long places = 2ll * tw_num_cus();
+  if (!window || blocks < 8 || lists < places) return true;
+  return counted && longest * places > LONG_TURN * lists;
 }
 
 template <int MODE, int WR, int WT>
@@ -746,7 +751,7 @@ int launch_new(NewArgs a, hipStream_t s) {
     longest = std::min(longest, (((long long)a.sinks + TW_PAGE - 1) / TW_PAGE + ((long long)a.window + M / a.G + TW_PAGE - 2) / TW_PAGE + 1 + 3) / 4);
   a.stream = a.rb_max == 1 && lists * longest > STREAM_TILES;
   tw_prof_before(TW_K_NEW_TOKENS, s);
-  if (!cut_lists(MODE == MODE_WINDOW, a.rb_max, lists, longest)) {
+  if (!cut_lists(MODE == MODE_WINDOW, a.n_new != nullptr, a.rb_max, lists, longest)) {
     TW_LAUNCH((new_tokens_kernel<MODE, WR, WT, false>), dim3((unsigned)lists), dim3(64 * WR * WT), 0, s, a);
     return tw_prof_after(s);
   }

@@ -235,3 +235,10 @@ def test_few_rows_carry_their_weights_in_16_bits(lens, rows, hq, hkv):
             got = out[off[b]:off[b] + m][some].double()
             worst = ((got - want).abs() - bound).max().item() if some.any() else 0
             assert worst <= 0, (window, b, worst)
+
+
+@pytest.mark.parametrize("many", [[512, 1, 1, 1], [1, 0, 512, 30], [500, 512, 512, 512]])
+@pytest.mark.parametrize("window,sinks", [(2**31 - 1, 0), (12500, 9)])
+def test_a_chunk_beside_single_tokens_over_long_contexts(many, window, sinks):
+    """Row blocks enough for the chip by the largest count, few by the others, over lists of 200 tiles."""
+    run_window(Cache([13000, 12900, 13003, 700], 32, 8, seed=4), many, 512, window, sinks, seed=1)

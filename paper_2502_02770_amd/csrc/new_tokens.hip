@@ -26,10 +26,10 @@
 // tile ahead of it is computed.
 //
 // Bounds.  Few rows (32 or 64 to a workgroup, 2 or 4 waves that split a tile's tokens): HBM, 8 drafts of 32 over 32768 tokens
-// 1.08 GB in 208 us (5.2 TB/s; a large copy reads and writes 4.9).  128 rows (4 waves of 32 rows, all tokens each): a wave's tile
-// is 32 matrix instructions of 32 cycles, 16 of which keep the SIMD from issuing vector instructions, and 149 vector
-// instructions of 4 cycles (8 for the 32 exponentials): 1024 cycles of the matrix unit against 1236 of issue.  Two prompts
-// of 8192 tokens under a window of 4096: 826 us, 1.00 PFLOP/s of the pairs that are visible; an 8192^3 library product 1.21.
+// 1.08 GB in 209 us (5.2 TB/s; a large copy reads and writes 4.9).  128 rows (4 waves of 32 rows, all tokens each): a wave's tile
+// is 32 matrix instructions of 32 cycles, 16 of which keep the SIMD from issuing vector instructions, and 151 vector
+// instructions of 4 cycles (8 for the 32 exponentials): 1024 cycles of the matrix unit against 1244 of issue.  Two prompts
+// of 8192 tokens under a window of 4096: 828 us, 1.00 PFLOP/s of the pairs that are visible; an 8192^3 library product 1.21.
 #include <algorithm>
 #include "tw_common.h"
 

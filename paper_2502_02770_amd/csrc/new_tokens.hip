@@ -735,23 +735,24 @@ int rows_per_block(long long rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 
 //   mixed    512 and 3 single tokens over 32768: 815 / 361    512 and 31 over 8192 (16 tiles a turn): 531 / 260
 //            2048 and 15 over 16384, window 4096 (5): 254 / 270    8192 and 63 over 8192 (0.5): 1377 / 1767, with 900 for the launch that joins
 constexpr long long LONG_TURN = 192;
-bool cut_lists(bool window, bool counted, int blocks, long long lists, long long longest) {
+constexpr long long JOIN_ROWS = 1ll << 26;       // rows from which on the launch that joins, four to a workgroup, would have 2^32 threads
+bool cut_lists(bool window, bool counted, int blocks, long long lists, long long longest, long long rows) {
   if (longest <= std::min(32ll, 6 + lists / 32)) return false;
   const long long places = 2ll * tw_num_cus();
   if (!window || blocks < 8 || lists < places) return true;
-  return counted && longest * places > LONG_TURN * lists;
+  return counted && longest * places > LONG_TURN * lists && rows < JOIN_ROWS;
 }
 
 template <int MODE, int WR, int WT>
 int launch_new(NewArgs a, hipStream_t s) {
   constexpr int M = 32 * WR;
-  const long long lists = (long long)a.rb_max * a.batch * a.Hkv;
+  const long long lists = (long long)a.rb_max * a.batch * a.Hkv, rows = (long long)a.max_new * a.Hq;
   long long longest = ((long long)a.max_pages * TW_PAGE + TILE - 1) / TILE;      // tiles that a list can have
   if (MODE == MODE_WINDOW)
     longest = std::min(longest, (((long long)a.sinks + TW_PAGE - 1) / TW_PAGE + ((long long)a.window + M / a.G + TW_PAGE - 2) / TW_PAGE + 1 + 3) / 4);
   a.stream = a.rb_max == 1 && lists * longest > STREAM_TILES;
   tw_prof_before(TW_K_NEW_TOKENS, s);
-  if (!cut_lists(MODE == MODE_WINDOW, a.n_new != nullptr, a.rb_max, lists, longest)) {
+  if (!cut_lists(MODE == MODE_WINDOW, a.n_new != nullptr, a.rb_max, lists, longest, rows)) {
     TW_LAUNCH((new_tokens_kernel<MODE, WR, WT, false>), dim3((unsigned)lists), dim3(64 * WR * WT), 0, s, a);
     return tw_prof_after(s);
   }
@@ -760,7 +761,6 @@ int launch_new(NewArgs a, hipStream_t s) {
   TW_LAUNCH((new_tokens_kernel<MODE, WR, WT, true>), dim3((unsigned)std::min(most, 2ll * a.cus)), dim3(64 * WR * WT), 0, s, a);
   if (int e = tw_prof_after(s)) return e;
   tw_prof_before(TW_K_NEW_COMBINE, s);
-  const long long rows = (long long)a.max_new * a.Hq;
   if (rows * a.batch <= COMBINE_FEW) TW_LAUNCH((new_tokens_combine_kernel<M, 8>), dim3((unsigned)rows, (unsigned)a.batch), dim3(256), 0, s, a);
   else TW_LAUNCH((new_tokens_combine_kernel<M, 2>), dim3((unsigned)((rows + 3) / 4), (unsigned)a.batch), dim3(256), 0, s, a);
   return tw_prof_after(s);

@@ -242,3 +242,9 @@ def test_few_rows_carry_their_weights_in_16_bits(lens, rows, hq, hkv):
 def test_a_chunk_beside_single_tokens_over_long_contexts(many, window, sinks):
     """Row blocks enough for the chip by the largest count, few by the others, over lists of 200 tiles."""
     run_window(Cache([13000, 12900, 13003, 700], 32, 8, seed=4), many, 512, window, sinks, seed=1)
+
+
+@pytest.mark.parametrize("hq,hkv,max_new", [(64, 64, 1 << 20), (64, 64, (1 << 20) - 1), (64, 8, 1 << 20), (8, 8, 1 << 20)])
+def test_counts_far_below_their_bound(hq, hkv, max_new):
+    """The largest max_new over a table for lists of 2^22 tiles: up to 2^26 rows by the arguments, a few that are there."""
+    run_window(Cache([300], hq, hkv, seed=7, max_pages=1 << 24), [5], max_new, 2**31 - 1, 0, seed=2)

@@ -477,7 +477,8 @@ int twilight_window_attention(const twilight_kv_t* kv, const void* q, const int3
  * i < keep_count[b]; its bf16 rows, codes and (scale, zero), bit for bit.  The
  * bounds of the pages that hold dst_start[b] .. dst_start[b] + keep_count[b] - 1
  * are taken again from the rows up to that end, and with keep_count[b] = 0
- * those of the page that ends at dst_start[b] inside it.  After the
+ * those of the page that ends at dst_start[b] inside it.  With k_pool NULL the
+ * codes and (scale, zero) alone are moved (v_pool and page_minmax NULL too).  After the
  * verification of a draft: keep_idx the accepted tokens' positions, dst_start
  * the position of the first drafted one; the caller sets seq_lens to
  * dst_start + keep_count.  Entries outside [0, seq_lens[b]) or on unmapped
@@ -503,6 +504,93 @@ int twilight_pages_copy(const twilight_kv_t* kv, const int32_t* copy_src, const 
 int twilight_tokens_compact(const twilight_kv_t* kv, const int32_t* keep_idx, const int32_t* keep_count, int32_t keep_stride,
                             const int32_t* dst_start, const int32_t* dst_table, void* stream);
 
+/*
+ * A cache held in 4 bits: K and V as codes with an fp16 (scale, zero) per group
+ * of 32 dims, 160 bytes per token and KV head where bf16 takes 512.  K is in
+ * kq_pool and kq_meta; V in two more pools of the same layout (twilight_kv_t),
+ *   vq_pool        u8   [num_pool_pages][num_kv_heads][16][64]
+ *   vq_meta        fp16 [num_pool_pages][num_kv_heads][16][4][2]
+ * quant_bits must be 4 (or 0); k_pool and v_pool are not used.  All pools, rows
+ * and workspaces are 16-byte aligned (TW_EINVAL); max_pages_per_seq <= 2^24.
+ * Whole pages move by twilight_pages_copy and tokens by twilight_tokens_compact,
+ * each called once for K and once with kq_pool, kq_meta those of V (and k_pool,
+ * v_pool, page_minmax NULL).
+ *
+ * twilight_kv4_append: twilight_kquant_append for such a cache.  K and V are
+ * quantised by its formulas; page_minmax (of the rows as they came in) is kept
+ * up where it is not NULL.  seq_lens is neither read nor written.
+ *   k_new, v_new   bf16 [total_new][num_kv_heads][128], finite, |x| < 3e4
+ *   start_pos, n_new, new_offsets   i32 [batch]; n_new clamped to max_new
+ *   max_new        host: upper bound of n_new[] (sizes the launch), <= 2^27
+ *
+ * twilight_kv4_read: rows back as bf16, code * scale + zero rounded once more;
+ * of sequence b the positions start_pos[b] .. start_pos[b] + n_rows[b] - 1 to
+ * rows row_offsets[b] .. of k_out and v_out (the form that twilight_kquant_append
+ * takes: a sequence goes back to a bf16 cache).  Positions from seq_lens[b] on
+ * are passed over, those on unmapped pages give rows of zeros.
+ *   start_pos, n_rows, row_offsets   i32 [batch]; n_rows clamped to max_rows
+ *   k_out, v_out   bf16 [rows][num_kv_heads][128]
+ *
+ * twilight_kv4_attention: twilight_window_attention over such a cache, with the
+ * same arguments, masks and results, for single tokens, drafts, chunks and
+ * prompts: the tokens' K and V are code * scale + zero.  Scores are of that
+ * value itself (the codes meet q exactly), softmax statistics and sums in fp32;
+ * for their product weights and V are rounded to fp16 (11 bits: off by at most
+ * 2^-11 of each).  |q| < 2^100; the pools hold finite (scale, zero).
+ *   ws             >= twilight_workspace_bytes(TW_WS_KV4, kv, max_new, 0),
+ *                  for one call at a time
+ */
+int twilight_kv4_append(const twilight_kv_t* kv, void* vq_pool, void* vq_meta, const void* k_new, const void* v_new,
+                        const int32_t* start_pos, const int32_t* n_new, const int32_t* new_offsets, int32_t max_new, void* stream);
+int twilight_kv4_read(const twilight_kv_t* kv, const void* vq_pool, const void* vq_meta, const int32_t* start_pos, const int32_t* n_rows,
+                      const int32_t* row_offsets, int32_t max_rows, void* k_out, void* v_out, void* stream);
+int twilight_kv4_attention(const twilight_kv_t* kv, const void* vq_pool, const void* vq_meta, const void* q, const int32_t* n_new,
+                           const int32_t* new_offsets, int32_t max_new, int32_t window, int32_t num_sinks, void* out, float* lse,
+                           void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Tokens given up by the attention they got.
+ *
+ * twilight_attention_mass: what every cached token got of the newest tokens'
+ * attention, added to what it had.  For t < seq_lens[b], N = n_new[b]:
+ *   mass_out[b][t] = had + sum_{i, head} exp(q_i.K_t / sqrt(128) - lse_i),
+ *   had = decay * mass_in[b][t], or 0 for the new tokens themselves,
+ * over the new tokens i that see t (as in twilight_window_attention, whose
+ * arguments and lse these are; of a single token's or a prompt's last rows as
+ * well as of all).  K is bf16 where k_pool is given, else the 4-bit copy in
+ * kq_pool and kq_meta: what the attention that left lse has read.  Sums are
+ * fp32, in an order that does not depend on timing.  A row whose lse is not
+ * finite adds nothing, nor does one add to tokens on unmapped pages.
+ *   lse            fp32 [rows][num_q_heads], natural logarithms
+ *   decay          host, >= 0 and finite (1: plain sums)
+ *   mass_in, mass_out   fp32 [batch][max_pages_per_seq * 16], 16-byte aligned,
+ *                  the same or not overlapping; positions from seq_lens[b] on
+ *                  are left
+ *   max_pages_per_seq <= 2^22
+ *
+ * twilight_keep_tokens: the tokens to keep, for twilight_tokens_compact.  Of
+ * sequence b, k = min(budget[b], seq_lens[b], keep_stride) tokens (none below 0):
+ * the first s = min(num_sinks, k), the latest min(num_recent, k - s), and of
+ * those between the ones with the largest mass; equal ones from the lowest
+ * position up, and what is no number after all others.
+ *   mass           fp32 [batch][max_pages_per_seq * 16], 16-byte aligned
+ *   budget         i32 [batch]
+ *   num_sinks, num_recent   host, >= 0
+ *   keep_idx       i32 [batch][keep_stride]  out, k positions, ascending
+ *   keep_count     i32 [batch]               out, k
+ *   mass_out       fp32 [batch][keep_stride] out, their mass, or NULL; not
+ *                  overlapping mass.  With keep_stride = max_pages_per_seq * 16
+ *                  it is the mass of the compacted cache.
+ *                  Entries from k on are left in both.
+ *   ws             >= twilight_workspace_bytes(TW_WS_KEEP, kv, 0, 0), for one
+ *                  call at a time, 16-byte aligned
+ * Of kv only its shape and seq_lens are used.
+ */
+int twilight_attention_mass(const twilight_kv_t* kv, const void* q, const float* lse, const int32_t* n_new, const int32_t* new_offsets,
+                            int32_t max_new, int32_t window, int32_t num_sinks, float decay, const float* mass_in, float* mass_out, void* stream);
+int twilight_keep_tokens(const twilight_kv_t* kv, const float* mass, const int32_t* budget, int32_t num_sinks, int32_t num_recent,
+                         int32_t* keep_idx, int32_t* keep_count, int32_t keep_stride, float* mass_out, void* ws, size_t ws_bytes, void* stream);
+
 /* Workspace sizes (host-only query; no GPU needed). */
 #define TW_WS_SELECT 0
 #define TW_WS_PRUNE 1
@@ -513,9 +601,11 @@ int twilight_tokens_compact(const twilight_kv_t* kv, const int32_t* keep_idx, co
 #define TW_WS_SELECT_PRUNE 6
 #define TW_WS_NEW_TOKENS 7
 #define TW_WS_PAGES 8
+#define TW_WS_KV4 9
+#define TW_WS_KEEP 10
 /*  max_sel: as passed to the call (0 with sel_pages == NULL; max_cand for
- *  TW_WS_PRUNE_TOKENS; max_new for TW_WS_NEW_TOKENS and, 0 if nothing is to
- *  be reserved, for TW_WS_PAGES);
+ *  TW_WS_PRUNE_TOKENS; max_new for TW_WS_NEW_TOKENS, TW_WS_KV4 and, 0 if
+ *  nothing is to be reserved, for TW_WS_PAGES; 0 for TW_WS_KEEP);
  *  union_stride: as passed to sparse_decode (0 for dense), kept_stride for
  *  TW_WS_DECODE_PER_HEAD, new_batch (0 if nothing is to be forked) for
  *  TW_WS_PAGES. */

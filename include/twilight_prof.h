@@ -53,7 +53,13 @@ struct twilight_kv;   /* twilight.h */
 #define TW_K_PAGES_FORK 14
 #define TW_K_PAGES_COPY 15
 #define TW_K_COMPACT 16
-#define TW_K_COUNT 17
+#define TW_K_KV4_ATTENTION 17     /* attention over K and V in 4 bits */
+#define TW_K_KV4_COMBINE 18
+#define TW_K_KV4_APPEND 19
+#define TW_K_KV4_READ 20
+#define TW_K_MASS 21              /* accumulated attention weight */
+#define TW_K_KEEP 22              /* tokens to keep: every launch of twilight_keep_tokens */
+#define TW_K_COUNT 23
 int twilight_prof_enable(int mode);
 int twilight_prof_select(int kernel_id, int every);
 int twilight_prof_collect(int32_t* kernel_ids /*host*/, float* ms /*host*/, int32_t cap);

@@ -14,12 +14,13 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("TWILIGHT_LIB") or os.path.join(_PKG, "libtwilight.so")   # override: tuning builds
 
 TW_WS_SELECT, TW_WS_PRUNE, TW_WS_DECODE, TW_WS_DECODE_PER_HEAD, TW_WS_PRUNE_TOKENS, TW_WS_DS_SELECT, TW_WS_SELECT_PRUNE = 0, 1, 2, 3, 4, 5, 6
-TW_WS_NEW_TOKENS, TW_WS_PAGES = 7, 8
+TW_WS_NEW_TOKENS, TW_WS_PAGES, TW_WS_KV4, TW_WS_KEEP = 7, 8, 9, 10
 TW_STATUS_UNION_TRUNCATED, TW_STATUS_KEPT_TRUNCATED, TW_STATUS_POOL_EXHAUSTED, TW_STATUS_PAGE_COUNT = 1, 2, 4, 8
 TW_STATIC_SELECT_WS_BYTES = 8 << 20
 KERNEL_NAMES = ["kquant_append", "page_score", "page_select", "int4_score", "topp", "union",
                 "sparse_decode", "combine", "score_topp", "select_score_topp", "new_tokens", "new_combine",
-                "pages_free", "pages_take", "pages_fork", "pages_copy", "compact"]
+                "pages_free", "pages_take", "pages_fork", "pages_copy", "compact",
+                "kv4_attention", "kv4_combine", "kv4_append", "kv4_read", "attention_mass", "keep_tokens"]
 
 _vp, _i32, _i64, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
 
@@ -66,6 +67,11 @@ def lib():
     L.twilight_pages_fork.argtypes = [kvp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
     L.twilight_pages_copy.argtypes = [kvp, _vp, _vp, _i32, _vp]
     L.twilight_tokens_compact.argtypes = [kvp, _vp, _vp, _i32, _vp, _vp, _vp]
+    L.twilight_kv4_append.argtypes = [kvp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp]
+    L.twilight_kv4_read.argtypes = [kvp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp]
+    L.twilight_kv4_attention.argtypes = [kvp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _sz, _vp]
+    L.twilight_attention_mass.argtypes = [kvp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _f32, _vp, _vp, _vp]
+    L.twilight_keep_tokens.argtypes = [kvp, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _sz, _vp]
     L.twilight_workspace_bytes.argtypes = [ctypes.c_int, kvp, _i32, _i32]
     L.twilight_pinned_device_pointer.argtypes = [_vp, ctypes.POINTER(_vp)]
     L.twilight_pinned_device_pointer.restype = ctypes.c_int
@@ -86,6 +92,7 @@ def lib():
               "twilight_int4_score_tokens", "twilight_topp_prune_tokens",
               "twilight_tree_attention", "twilight_window_attention", "twilight_pages_reserve", "twilight_pages_free",
               "twilight_pages_fork", "twilight_pages_copy", "twilight_tokens_compact",
+              "twilight_kv4_append", "twilight_kv4_read", "twilight_kv4_attention", "twilight_attention_mass", "twilight_keep_tokens",
               "twilight_sparse_decode", "twilight_sparse_decode_per_head", "twilight_prof_enable", "twilight_prof_select", "twilight_prof_collect"):
         getattr(L, f).restype = ctypes.c_int
     _lib = L
@@ -120,6 +127,20 @@ def _sums(t):
         return None
     assert t.dtype is _F32 and t.is_cuda and t.is_contiguous(), _NEEDED
     return t.data_ptr()
+
+
+def _codes(t, last):
+    """A pool of codes or (scale, zero): [pages, heads, 16, last...]."""
+    assert t.is_cuda and t.is_contiguous() and (t.dtype is torch.uint8 if last == (64,) else t.dtype is torch.float16) and t.shape[2:] == (16, *last), \
+        "pools of codes u8 [pages, heads, 16, 64] and (scale, zero) f16 [pages, heads, 16, 4, 2] on the GPU required"
+    return t.data_ptr()
+
+
+def _v_pools(kv, vq_pool, vq_meta):
+    """V's pools of a cache in 4 bits, as many pages and heads as the cache has."""
+    a = _codes(vq_pool, (64,)), _codes(vq_meta, (4, 2))
+    assert vq_pool.shape[:2] == vq_meta.shape[:2] == (kv.num_pool_pages, kv.num_kv_heads), "V's pools as large as K's"
+    return a
 
 
 def _count(x):
@@ -293,6 +314,42 @@ def twilight_tokens_compact(kv, keep_idx, keep_count, keep_stride, dst_start, ds
     """dst_table None: in place."""
     _check(lib().twilight_tokens_compact(ctypes.byref(kv), _ints(keep_idx), _ints(keep_count), _count(keep_stride),
                                          _ints(dst_start), _ints(dst_table), _stream_of(keep_idx)))
+
+
+def twilight_kv4_append(kv, vq_pool, vq_meta, k_new, v_new, start_pos, n_new, new_offsets, max_new):
+    codes, meta = _v_pools(kv, vq_pool, vq_meta)
+    assert k_new.shape == v_new.shape, "a row of V per row of K"
+    _check(lib().twilight_kv4_append(ctypes.byref(kv), codes, meta, _rows(k_new), _rows(v_new), _ints(start_pos), _ints(n_new),
+                                     _ints(new_offsets), _count(max_new), _stream_of(k_new)))
+
+
+def twilight_kv4_read(kv, vq_pool, vq_meta, start_pos, n_rows, row_offsets, max_rows, k_out, v_out):
+    codes, meta = _v_pools(kv, vq_pool, vq_meta)
+    assert k_out.shape == v_out.shape, "a row of V per row of K"
+    _check(lib().twilight_kv4_read(ctypes.byref(kv), codes, meta, _ints(start_pos), _ints(n_rows), _ints(row_offsets), _count(max_rows),
+                                   _rows(k_out), _rows(v_out), _stream_of(k_out)))
+
+
+def twilight_kv4_attention(kv, vq_pool, vq_meta, q, n_new, new_offsets, max_new, window, num_sinks, out, lse, ws):
+    codes, meta = _v_pools(kv, vq_pool, vq_meta)
+    _check(lib().twilight_kv4_attention(ctypes.byref(kv), codes, meta, _rows(q), _ints(n_new), _ints(new_offsets), _count(max_new),
+                                        _limit(window), _limit(num_sinks), _rows(out), _sums(lse), _ptr(ws), ws.numel() * ws.element_size(),
+                                        _stream_of(q)))
+
+
+def twilight_attention_mass(kv, q, lse, n_new, new_offsets, max_new, window, num_sinks, decay, mass_in, mass_out):
+    assert mass_in.numel() == mass_out.numel() == kv.batch * kv.max_pages_per_seq * 16, "a weight per position of the page table"
+    _check(lib().twilight_attention_mass(ctypes.byref(kv), _rows(q), _sums(lse), _ints(n_new), _ints(new_offsets), _count(max_new),
+                                         _limit(window), _limit(num_sinks), float(decay), _sums(mass_in), _sums(mass_out), _stream_of(q)))
+
+
+def twilight_keep_tokens(kv, mass, budget, num_sinks, num_recent, keep_idx, keep_count, keep_stride, mass_out, ws):
+    assert mass.numel() == kv.batch * kv.max_pages_per_seq * 16, "a weight per position of the page table"
+    assert budget.numel() == keep_count.numel() == kv.batch and keep_idx.numel() >= kv.batch * keep_stride, "a row per sequence"
+    assert mass_out is None or mass_out.numel() >= kv.batch * keep_stride, "a row per sequence"
+    _check(lib().twilight_keep_tokens(ctypes.byref(kv), _sums(mass), _ints(budget), _limit(num_sinks), _limit(num_recent), _ints(keep_idx),
+                                      _ints(keep_count), _count(keep_stride), _sums(mass_out), _ptr(ws), ws.numel() * ws.element_size(),
+                                      _stream_of(mass)))
 
 
 def twilight_decode_plan(kv, which=TW_WS_DECODE, dense=False):

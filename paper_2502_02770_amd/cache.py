@@ -69,6 +69,55 @@ class PagedKV:
         B.twilight_tokens_compact(self.kv, keep_idx, keep_count, keep_idx.shape[1], dst_start, dst_table)
 
 
+class PagedKV4(PagedKV):
+    """A cache held in 4 bits, K and V (twilight_kv4_append and its kind): no bf16 pools; key bounds where with_bounds says so, for the
+    page selector, whose quantised K copy this is."""
+
+    def __init__(self, num_q_heads, num_kv_heads, page_table, seq_lens, num_pool_pages, device="cuda", with_bounds=False):
+        dev = self.device = torch.device(device)
+        self.Hq, self.Hkv, self.num_pool_pages, self.quant_bits = int(num_q_heads), int(num_kv_heads), int(num_pool_pages), 4
+        P, H = self.num_pool_pages, self.Hkv
+        self.k_pool = self.v_pool = None
+        self.kq_pool, self.vq_pool = (torch.zeros(P, H, 16, 64, dtype=torch.uint8, device=dev) for _ in range(2))
+        self.kq_meta, self.vq_meta = (torch.zeros(P, H, 16, 4, 2, dtype=torch.float16, device=dev) for _ in range(2))
+        self.page_minmax = torch.zeros(P, H, 2, 128, dtype=torch.bfloat16, device=dev) if with_bounds else None
+        self._set_batch(page_table, seq_lens)
+
+    def _set_batch(self, page_table, seq_lens):
+        assert page_table.dim() == 2 and seq_lens.numel() == page_table.shape[0], "a length per row of the table"
+        self.page_table = page_table.to(self.device, torch.int32).contiguous()
+        self.seq_lens = seq_lens.to(self.device, torch.int32).contiguous()
+        self.batch, self.max_pages = self.page_table.shape
+        shape = self.batch, self.Hq, self.Hkv, self.max_pages, self.num_pool_pages, self.page_table, self.seq_lens, None, None
+        self.kv = B.make_kv(*shape, self.kq_pool, self.kq_meta, self.page_minmax)
+        self._kv_of_v = B.make_kv(*shape, self.vq_pool, self.vq_meta)        # V's codes where those of K are, for what moves rows
+
+    def append(self, k_new, v_new, start_pos, n_new, new_offsets, max_new):
+        """twilight_kv4_append; does not advance seq_lens."""
+        B.twilight_kv4_append(self.kv, self.vq_pool, self.vq_meta, k_new, v_new, start_pos, n_new, new_offsets, max_new)
+
+    def read(self, start_pos, n_rows, row_offsets, max_rows, k_out, v_out):
+        """twilight_kv4_read: rows back as bf16."""
+        B.twilight_kv4_read(self.kv, self.vq_pool, self.vq_meta, start_pos, n_rows, row_offsets, max_rows, k_out, v_out)
+
+    def over(self, page_table, seq_lens):
+        """A cache of another batch over the same pools (rows of a fork, a larger or smaller batch)."""
+        c = object.__new__(PagedKV4)
+        c.__dict__.update(self.__dict__)
+        c._set_batch(page_table, seq_lens)
+        return c
+
+    def copy_pages(self, src, dst):
+        """twilight_pages_copy: whole pages src[i] -> dst[i] of this layer; negative entries are passed over."""
+        super().copy_pages(src, dst)
+        B.twilight_pages_copy(self._kv_of_v, src, dst, src.numel())
+
+    def compact(self, keep_idx, keep_count, dst_start, dst_table=None):
+        """twilight_tokens_compact; does not change seq_lens.  Not with key bounds, which the codes do not give back."""
+        super().compact(keep_idx, keep_count, dst_start, dst_table)
+        B.twilight_tokens_compact(self._kv_of_v, keep_idx, keep_count, keep_idx.shape[1], dst_start, dst_table)
+
+
 class PagePool:
     """Counts and status word of a pool of pages, shared by the layers whose caches have the same page table.  `cache` is any
     of those layers; the calls change its page_table, or make a new one (fork)."""
@@ -146,7 +195,8 @@ class NewTokens:
         rows = c.batch * self.max_new
         self.out = torch.zeros(rows, c.Hq, 128, dtype=torch.bfloat16, device=c.device)
         self.lse = torch.zeros(rows, c.Hq, dtype=torch.float32, device=c.device) if with_lse else None
-        self.ws = torch.empty(B.twilight_workspace_bytes(B.TW_WS_NEW_TOKENS, c.kv, self.max_new), dtype=torch.uint8, device=c.device)
+        self.ws = torch.empty(B.twilight_workspace_bytes(B.TW_WS_KV4 if isinstance(c, PagedKV4) else B.TW_WS_NEW_TOKENS, c.kv, self.max_new),
+                              dtype=torch.uint8, device=c.device)
 
     def _check(self, q, n_new):
         assert q.shape == self.out.shape, "q [batch * max_new, heads, 128]"
@@ -155,6 +205,7 @@ class NewTokens:
     def tree(self, q, tree_mask, n_new=None):
         """A drafted tree per sequence; tree_mask i32 [rows, words] (tree_mask_of_parents)."""
         self._check(q, n_new)
+        assert not isinstance(self.cache, PagedKV4), "trees are read from bf16 pools"
         assert tree_mask.dim() == 2 and tree_mask.shape[0] == q.shape[0], "a mask row per row of q"
         B.twilight_tree_attention(self.cache.kv, q, n_new, None, self.max_new, tree_mask, tree_mask.shape[1], self.out, self.lse, self.ws)
         return self.out
@@ -162,8 +213,46 @@ class NewTokens:
     def window(self, q, window, num_sinks=0, n_new=None):
         """Consecutive tokens under a sliding window with sinks."""
         self._check(q, n_new)
-        B.twilight_window_attention(self.cache.kv, q, n_new, None, self.max_new, window, num_sinks, self.out, self.lse, self.ws)
+        c = self.cache
+        if isinstance(c, PagedKV4):
+            B.twilight_kv4_attention(c.kv, c.vq_pool, c.vq_meta, q, n_new, None, self.max_new, window, num_sinks, self.out, self.lse, self.ws)
+        else:
+            B.twilight_window_attention(c.kv, q, n_new, None, self.max_new, window, num_sinks, self.out, self.lse, self.ws)
         return self.out
+
+
+class TokenMass:
+    """The attention that every token of a layer's cache (PagedKV or PagedKV4) has got, and what it is worth keeping by it."""
+
+    def __init__(self, cache):
+        c = self.cache = cache
+        self.mass, self._spare = (torch.zeros(c.batch, c.max_pages * 16, dtype=torch.float32, device=c.device) for _ in range(2))
+        self.keep_idx = torch.zeros(c.batch, c.max_pages * 16, dtype=torch.int32, device=c.device)
+        self.keep_count, self._start = (torch.zeros(c.batch, dtype=torch.int32, device=c.device) for _ in range(2))
+        self.ws = torch.empty(B.twilight_workspace_bytes(B.TW_WS_KEEP, c.kv), dtype=torch.uint8, device=c.device)
+
+    def add(self, q, lse, max_new, window=2**31 - 1, num_sinks=0, n_new=None, new_offsets=None, decay=1.0):
+        """What the newest tokens' attention gave (twilight_attention_mass); q, lse and the rest as of the attention call."""
+        assert n_new is None or n_new.numel() == self.cache.batch, "a count per sequence"
+        assert lse.numel() * 128 == q.numel() and (new_offsets is not None or q.shape[0] >= self.cache.batch * max_new), "a row per new token"
+        B.twilight_attention_mass(self.cache.kv, q, lse, n_new, new_offsets, max_new, window, num_sinks, decay, self.mass, self.mass)
+
+    def keep(self, budget, num_sinks=0, num_recent=0):
+        """-> (keep_idx [batch, max_pages * 16], keep_count): the tokens worth most (twilight_keep_tokens)."""
+        self._spare.zero_()                        # (tokens that come behind the kept ones begin with nothing)
+        B.twilight_keep_tokens(self.cache.kv, self.mass, budget, num_sinks, num_recent, self.keep_idx, self.keep_count, self.keep_idx.shape[1],
+                               self._spare, self.ws)
+        return self.keep_idx, self.keep_count
+
+    def evict(self, budget, num_sinks=0, num_recent=0):
+        """Every sequence cut down to its budget: the tokens worth keeping moved together in place, seq_lens set to their number, and
+        their mass kept for the steps to come.  The pages behind are the caller's to give back (PagePool.free), and no page may be
+        shared with another sequence.  -> keep_count"""
+        idx, count = self.keep(budget, num_sinks, num_recent)
+        self.cache.compact(idx, count, self._start)
+        self.cache.seq_lens.copy_(count)
+        self.mass.copy_(self._spare)               # (not exchanged: a captured graph names them)
+        return count
 
 
 def tree_mask_of_parents(parents):

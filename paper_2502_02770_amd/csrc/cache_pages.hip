@@ -364,7 +364,7 @@ __global__ __launch_bounds__(64 * WAVES) void compact_kernel(RowsArgs a) {
       m[j] = mv[4 * j + sub];
       const int r = m[j].src >= 0 ? m[j].src : a.bounds ? m[j].dst : -1;       // rows that stay count for the bounds
       k[j] = v[j] = make_uint4(0u, 0u, 0u, 0u);
-      if (r >= 0) k[j] = load(a.k + at(r, 16) + piece);
+      if (r >= 0 && a.k) k[j] = load(a.k + at(r, 16) + piece);
       if (m[j].src >= 0 && a.v) v[j] = load(a.v + at(m[j].src, 16) + piece);
     }
     const Move mc = mv[piece];
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(64 * WAVES) void compact_kernel(RowsArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (m[j].src >= 0) {
-        store(a.k + at(m[j].dst, 16) + piece, k[j]);
+        if (a.k) store(a.k + at(m[j].dst, 16) + piece, k[j]);
         if (a.v) store(a.v + at(m[j].dst, 16) + piece, v[j]);
       }
     if (mc.src >= 0) {
@@ -538,7 +538,8 @@ extern "C" int twilight_tokens_compact(const twilight_kv_t* kv, const int32_t* k
                                        const int32_t* dst_start, const int32_t* dst_table, void* stream) {
   TwDims d;
   if (int e = check_pages(kv, &d)) return e;
-  if (!keep_idx || !keep_count || keep_stride <= 0 || !dst_start || !kv->k_pool || !pools_aligned(kv)) return TW_EINVAL;
+  if (!keep_idx || !keep_count || keep_stride <= 0 || !dst_start || !pools_aligned(kv)) return TW_EINVAL;
+  if (!kv->k_pool && (!kv->kq_pool || kv->v_pool || kv->page_minmax)) return TW_EINVAL;      // codes alone: bounds would need K
   hipStream_t s = (hipStream_t)stream;
   RowsArgs a = rows_args(kv, d);
   a.table = kv->page_table; a.to = dst_table; a.seq_lens = kv->seq_lens;

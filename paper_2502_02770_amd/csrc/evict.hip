@@ -1,0 +1,458 @@
+// Tokens given up by the attention they got: the weights accumulated per cached token (twilight_attention_mass), and the choice of
+// the tokens to keep (twilight_keep_tokens).  twilight_tokens_compact then moves what is kept.
+#include <algorithm>
+#include "kv4_common.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kScaleLog2 = 0.08838834764831845f * 1.4426950408889634f;   // log2(e) / sqrt(128)
+
+// ------------------------------------------------------------------------------------------------------- accumulated weights
+// mass[t] = decay mass[t] + sum over new tokens i and query heads of exp(q.K_t / sqrt(128) - lse_i): K once, nothing else of the cache.
+//
+// A workgroup has PT pages of a sequence, its four waves the KV heads in turn; a wave holds its head's K of those pages as
+// matrix operands (for codes 128 + c in bf16, as in kv4_attention.hip) and goes through the head's rows (query heads x new tokens) by 16:
+// S = Q K^T, v_mfma_f32_16x16x32_bf16, a lane has one token and four rows.  The waves' sums are added in their order, so that
+// the result does not depend on timing.
+struct MassArgs {
+  const uint4* q;
+  const float* lse;
+  const uint4* k;                                // bf16 rows, or codes
+  const uint4* meta;
+  const int32_t* page_table;
+  const int32_t* seq_lens;
+  const int32_t* n_new;
+  const int32_t* offsets;
+  const float* mass_in;
+  float* mass_out;
+  int Hq, Hkv, G, lgG, max_pages, max_new, window, sinks;
+  unsigned pool_pages;
+  float decay;
+};
+
+template <bool CODES, int PT>
+__global__ __launch_bounds__(256) void attention_mass_kernel(MassArgs a) {
+  __shared__ float red[4][16 * PT];
+  const int b = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r16 = lane & 15, jq = lane >> 4;
+  const int len = max(0, min(a.seq_lens[b], a.max_pages * TW_PAGE)), n = a.n_new ? max(0, min(a.n_new[b], a.max_new)) : a.max_new;
+  const long long first = (long long)blockIdx.x * (16 * PT);
+  if (first >= len) return;
+  const int t0 = (int)first, ctx = len - n, off = a.offsets ? a.offsets[b] : b * a.max_new, rows = n * a.G;
+  int slot[PT];                                  // of the pages' first token, head 0; -1: nobody sees them
+  const int32_t* table = a.page_table + (long long)b * a.max_pages + t0 / TW_PAGE;
+#pragma unroll
+  for (int p = 0; p < PT; ++p) {
+    const int id = t0 + 16 * p < len ? table[p] : -1;
+    slot[p] = __builtin_amdgcn_readfirstlane((unsigned)id < a.pool_pages ? id * a.Hkv * TW_PAGE : -1);
+  }
+  float acc[PT];
+#pragma unroll
+  for (int p = 0; p < PT; ++p) acc[p] = 0.f;
+
+  for (int h = wave; h < a.Hkv; h += 4) {
+    tw_bf16x8 kf[PT][4];
+    uint4 km[PT];
+#pragma unroll
+    for (int p = 0; p < PT; ++p) {
+      const int row = max(slot[p], 0) + h * TW_PAGE + r16;
+      if (CODES) {
+        uint4 c = a.k[(long long)row * 4 + jq];
+        km[p] = a.meta[row];
+        tw_transpose_quarters(c);
+        kf[p][0] = tw_codes_bf16(c.x); kf[p][1] = tw_codes_bf16(c.y); kf[p][2] = tw_codes_bf16(c.z); kf[p][3] = tw_codes_bf16(c.w);
+      } else {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) kf[p][g] = tw_as_bf16(tw_ld_stream(a.k + (long long)row * 16 + 4 * g + jq));
+      }
+    }
+    for (int r0 = 0; r0 < rows; r0 += 16) {
+      // positions of the block's rows: does none of them see the pages?
+      const int p_lo = ctx + (r0 >> a.lgG), p_hi = ctx + ((min(r0 + 16, rows) - 1) >> a.lgG);
+      if (t0 > p_hi || (t0 + 16 * PT - 1 <= p_lo - a.window && t0 >= a.sinks)) continue;
+      const bool all = t0 + 16 * PT - 1 <= p_lo && (t0 > p_hi - a.window || t0 + 16 * PT <= a.sinks);
+      const int mine = min(r0 + r16, rows - 1);
+      const uint4* qp = a.q + ((long long)(off + (mine >> a.lgG)) * a.Hq + h * a.G + (mine & (a.G - 1))) * 16 + jq;
+      tw_bf16x8 qf[4];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const uint4 x = qp[4 * g];
+        qf[g] = CODES ? tw_q_like_codes(x) : tw_as_bf16(x);
+      }
+      float l2[4];                               // lse in powers of 2; infinite (weights of 0) where there is no row, or none with a weight
+      int pos[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = r0 + 4 * jq + i;
+        float l = __builtin_inff();
+        if (r < rows) l = a.lse[(long long)(off + (r >> a.lgG)) * a.Hq + h * a.G + (r & (a.G - 1))];
+        l2[i] = __builtin_fabsf(l) < __builtin_inff() ? l * kLog2e : __builtin_inff();
+        pos[i] = ctx + (r >> a.lgG);
+      }
+      tw_v4f less[4];                            // -128 Q_g of the lane's rows: a product with a constant
+      if (CODES) {
+        tw_bf16x8 c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = (__bf16)-128.f;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) less[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], c, tw_v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      }
+#pragma unroll
+      for (int p = 0; p < PT; ++p) {
+        tw_v4f s = {0.f, 0.f, 0.f, 0.f};
+        if (CODES) {
+          const uint32_t w[4] = {km[p].x, km[p].y, km[p].z, km[p].w};
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const tw_v4f t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], kf[p][g], less[g], 0, 0, 0);
+            const float z = tw_half_hi(w[g]) * (-1.f / 128.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] = __builtin_fmaf(tw_half_lo(w[g]), t[i], __builtin_fmaf(z, less[g][i], s[i]));
+          }
+        } else {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], kf[p][g], s, 0, 0, 0);
+        }
+        if (slot[p] < 0) continue;
+        const int t = t0 + 16 * p + r16;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // (the maximum makes 0 of what is no number: a row that sees such a token has an lse that says so)
+          float w = fmaxf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[i], kScaleLog2, -l2[i])), 0.f);
+          if (!all) w = t <= pos[i] && (t > pos[i] - a.window || t < a.sinks) ? w : 0.f;
+          acc[p] += w;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < PT; ++p) {
+    acc[p] = tw_quarters_sum(acc[p]);
+    if (jq == 0) red[wave][16 * p + r16] = acc[p];
+  }
+  __syncthreads();
+  const int t = t0 + (int)threadIdx.x;
+  if (threadIdx.x < 16 * PT && t < len) {
+    const long long at = (long long)b * a.max_pages * TW_PAGE + t;
+    const float had = t < ctx ? a.decay * a.mass_in[at] : 0.f;
+    a.mass_out[at] = had + ((red[0][threadIdx.x] + red[1][threadIdx.x]) + (red[2][threadIdx.x] + red[3][threadIdx.x]));
+  }
+}
+
+// -------------------------------------------------------------------------------------------------------------- what to keep
+// The budget's share of a sequence's tokens: its first ones, its latest ones, and of those between the heaviest.  A weight's bits in
+// the order of the numbers are a key; the key of the last token kept is found by three histograms (of 11, 11 and 10 bits), each of
+// the tokens that share the bits found before, and equal keys go to the lowest positions.
+struct KeepArgs {
+  const float* mass;
+  const int32_t* seq_lens;
+  const int32_t* budget;
+  int32_t* idx;
+  int32_t* count;
+  float* mass_out;                               // or nullptr
+  uint32_t* ws;                                  // [batch][chunks][CHUNK_WORDS]
+  int max_pages, sinks, recent, stride, chunks, blocks;   // blocks of SUB tokens to a chunk
+};
+constexpr int KEEP_THREADS = 1024, SUB = 8 * KEEP_THREADS;
+constexpr int CHUNK_WORDS = 2048 + 2048 + 1024 + 2;     // three histograms, tokens above the first two's digits
+
+struct KeepSeq {
+  int len, kept, first, last, want;              // tokens, of them kept; of those kept first and latest ones, and of those between
+};
+__device__ __forceinline__ KeepSeq keep_seq(const KeepArgs& a, int b) {
+  KeepSeq s;
+  s.len = max(0, min(a.seq_lens[b], a.max_pages * TW_PAGE));
+  s.kept = max(0, min(min(a.budget[b], s.len), a.stride));
+  s.first = min(a.sinks, s.kept);
+  s.last = min(a.recent, s.kept - s.first);
+  s.want = s.kept - s.first - s.last;
+  return s;
+}
+// larger weight, larger key; no number: 0, below all of them
+__device__ __forceinline__ uint32_t keep_key(float x) { return x == x ? tw_float_key(x + 0.0f) : 0u; }
+
+// The bin, from the highest down, in which the want-th token lies, and how many are in those above it.  hist: this thread's bins
+// (2 of 2048, the higher in .x, or 1 of 1024).
+struct Digit { uint32_t bin, above; };
+template <int PER>
+__device__ __forceinline__ Digit find_digit(uint32_t hi, uint32_t lo, uint32_t want, uint32_t* scratch) {
+  uint32_t total;
+  const uint32_t incl = tw_block_scan_u32(hi + lo, scratch, &total), before = incl - hi - lo;
+  uint32_t* found = scratch + 16;
+  if (before < want && want <= incl) {
+    const uint32_t top = PER * KEEP_THREADS - 1 - PER * threadIdx.x;
+    const bool second = PER == 2 && want > before + hi;
+    found[0] = second ? top - 1 : top;
+    found[1] = second ? before + hi : before;
+  }
+  __syncthreads();
+  const Digit d = {found[0], found[1]};
+  __syncthreads();
+  return d;
+}
+
+// 8 consecutive weights of a row (those behind its end are not read)
+__device__ __forceinline__ void load8(const float* row, int t, int len, float* x) {
+  if (t + 8 <= len) {
+    const float4 u = *(const float4*)(row + t), v = *(const float4*)(row + t + 4);
+    x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = t + i < len ? row[t + i] : 0.f;
+  }
+}
+
+// A thread's tokens t .. t + E - 1 written where they are kept.  above, ties: tokens kept for a larger key, and tokens of the last
+// key, before t; room: how many of the latter are kept.
+template <int E>
+__device__ __forceinline__ void emit(const KeepArgs& a, int b, const KeepSeq& s, int t, const uint32_t* key, const float* x, uint32_t last_key, bool any,
+                                     uint32_t above, uint32_t ties, uint32_t room) {
+  const long long out = (long long)b * a.stride;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int p = t + i;
+    if (p >= s.len) break;
+    int at = -1;
+    if (p < s.first) at = p;
+    else if (p >= s.len - s.last) at = s.kept - (s.len - p);
+    else if (any) {
+      const bool tie = key[i] == last_key;
+      if (key[i] > last_key || (tie && ties < room)) at = s.first + (int)(above + min(ties, room));
+      above += key[i] > last_key;
+      ties += tie;
+    }
+    if (at >= 0) {
+      a.idx[out + at] = p;
+      if (a.mass_out) a.mass_out[out + at] = x[i];
+    }
+  }
+}
+
+// A whole sequence per workgroup, E tokens per thread in registers.
+template <int E>
+__global__ __launch_bounds__(KEEP_THREADS) void keep_whole_kernel(KeepArgs a) {
+  __shared__ uint32_t hist[2048];
+  __shared__ uint32_t scratch[20];
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const KeepSeq s = keep_seq(a, b);
+  if (tid == 0) a.count[b] = s.kept;
+  if (s.kept == 0) return;
+  const float* row = a.mass + (long long)b * a.max_pages * TW_PAGE;
+  float x[E];
+  uint32_t key[E];
+  const int t = tid * E;
+#pragma unroll
+  for (int i = 0; i < E; i += 8) {
+    if (E >= 8) load8(row, t + i, s.len, x + i);
+    else
+#pragma unroll
+      for (int k = 0; k < E; ++k) x[k] = t + k < s.len ? row[t + k] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < E; ++i) key[i] = keep_key(x[i]);
+  const int lo = s.first, hi = s.len - s.last;
+  uint32_t prefix = 0, want = (uint32_t)s.want;
+  if (s.want > 0) {
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+      hist[tid] = 0; hist[tid + 1024] = 0;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (t + i >= lo && t + i < hi && (pass == 0 || key[i] >> (shift + bits) == prefix)) atomicAdd(&hist[(key[i] >> shift) & ((1u << bits) - 1u)], 1u);
+      __syncthreads();
+      const Digit d = pass < 2 ? find_digit<2>(hist[2047 - 2 * tid], hist[2046 - 2 * tid], want, scratch) : find_digit<1>(hist[1023 - tid], 0u, want, scratch);
+      prefix = prefix << bits | d.bin;
+      want -= d.above;
+    }
+  }
+  // kept for a larger key, and of the last key, before this thread's tokens
+  uint32_t mine = 0;
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+    if (t + i >= lo && t + i < hi) mine += (key[i] > prefix ? 1u : 0u) + (key[i] == prefix ? 0x10000u : 0u);
+  uint32_t total;
+  const uint32_t before = tw_block_scan_u32(mine, scratch, &total) - mine;
+  emit<E>(a, b, s, t, key, x, prefix, s.want > 0, before & 0xFFFFu, before >> 16, want);
+}
+
+// Long sequences: a workgroup per chunk of tokens, a launch per histogram and one that writes.  PASS 0 .. 2 make a chunk's histogram of
+// that digit; 1 .. 3 first find the digit before from all chunks' histograms.
+template <int PASS>
+__global__ __launch_bounds__(KEEP_THREADS) void keep_chunk_kernel(KeepArgs a) {
+  __shared__ uint32_t hist[2048];
+  __shared__ uint32_t scratch[20];
+  const int b = blockIdx.y, c = blockIdx.x, tid = threadIdx.x;
+  const KeepSeq s = keep_seq(a, b);
+  if (PASS == 3 && c == 0 && tid == 0) a.count[b] = s.kept;
+  const int span = a.blocks * SUB;
+  const long long t0 = (long long)c * span;
+  if (s.kept == 0 || t0 >= s.len) return;
+  const int chunks = (s.len + span - 1) / span;  // of this sequence
+  uint32_t* const all = a.ws + (long long)b * a.chunks * CHUNK_WORDS;
+  uint32_t* const own = all + (long long)c * CHUNK_WORDS;
+  const float* row = a.mass + (long long)b * a.max_pages * TW_PAGE;
+  const int lo = s.first, hi = s.len - s.last;
+  uint32_t prefix = 0, want = (uint32_t)s.want, above = 0, ties = 0;
+  if (s.want > 0) {
+#pragma unroll
+    for (int pass = 0; pass < PASS; ++pass) {
+      uint32_t h0 = 0, h1 = 0, p0 = 0;           // all chunks' tokens of this thread's bins, those of the chunks before this one
+      for (int k = 0; k < chunks; ++k) {
+        const uint32_t* h = all + (long long)k * CHUNK_WORDS + 2048 * pass;
+        if (pass < 2) {
+          const uint2 x = *(const uint2*)(h + 2046 - 2 * tid);
+          h0 += x.y; h1 += x.x;
+        } else {
+          const uint32_t x = h[1023 - tid];
+          h0 += x;
+          if (k < c) p0 += x;
+        }
+      }
+      const Digit d = pass < 2 ? find_digit<2>(h0, h1, want, scratch) : find_digit<1>(h0, 0u, want, scratch);
+      if (PASS < 3 && pass == PASS - 1) {        // this chunk's tokens above the digit, for those behind it
+        uint32_t x = 0;
+        const uint32_t y0 = own[2048 * pass + 2047 - 2 * tid], y1 = own[2048 * pass + 2046 - 2 * tid];
+        if (2047u - 2 * tid > d.bin) x += y0;
+        if (2046u - 2 * tid > d.bin) x += y1;
+        uint32_t total;
+        tw_block_scan_u32(x, scratch, &total);
+        if (tid == 0) own[5120 + pass] = total;
+      }
+      if (pass == 2) {
+        uint32_t x = 1023u - tid > d.bin ? p0 : 0u, total;
+        for (int k = tid; k < c; k += KEEP_THREADS) x += all[(long long)k * CHUNK_WORDS + 5120] + all[(long long)k * CHUNK_WORDS + 5121];
+        tw_block_scan_u32(x, scratch, &total);
+        above = total;
+        if (1023u - tid == d.bin) scratch[18] = p0;
+        __syncthreads();
+        ties = scratch[18];
+        __syncthreads();
+      }
+      prefix = prefix << (pass == 2 ? 10 : 11) | d.bin;
+      want -= d.above;
+    }
+  }
+  if (PASS < 3) {
+    if (s.want == 0) return;
+    constexpr int shift = PASS == 0 ? 21 : PASS == 1 ? 10 : 0, bits = PASS == 2 ? 10 : 11;
+    hist[tid] = 0; hist[tid + 1024] = 0;
+    __syncthreads();
+    for (int k = 0; k < a.blocks; ++k) {
+      const long long t = t0 + (long long)k * SUB + 8 * tid;
+      if (t >= hi) break;
+      float x[8];
+      load8(row, (int)t, s.len, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t key = keep_key(x[i]);
+        if (t + i >= lo && t + i < hi && (PASS == 0 || key >> (shift + bits) == prefix)) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1u)], 1u);
+      }
+    }
+    __syncthreads();
+    own[2048 * PASS + tid] = hist[tid];
+    if (PASS < 2) own[2048 * PASS + 1024 + tid] = hist[tid + 1024];
+    return;
+  }
+  for (int k = 0; k < a.blocks; ++k) {
+    const long long at = t0 + (long long)k * SUB;
+    if (at >= s.len) break;
+    const int t = (int)at + 8 * tid;
+    float x[8];
+    uint32_t key[8], mine = 0, total;
+    load8(row, t, s.len, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      key[i] = keep_key(x[i]);
+      if (t + i >= lo && t + i < hi) mine += (key[i] > prefix ? 1u : 0u) + (key[i] == prefix ? 0x10000u : 0u);
+    }
+    const uint32_t before = tw_block_scan_u32(mine, scratch, &total) - mine;
+    emit<8>(a, b, s, t, key, x, prefix, s.want > 0, above + (before & 0xFFFFu), ties + (before >> 16), want);
+    above += total & 0xFFFFu;
+    ties += total >> 16;
+  }
+}
+
+constexpr int WHOLE_TOKENS = 32 * KEEP_THREADS, MOST_CHUNKS = 128;
+
+// Chunks of a long row, and blocks of SUB tokens in each.
+void keep_chunks(const TwDims& d, int* chunks, int* blocks) {
+  const long long subs = ((long long)d.max_pages * TW_PAGE + SUB - 1) / SUB;
+  *blocks = (int)((subs + MOST_CHUNKS - 1) / MOST_CHUNKS);
+  *chunks = (int)((subs + *blocks - 1) / *blocks);
+}
+
+template <bool CODES>
+int launch_mass(const MassArgs& a, int batch, hipStream_t s) {
+  tw_prof_before(TW_K_MASS, s);
+  const long long pages = (long long)a.max_pages * batch;
+  if (pages <= 2ll * tw_num_cus()) TW_LAUNCH((attention_mass_kernel<CODES, 1>), dim3((unsigned)a.max_pages, (unsigned)batch), dim3(256), 0, s, a);
+  else TW_LAUNCH((attention_mass_kernel<CODES, 4>), dim3((unsigned)((a.max_pages + 3) / 4), (unsigned)batch), dim3(256), 0, s, a);
+  return tw_prof_after(s);
+}
+
+}  // namespace
+
+size_t tw_keep_workspace(const TwDims& d) {
+  if ((long long)d.max_pages * TW_PAGE <= WHOLE_TOKENS) return 256;
+  int chunks, blocks;
+  keep_chunks(d, &chunks, &blocks);
+  return ((size_t)d.batch * chunks * CHUNK_WORDS * 4 + 255) & ~(size_t)255;
+}
+
+extern "C" int twilight_attention_mass(const twilight_kv_t* kv, const void* q, const float* lse, const int32_t* n_new, const int32_t* new_offsets,
+                                       int32_t max_new, int32_t window, int32_t num_sinks, float decay, const float* mass_in, float* mass_out,
+                                       void* stream) {
+  TwDims d;
+  if (int e = tw_check_kv(kv, &d)) return e;
+  const bool codes = kv->k_pool == nullptr;
+  if (!q || !lse || !mass_in || !mass_out) return TW_EINVAL;
+  if (codes && (!kv->kq_pool || !kv->kq_meta || d.bits != 4)) return TW_EINVAL;
+  if (window < 1 || num_sinks < 0 || max_new <= 0 || max_new > TW_MAX_NEW || d.max_pages > TW_MAX_ROW_PAGES / 4) return TW_EINVAL;
+  if ((long long)max_new * d.batch >= (1ll << 31) || !(decay >= 0.f) || decay > 3.4e38f) return TW_EINVAL;
+  const void* k = codes ? kv->kq_pool : kv->k_pool;
+  if (((uintptr_t)q | (uintptr_t)k | (codes ? (uintptr_t)kv->kq_meta : 0)) & 15) return TW_EINVAL;
+  const int32_t most = 1 << 30;                  // longer than any sequence
+  MassArgs a;
+  a.q = (const uint4*)q; a.lse = lse; a.k = (const uint4*)k; a.meta = (const uint4*)kv->kq_meta; a.page_table = kv->page_table;
+  a.seq_lens = kv->seq_lens; a.n_new = n_new; a.offsets = new_offsets; a.mass_in = mass_in; a.mass_out = mass_out;
+  a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.G; a.lgG = __builtin_ctz(d.G); a.max_pages = d.max_pages; a.max_new = max_new;
+  a.window = std::min(window, most); a.sinks = std::min(num_sinks, most); a.pool_pages = (unsigned)d.pool_pages; a.decay = decay;
+  return codes ? launch_mass<true>(a, d.batch, (hipStream_t)stream) : launch_mass<false>(a, d.batch, (hipStream_t)stream);
+}
+
+extern "C" int twilight_keep_tokens(const twilight_kv_t* kv, const float* mass, const int32_t* budget, int32_t num_sinks, int32_t num_recent,
+                                    int32_t* keep_idx, int32_t* keep_count, int32_t keep_stride, float* mass_out, void* ws, size_t ws_bytes, void* stream) {
+  TwDims d;
+  if (int e = tw_check_kv(kv, &d)) return e;
+  if (!mass || !budget || !keep_idx || !keep_count || keep_stride <= 0 || num_sinks < 0 || num_recent < 0 || d.max_pages > TW_MAX_ROW_PAGES) return TW_EINVAL;
+  if (((uintptr_t)mass | (uintptr_t)ws) & 15) return TW_EINVAL;
+  if (!ws || ws_bytes < tw_keep_workspace(d)) return TW_EWORKSPACE;
+  KeepArgs a = {};
+  a.mass = mass; a.seq_lens = kv->seq_lens; a.budget = budget; a.idx = keep_idx; a.count = keep_count; a.mass_out = mass_out; a.ws = (uint32_t*)ws;
+  a.max_pages = d.max_pages; a.sinks = num_sinks; a.recent = num_recent; a.stride = keep_stride;
+  hipStream_t s = (hipStream_t)stream;
+  const long long tokens = (long long)d.max_pages * TW_PAGE;
+  if (tokens <= WHOLE_TOKENS) {
+    tw_prof_before(TW_K_KEEP, s);
+    const dim3 grid((unsigned)d.batch), block(KEEP_THREADS);
+    if (tokens <= 2 * KEEP_THREADS) TW_LAUNCH(keep_whole_kernel<2>, grid, block, 0, s, a);
+    else if (tokens <= 8 * KEEP_THREADS) TW_LAUNCH(keep_whole_kernel<8>, grid, block, 0, s, a);
+    else TW_LAUNCH(keep_whole_kernel<32>, grid, block, 0, s, a);
+    return tw_prof_after(s);
+  }
+  keep_chunks(d, &a.chunks, &a.blocks);
+  const dim3 grid((unsigned)a.chunks, (unsigned)d.batch), block(KEEP_THREADS);
+  for (int pass = 0; pass < 4; ++pass) {
+    tw_prof_before(TW_K_KEEP, s);
+    switch (pass) {
+      case 0: TW_LAUNCH(keep_chunk_kernel<0>, grid, block, 0, s, a); break;
+      case 1: TW_LAUNCH(keep_chunk_kernel<1>, grid, block, 0, s, a); break;
+      case 2: TW_LAUNCH(keep_chunk_kernel<2>, grid, block, 0, s, a); break;
+      default: TW_LAUNCH(keep_chunk_kernel<3>, grid, block, 0, s, a); break;
+    }
+    if (int e = tw_prof_after(s)) return e;
+  }
+  return TW_OK;
+}

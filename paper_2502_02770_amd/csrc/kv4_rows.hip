@@ -1,0 +1,169 @@
+// Rows of a cache that holds K and V in 4 bits: written (twilight_kv4_append) and read back as bf16 (twilight_kv4_read).
+//
+// A row of 128 dims has a code of 4 bits per dim and an fp16 (scale, zero) per group of 32: 160 bytes for K and V where bf16 has 512.
+// One workgroup = one (sequence, KV head, logical page): 16 token slots x 16 lanes, a lane has 8 consecutive dims of K and of V (one
+// 16-byte piece, one word of codes each), a quad of lanes a group.
+#include "tw_common.h"
+#include "kquant_common.h"
+
+namespace {
+
+struct RowArgs4 {
+  const uint4* k_new;                            // append: rows in; read: rows out
+  const uint4* v_new;
+  uint4* k_out;
+  uint4* v_out;
+  const int32_t* start;
+  const int32_t* n_rows;
+  const int32_t* offsets;
+  const int32_t* page_table;
+  const int32_t* seq_lens;
+  uint32_t* k_codes;
+  uint32_t* k_meta;
+  uint32_t* v_codes;
+  uint32_t* v_meta;
+  uint4* bounds;                                 // or nullptr
+  int Hkv, max_pages, most;                      // most: bound of n_rows
+  unsigned pool_pages;
+};
+
+// The workgroup's page of the rows start .. start + n - 1 of its sequence, and this thread's position in it; false: none.
+__device__ __forceinline__ bool page_of(const RowArgs4& a, int b, long long start, long long end, long long* page, long long* tok) {
+  if (start < 0 || end <= start) return false;
+  const long long lp = start / TW_PAGE + blockIdx.x;
+  if (lp * TW_PAGE >= end || lp >= a.max_pages) return false;
+  *page = a.page_table[(long long)b * a.max_pages + lp];
+  *tok = lp * TW_PAGE + (threadIdx.x >> 4);
+  return true;
+}
+
+__global__ __launch_bounds__(256) void kv4_append_kernel(RowArgs4 a) {
+  const int b = blockIdx.z, h = blockIdx.y, ts = threadIdx.x >> 4, seg = threadIdx.x & 15;
+  const long long start = a.start[b], end = start + min(a.n_rows[b], a.most);
+  long long page, tok;
+  if (!page_of(a, b, start, end, &page, &tok) || page < 0 || page >= a.pool_pages) return;
+  const bool is_new = tok >= start && tok < end;
+  const long long slot = (page * a.Hkv + h) * TW_PAGE + ts;
+  uint4 rk = make_uint4(0u, 0u, 0u, 0u), rv = rk;
+  if (is_new) {
+    const long long row = ((long long)a.offsets[b] + (tok - start)) * a.Hkv + h;
+    rk = tw_ld_stream(a.k_new + row * 16 + seg);
+    rv = tw_ld_stream(a.v_new + row * 16 + seg);
+  }
+  float x[8], y[8];
+  tw_unpack8(rk, x);
+  tw_unpack8(rv, y);
+  uint32_t wk, wv, none, mk, mv;
+  tw_quantize_lane8<4>(x, seg, &wk, &none, &mk);
+  tw_quantize_lane8<4>(y, seg, &wv, &none, &mv);
+  if (is_new) {
+    a.k_codes[slot * 16 + seg] = wk;
+    a.v_codes[slot * 16 + seg] = wv;
+    if ((seg & 3) == 0) { a.k_meta[slot * 4 + (seg >> 2)] = mk; a.v_meta[slot * 4 + (seg >> 2)] = mv; }
+  }
+  if (!a.bounds) return;
+
+  // element-wise bounds of K over the page's tokens, of which those before `start` have theirs there
+  __shared__ float red[4][2][16][8];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float lo = is_new ? x[i] : __builtin_inff(), hi = is_new ? x[i] : -__builtin_inff();
+    lo = fminf(lo, __shfl_xor(lo, 16, 64)); hi = fmaxf(hi, __shfl_xor(hi, 16, 64));
+    lo = fminf(lo, __shfl_xor(lo, 32, 64)); hi = fmaxf(hi, __shfl_xor(hi, 32, 64));
+    if (lane < 16) { red[wave][0][seg][i] = lo; red[wave][1][seg][i] = hi; }
+  }
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  const int which = threadIdx.x >> 4;            // 0: lower bounds, 1: upper ones
+  uint4* at = a.bounds + (page * a.Hkv + h) * 32 + which * 16 + seg;
+  float old[8];
+  const bool begun = (tok - ts) < start;
+  tw_unpack8(begun ? *at : make_uint4(0u, 0u, 0u, 0u), old);
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float v = red[0][which][seg][i];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) v = which ? fmaxf(v, red[k][which][seg][i]) : fminf(v, red[k][which][seg][i]);
+    if (begun) v = which ? fmaxf(v, old[i]) : fminf(v, old[i]);
+    w[i] = __float_as_uint(v);                   // of bf16 values: the upper 16 bits are all of it
+  }
+  *at = make_uint4(w[0] >> 16 | (w[1] & 0xFFFF0000u), w[2] >> 16 | (w[3] & 0xFFFF0000u), w[4] >> 16 | (w[5] & 0xFFFF0000u), w[6] >> 16 | (w[7] & 0xFFFF0000u));
+}
+
+// 8 codes times scale plus zero, rounded to bf16 (code * scale is exact in fp32, so there is one rounding before that).
+__device__ __forceinline__ uint4 values_of(uint32_t w, uint32_t meta) {
+  const float s = __half2float(__ushort_as_half((unsigned short)meta)), z = __half2float(__ushort_as_half((unsigned short)(meta >> 16)));
+  union { __bf16 e[8]; uint4 v; } x;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x.e[i] = (__bf16)__builtin_fmaf((float)((w >> (8 * (i & 3) + 4 * (i >> 2))) & 15u), s, z);
+  return x.v;
+}
+
+__global__ __launch_bounds__(256) void kv4_read_kernel(RowArgs4 a) {
+  const int b = blockIdx.z, h = blockIdx.y, ts = threadIdx.x >> 4, seg = threadIdx.x & 15;
+  const long long start = a.start[b], end = min(start + min(a.n_rows[b], a.most), (long long)min(a.seq_lens[b], a.max_pages * TW_PAGE));
+  long long page, tok;
+  if (!page_of(a, b, start, end, &page, &tok) || tok < start || tok >= end) return;
+  const long long row = (((long long)a.offsets[b] + (tok - start)) * a.Hkv + h) * 16 + seg;
+  uint4 k = make_uint4(0u, 0u, 0u, 0u), v = k;
+  if (page >= 0 && page < a.pool_pages) {
+    const long long slot = (page * a.Hkv + h) * TW_PAGE + ts;
+    k = values_of(a.k_codes[slot * 16 + seg], a.k_meta[slot * 4 + (seg >> 2)]);
+    v = values_of(a.v_codes[slot * 16 + seg], a.v_meta[slot * 4 + (seg >> 2)]);
+  }
+  tw_st_stream(a.k_out + row, k);
+  tw_st_stream(a.v_out + row, v);
+}
+
+constexpr int MOST_ROWS = 1 << 27;                // rows of a sequence: a launch has fewer than 2^32 threads along its pages
+
+int rows_args4(const twilight_kv_t* kv, const void* vq_pool, const void* vq_meta, const int32_t* start, const int32_t* n, const int32_t* offsets,
+               int32_t most, TwDims* d, RowArgs4* a) {
+  if (int e = tw_check_kv(kv, d)) return e;
+  if (!kv->kq_pool || !kv->kq_meta || !vq_pool || !vq_meta || !start || !n || !offsets || most < 0 || most > MOST_ROWS || d->bits != 4) return TW_EINVAL;
+  if (d->max_pages > TW_MAX_ROW_PAGES) return TW_EINVAL;
+  if (((uintptr_t)kv->kq_pool | (uintptr_t)kv->kq_meta | (uintptr_t)vq_pool | (uintptr_t)vq_meta | (uintptr_t)kv->page_minmax) & 15) return TW_EINVAL;
+  *a = RowArgs4{};
+  a->start = start; a->n_rows = n; a->offsets = offsets; a->page_table = kv->page_table; a->seq_lens = kv->seq_lens;
+  a->k_codes = (uint32_t*)kv->kq_pool; a->k_meta = (uint32_t*)kv->kq_meta; a->v_codes = (uint32_t*)vq_pool; a->v_meta = (uint32_t*)vq_meta;
+  a->Hkv = d->Hkv; a->max_pages = d->max_pages; a->most = most; a->pool_pages = (unsigned)d->pool_pages;
+  return TW_OK;
+}
+
+// pages that `most` rows starting anywhere inside a page touch
+unsigned pages_touched(const TwDims& d, int most) {
+  const long long n = ((long long)most + TW_PAGE - 1) / TW_PAGE + 1;
+  return (unsigned)(n < d.max_pages ? n : d.max_pages);
+}
+
+}  // namespace
+
+extern "C" int twilight_kv4_append(const twilight_kv_t* kv, void* vq_pool, void* vq_meta, const void* k_new, const void* v_new,
+                                   const int32_t* start_pos, const int32_t* n_new, const int32_t* new_offsets, int32_t max_new, void* stream) {
+  TwDims d;
+  RowArgs4 a;
+  if (int e = rows_args4(kv, vq_pool, vq_meta, start_pos, n_new, new_offsets, max_new, &d, &a)) return e;
+  if (!k_new || !v_new || (((uintptr_t)k_new | (uintptr_t)v_new) & 15)) return TW_EINVAL;
+  if (max_new == 0) return TW_OK;
+  a.k_new = (const uint4*)k_new; a.v_new = (const uint4*)v_new; a.bounds = (uint4*)kv->page_minmax;
+  hipStream_t s = (hipStream_t)stream;
+  tw_prof_before(TW_K_KV4_APPEND, s);
+  TW_LAUNCH(kv4_append_kernel, dim3(pages_touched(d, max_new), (unsigned)d.Hkv, (unsigned)d.batch), dim3(256), 0, s, a);
+  return tw_prof_after(s);
+}
+
+extern "C" int twilight_kv4_read(const twilight_kv_t* kv, const void* vq_pool, const void* vq_meta, const int32_t* start_pos, const int32_t* n_rows,
+                                 const int32_t* row_offsets, int32_t max_rows, void* k_out, void* v_out, void* stream) {
+  TwDims d;
+  RowArgs4 a;
+  if (int e = rows_args4(kv, vq_pool, vq_meta, start_pos, n_rows, row_offsets, max_rows, &d, &a)) return e;
+  if (!k_out || !v_out || (((uintptr_t)k_out | (uintptr_t)v_out) & 15)) return TW_EINVAL;
+  if (max_rows == 0) return TW_OK;
+  a.k_out = (uint4*)k_out; a.v_out = (uint4*)v_out;
+  hipStream_t s = (hipStream_t)stream;
+  tw_prof_before(TW_K_KV4_READ, s);
+  TW_LAUNCH(kv4_read_kernel, dim3(pages_touched(d, max_rows), (unsigned)d.Hkv, (unsigned)d.batch), dim3(256), 0, s, a);
+  return tw_prof_after(s);
+}

@@ -7,6 +7,8 @@
 int tw_decode_chunk(bool dense);
 size_t tw_new_tokens_workspace(const TwDims& d, int max_new);
 size_t tw_pages_workspace(const TwDims& d, int max_new, int new_batch);
+size_t tw_kv4_workspace(const TwDims& d, int max_new);
+size_t tw_keep_workspace(const TwDims& d);
 long long tw_decode_max_items(const TwDims& d, bool dense, int union_stride);
 
 int tw_check_kv(const twilight_kv_t* kv, TwDims* d) {
@@ -92,6 +94,10 @@ extern "C" size_t twilight_workspace_bytes(int which, const twilight_kv_t* kv, i
       return tw_new_tokens_workspace(d, max_sel);
     case TW_WS_PAGES:
       return tw_pages_workspace(d, max_sel, union_stride);
+    case TW_WS_KV4:
+      return tw_kv4_workspace(d, max_sel);
+    case TW_WS_KEEP:
+      return tw_keep_workspace(d);
     default:
       return 0;
   }
@@ -113,7 +119,8 @@ extern "C" int twilight_abi_version(void) { return TW_ABI_VERSION; }
 extern "C" const char* twilight_kernel_name(int id) {
   static const char* names[TW_K_COUNT] = {"kquant_append", "page_score", "page_select", "int4_score",
                                           "topp", "union", "sparse_decode", "combine", "score_topp", "select_score_topp",
-                                          "new_tokens", "new_combine", "pages_free", "pages_take", "pages_fork", "pages_copy", "compact"};
+                                          "new_tokens", "new_combine", "pages_free", "pages_take", "pages_fork", "pages_copy", "compact",
+                                          "kv4_attention", "kv4_combine", "kv4_append", "kv4_read", "attention_mass", "keep_tokens"};
   return (id >= 0 && id < TW_K_COUNT) ? names[id] : "?";
 }
 

@@ -24,6 +24,8 @@
 namespace {
 
 typedef _Float16 tw_f16x8 __attribute__((ext_vector_type(8)));
+typedef float tw_f32x16 __attribute__((ext_vector_type(16)));
+typedef short tw_s16x4 __attribute__((ext_vector_type(4)));
 typedef int tw_v2i __attribute__((ext_vector_type(2)));
 #define TW_LDS __attribute__((address_space(3)))
 #define TW_GLB __attribute__((address_space(1)))
@@ -405,31 +407,375 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(Kv4Args a) {
   }
 }
 
+// ------------------------------------------------------------------------------------------------------ many rows
+// More than 32 rows: a workgroup takes M = 32 * WR of them, whose waves share a tile of 64 tokens in LDS: each turns one page's codes
+// into operands, K's to bf16 numbers 0 .. 15, V's to fp16 values, while the tile before is computed (as in new_tokens.hip: 32 rows to a
+// wave, WT waves that split a tile's tokens).  The scores' group products T_g are two v_mfma_f32_32x32x16_bf16 each, scaled and summed by
+// one fma per score and group; what the zeros add, sum_g z_g Q_g, is two more products for all groups: z (11 bits) in two bf16 parts, Q_g
+// in three.
+struct Kv4WideArgs : Kv4Args {
+  static constexpr int TILE_PAGES = 4, MIN_TILES = 2, STREAM_TILES = 1 << 30;
+};
+constexpr int WIDE_V = 64 * 256, WIDE_Z = 2 * WIDE_V, WIDE_S = WIDE_Z + 64 * 16, WIDE_BUF = WIDE_S + 64 * 8;
+
+template <int WR, int WT, bool SPLIT>
+__device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Item& it, unsigned char (&buf0)[WIDE_BUF], unsigned char (&buf1)[WIDE_BUF],
+                                            int lane, int wave) {
+  constexpr int M = 32 * WR, MT = 2 / WT;
+  static_assert(WR * WT == 4, "a page of the tile to a wave");
+  const int wr = wave / WT, wt = wave % WT, half = lane >> 5;
+  const int b = __builtin_amdgcn_readfirstlane(it.b), rb = __builtin_amdgcn_readfirstlane(it.rb), h = __builtin_amdgcn_readfirstlane(it.h);
+  const int n = __builtin_amdgcn_readfirstlane(it.n), len = __builtin_amdgcn_readfirstlane(it.len), off = __builtin_amdgcn_readfirstlane(it.off);
+  const int ctx = len - n, rows = n * a.G, row = rb * M + wr * 32 + (lane & 31);
+  const bool live = row < rows;
+  const int tok = min(row, rows - 1) >> a.lgG, pos = ctx + tok;
+  const long long qrow = (long long)(off + tok) * a.Hq + h * a.G + (min(row, rows - 1) & (a.G - 1));
+  const int p_lo = ctx + ((rb * M) >> a.lgG), p_hi = ctx + ((min(rb * M + M, rows) - 1) >> a.lgG);
+  const int w_lo = ctx + (min(rb * M + wr * 32, rows - 1) >> a.lgG), w_hi = ctx + (min(rb * M + wr * 32 + 31, rows - 1) >> a.lgG);
+  const bool idle_wave = rb * M + wr * 32 >= rows;
+  const auto sp = span_of<MODE_WINDOW>(a, len, p_lo, p_hi);
+  const int per = SPLIT ? __builtin_amdgcn_readfirstlane((int)quotient((uint32_t)(sp.tiles + it.chunks - 1), (uint32_t)it.chunks)) : sp.tiles;
+  const int u0 = SPLIT ? min(sp.tiles, per * __builtin_amdgcn_readfirstlane(it.chunk)) : 0, u1 = min(sp.tiles, u0 + per);
+
+  tw_bf16x8 qf[8], qz[2];                        // qz: Q_g in parts, each for both parts of z; the third for the lower half's slots alone
+  {
+    float part[2][4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint4 x = a.q[qrow * 16 + 4 * g + 2 * k + half];
+        float f[8];
+        tw_unpack8(x, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += f[i];
+        qf[2 * g + k] = tw_as_bf16(x);
+      }
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+      sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+      const float first = (float)(__bf16)sum, second = (float)(__bf16)(sum - first);
+      part[0][g] = half ? second : first;
+      part[1][g] = half ? 0.f : sum - first - second;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) qz[k][i] = (__bf16)part[k][i / 2];
+  }
+
+  // ---- LDS.  Rows of 16 pieces of 16 bytes, stored in an order that depends on the row, as in new_tokens.hip: K's piece ^ row % 16, V's
+  // piece ^ (4 (row % 4) + 2 (row / 4 % 2)).  This lane stages token lane / 4 of its wave's page, group lane % 4.
+  const int st = lane >> 2, sg = lane & 3, v_order = ((st & 3) << 2) | ((st >> 2 & 1) << 1);
+  // of piece 2 s + half of K's row (32 s changes the bits of the piece), of the 4 tokens and 16 dims that 16 lanes take of V's (64 d)
+  const unsigned k_at = (unsigned)((wt * (64 / WT) + (lane & 31)) * 256 + ((half ^ (lane & 15)) << 4));
+  const unsigned v_at = (unsigned)(WIDE_V + (wt * (64 / WT) + 4 * half + ((lane & 15) >> 2)) * 256 +
+                                   (((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ ((lane & 15) >> 2 << 2) ^ (half << 1)) << 4) + (lane & 1) * 8);
+
+  // ---- page ids of 64 tiles at a time: lane k holds those of tile base + k
+  const int32_t* table = a.page_table + (long long)b * a.max_pages;
+  int mine = 0, base = u0;
+  unsigned long long mapped[4];                  // per page of a tile: the tiles (bits) where it is mapped
+  auto refill = [&](int u) {
+    const int v0 = 4 * min(u + lane, u1 - 1);
+    int id[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) id[j] = table[min(sp.page(v0 + j), a.max_pages - 1)];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mapped[j] = __ballot(v0 + j < sp.pages && (unsigned)id[j] < a.pool_pages);
+    const int x = wave & 2 ? (wave & 1 ? id[3] : id[2]) : (wave & 1 ? id[1] : id[0]);
+    mine = (unsigned)x < a.pool_pages ? x : 0;   // (page 0 is read for one that is not there, and not used)
+  };
+  auto held_pages = [&](int u) -> unsigned {
+    const int k = u - base;
+    return (unsigned)(mapped[0] >> k & 1) | (unsigned)(mapped[1] >> k & 1) << 1 | (unsigned)(mapped[2] >> k & 1) << 2 | (unsigned)(mapped[3] >> k & 1) << 3;
+  };
+  struct Codes { uint4 k, v; uint32_t km, vm; };
+  auto fetch = [&](Codes& x, int u) {
+    const int tk = (__builtin_amdgcn_readlane(mine, u - base) * a.Hkv + h) * TW_PAGE + st;
+    x.k = a.k_codes[(long long)tk * 4 + sg];
+    x.v = a.v_codes[(long long)tk * 4 + sg];
+    x.km = ((const uint32_t*)a.k_meta)[(long long)tk * 4 + sg];
+    x.vm = ((const uint32_t*)a.v_meta)[(long long)tk * 4 + sg];
+  };
+  auto stage = [&](unsigned char* buf, const Codes& x, int u, unsigned held) {
+    const int t = wave * TW_PAGE + st;           // of the tile
+    const bool token = (held >> wave & 1u) && sp.page(4 * u + wave) * TW_PAGE + st < len;
+    const uint32_t km = token ? x.km : 0u, vm = token ? x.vm : 0u;            // what is no token: 0, whose weight is 0
+    const uint32_t kw[4] = {x.k.x, x.k.y, x.k.z, x.k.w}, vw[4] = {x.v.x, x.v.y, x.v.z, x.v.w};
+    union { uint32_t u; tw_f16x2 h; } s2, z2;
+    s2.u = __builtin_amdgcn_perm(vm, vm, 0x05040504u);
+    z2.u = __builtin_amdgcn_perm(vm, vm, 0x07060706u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t kn[2] = {kw[i] & 0x0F0F0F0Fu, kw[i] >> 4 & 0x0F0F0F0Fu}, vn[2] = {vw[i] & 0x0F0F0F0Fu, vw[i] >> 4 & 0x0F0F0F0Fu};
+      uint32_t ko[4], vo[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t w = kn[j >> 1] >> (16 * (j & 1));
+        ko[j] = __builtin_amdgcn_perm(__float_as_uint((float)(w >> 8 & 0xFFu)), __float_as_uint((float)(w & 0xFFu)), 0x07060302u);
+        union { uint32_t u; tw_f16x2 h; } c, o;
+        c.u = __builtin_amdgcn_perm(0x64646464u, vn[j >> 1], j & 1 ? 0x04030402u : 0x04010400u);      // 1024 + c
+        o.h = __builtin_elementwise_fma(c.h - tw_f16x2{(_Float16)1024.f, (_Float16)1024.f}, s2.h, z2.h);
+        vo[j] = o.u;
+      }
+      *(uint4*)(buf + t * 256 + (((4 * sg + i) ^ st) << 4)) = make_uint4(ko[0], ko[1], ko[2], ko[3]);
+      *(uint4*)(buf + WIDE_V + t * 256 + (((4 * sg + i) ^ v_order) << 4)) = make_uint4(vo[0], vo[1], vo[2], vo[3]);
+    }
+    const float z = tw_half_hi(km), z1 = (float)(__bf16)z;
+    union { __bf16 e[2]; uint32_t u; } zz;
+    zz.e[0] = (__bf16)z1; zz.e[1] = (__bf16)(z - z1);
+    *(uint32_t*)(buf + WIDE_Z + t * 16 + sg * 4) = zz.u;
+    // scales by (group, 32 tokens, half wave): the 16 tokens of a lane's scores together
+    const int t32 = t & 31;
+    *(unsigned short*)(buf + WIDE_S + ((sg * 2 + (t >> 5)) * 2 + (t32 >> 2 & 1)) * 32 + (4 * (t32 >> 3) + (t32 & 3)) * 2) = (unsigned short)km;
+  };
+
+  tw_f32x16 o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+  float m = kLow, l = 0.f;
+  auto scale_of = [](float m) -> float { return __builtin_fabsf(m) < kFar ? kScaleLog2 : 0.25f; };
+  auto m_log2 = [&]() -> float { return __builtin_fabsf(m) < kFar ? m : m * kScaleLog2 * 4.f; };
+
+  auto compute = [&](const unsigned char* buf, int u, unsigned held) {
+    bool none = true, all = held == 15u;         // does no row of the wave see the tile, does every row see all of it
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int t = sp.page(4 * u + j) * TW_PAGE;
+      none = none & ((t > w_hi) | ((t + TW_PAGE - 1 <= w_lo - a.window) & (t >= a.sinks)));
+      all = all & (t + TW_PAGE - 1 <= w_lo) & ((t > w_hi - a.window) | (t + TW_PAGE <= a.sinks));
+    }
+    if (none | idle_wave) return;
+    unsigned k_rd = k_at, v_rd = v_at;
+    asm volatile("" : "+v"(k_rd), "+v"(v_rd));   // (the 12 addresses made of these are worked out here: held, they would spill)
+    tw_f32x16 s[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int blk = WT == 2 ? wt : mt;
+      const tw_bf16x8 z = *(const tw_bf16x8*)(buf + WIDE_Z + (blk * 32 + (lane & 31)) * 16);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[mt][r] = 0.f;
+      s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(z, qz[0], s[mt], 0, 0, 0);
+      s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(z, qz[1], s[mt], 0, 0, 0);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        tw_f32x16 t;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) t[r] = 0.f;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const tw_bf16x8*)(buf + (k_rd ^ (unsigned)(32 * (2 * g + k))) + mt * 32 * 256), qf[2 * g + k], t, 0, 0, 0);
+        const unsigned char* sc = buf + WIDE_S + ((g * 2 + blk) * 2 + half) * 32;
+        const uint4 x = *(const uint4*)sc, y = *(const uint4*)(sc + 16);
+        const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[mt][r] = __builtin_fmaf(r & 1 ? tw_half_hi(w[r / 2]) : tw_half_lo(w[r / 2]), t[r], s[mt][r]);
+      }
+    }
+    if (!all) {
+      unsigned long long vis = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int t = sp.page(4 * u + j) * TW_PAGE;
+        const uint32_t see = low16(pos + 1 - t) & (~low16(pos - a.window + 1 - t) | low16(a.sinks - t));
+        if (held >> j & 1u) vis |= (unsigned long long)see << (16 * j);
+      }
+      vis >>= wt * (64 / WT) + 4 * half;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        const uint32_t w = (uint32_t)(vis >> (32 * mt));
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {           // the row's bit, spread over a word, chooses the score or -inf
+          const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)w, 8 * (r / 4) + r % 4, 1);
+          s[mt][r] = __uint_as_float((keep & __float_as_uint(s[mt][r])) | (~keep & 0xFF800000u));
+        }
+      }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[mt][r]);
+    {
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    }
+    float c = scale_of(m);
+    if (__any(mx * c > m + (kLift + kGrowth4))) {
+      const float was = m_log2(), mn = fmaxf(was, mx * kScaleLog2 - kLift), al = __builtin_amdgcn_exp2f(was - mn);
+      l *= al;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= al;
+      if (mn > was) m = __builtin_fabsf(mn) < kFar ? mn : mx * 0.25f;
+      c = scale_of(m);
+    }
+    tw_f16x8 p[2 * MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][r], c, -m));
+        l += w;
+        p[2 * mt + r / 8][r % 8] = (_Float16)w;
+      }
+    union Frag { tw_s16x4 s[2]; tw_f16x8 v; };
+#pragma unroll
+    for (int ks = 0; ks < 2 * MT; ++ks)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        Frag f;
+        f.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TW_LDS tw_s16x4*)(buf + (v_rd ^ (unsigned)(64 * d)) + ks * 4096));
+        f.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TW_LDS tw_s16x4*)(buf + (v_rd ^ (unsigned)(64 * d)) + ks * 4096 + 2048));
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.v, p[ks], o[d], 0, 0, 0);
+      }
+  };
+
+  if (u0 < u1) {
+    Codes x;
+    refill(u0);
+    fetch(x, u0);
+    unsigned held = held_pages(u0), next = 0;
+    stage(buf0, x, u0, held);
+    if (u0 + 1 < u1) {                           // (base moves on only past the tiles whose pages have been asked for)
+      fetch(x, u0 + 1);
+      next = held_pages(u0 + 1);
+    }
+    // tile u is in its buffer, tile u + 1's codes on their way to registers
+    auto turn = [&](const unsigned char* now, unsigned char* then, int u) {
+      __syncthreads();                           // the tile is there for every wave, and nobody reads the other buffer any more
+      const unsigned here = held;
+      if (u + 1 < u1) {
+        stage(then, x, u + 1, next);
+        held = next;
+        if (u + 2 < u1) {
+          if (u + 2 - base >= 64) { base = u + 2; refill(base); }
+          fetch(x, u + 2);
+          next = held_pages(u + 2);
+        }
+      }
+      compute(now, u, here);
+    };
+    for (int u = u0; u < u1; u += 2) {
+      turn(buf0, buf1, u);
+      if (u + 1 >= u1) break;
+      turn(buf1, buf0, u + 1);
+    }
+  }
+
+  // ---- the waves' states of the same rows merged
+  m = m_log2();
+  {
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  }
+  if constexpr (WT > 1) {
+    __syncthreads();                             // the tiles have been read
+    float* part = (float*)(buf0 + wr * 16384);
+    float2* ml = (float2*)buf1 + wr * 32;
+    static_assert(WR * 16384 <= WIDE_BUF, "one partial per row wave");
+    if (wt == 1) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) part[(d * 16 + r) * 64 + lane] = o[d][r];
+      if (half == 0) ml[lane] = make_float2(m, l);
+    }
+    __syncthreads();
+    if (wt != 0) return;
+    const float2 x = ml[lane & 31];
+    const float mn = fmaxf(m, x.x), s0 = __builtin_amdgcn_exp2f(m - mn), s1 = __builtin_amdgcn_exp2f(x.x - mn);
+    l = l * s0 + x.y * s1;
+    m = mn;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = o[d][r] * s0 + part[(d * 16 + r) * 64 + lane] * s1;
+  }
+  if (!live) return;
+  if (!SPLIT || it.chunks == 1) {
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    uint2* orow = a.out + qrow * 32;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        union { __bf16 e[4]; uint2 v; } w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w.e[i] = (__bf16)(o[d][4 * k + i] * inv);
+        orow[8 * d + 2 * k + half] = w.v;
+      }
+    if (a.lse && half == 0) a.lse[qrow] = row_lse(m, l);
+    return;
+  }
+  const long long prow = (long long)it.slot * M + wr * 32 + (lane & 31);
+  float4* acc = (float4*)(a.ws_acc + prow * 128);
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[8 * d + 2 * k + half] = make_float4(o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]);
+  if (half == 0) a.ws_ml[prow] = make_float2(m, l);
+}
+
+template <int WR, int WT, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void kv4_wide_kernel(Kv4WideArgs a) {
+  constexpr int M = 32 * WR;
+  __shared__ __align__(1024) unsigned char buf0[WIDE_BUF];
+  __shared__ __align__(1024) unsigned char buf1[WIDE_BUF];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  Item it;
+  if (!SPLIT) {
+    if (whole_item<M>(a, &it)) attend_wide<WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave);
+    return;
+  }
+  Seq seq;
+  bool stream = false;
+  const int chunk = __builtin_amdgcn_readfirstlane(plan_chunk<MODE_WINDOW, M>(a, lane, &seq, &stream));
+  uint32_t want = blockIdx.x;
+  while (find_item<MODE_WINDOW, M>(a, lane, chunk, seq, want, &it)) {
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    attend_wide<WR, WT, SPLIT>(a, it, buf0, buf1, ln, wave);
+    want += gridDim.x;
+    if (want >= it.items) break;
+    __syncthreads();                             // the buffers have been read
+    if (a.batch <= 64) seq = seq_of<MODE_WINDOW, M>(a, lane);
+  }
+}
+
 template <int M, int LANES>
 __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Args a) { join_parts<M, LANES>(a); }
 
 // ---------------------------------------------------------------- host side
-int rows_per_block4(long long rows) { return rows <= 16 ? 16 : 32; }
+int rows_per_block4(long long rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
+// Lists that cannot be long are not cut, nor are the row blocks of prompts that fill the chip by themselves, but where single tokens may
+// stand beside a chunk (as in new_tokens.hip).  Tiles of 256 tokens (up to 32 rows) or 64.
+template <class A>
 bool cut_lists4(bool counted, int blocks, long long lists, long long longest) {
-  if (longest <= std::min(8ll, 1 + lists / 64)) return false;
+  constexpr long long UNIT = 16 / A::TILE_PAGES;
+  if (longest <= std::min(8 * UNIT, UNIT * (1 + lists / 64))) return false;
   const long long places = 2ll * tw_num_cus();
   if (blocks < 8 || lists < places) return true;
-  return counted && longest * places > 48 * lists;
+  return counted && longest * places > 48 * UNIT * lists;
 }
 
-template <int RT>
-int launch_kv4(const Kv4Args& a, hipStream_t s) {
-  constexpr int M = 16 * RT;
+template <int M, class A, class Whole, class Cut>
+int launch_kv4(const A& a, Whole whole, Cut cut, hipStream_t s) {
   const long long lists = (long long)a.rb_max * a.batch * a.Hkv, rows = (long long)a.max_new * a.Hq;
-  long long longest = ((long long)a.max_pages + 15) / 16;                       // tiles that a list can have
-  longest = std::min(longest, (((long long)a.sinks + TW_PAGE - 1) / TW_PAGE + ((long long)a.window + M / a.G + TW_PAGE - 2) / TW_PAGE + 1 + 15) / 16);
+  const long long pages = std::min<long long>(a.max_pages, ((long long)a.sinks + TW_PAGE - 1) / TW_PAGE + ((long long)a.window + M / a.G + TW_PAGE - 2) / TW_PAGE + 1);
+  const long long longest = (pages + A::TILE_PAGES - 1) / A::TILE_PAGES;        // tiles that a list can have
   tw_prof_before(TW_K_KV4_ATTENTION, s);
-  if (!cut_lists4(a.n_new != nullptr, a.rb_max, lists, longest) || rows >= (1ll << 26)) {
-    TW_LAUNCH((kv4_attention_kernel<RT, false>), dim3((unsigned)lists), dim3(256), 0, s, a);
+  if (!cut_lists4<A>(a.n_new != nullptr, a.rb_max, lists, longest) || rows >= (1ll << 26)) {
+    TW_LAUNCH(whole, dim3((unsigned)lists), dim3(256), 0, s, a);
     return tw_prof_after(s);
   }
-  TW_LAUNCH((kv4_attention_kernel<RT, true>), dim3((unsigned)std::min(lists * longest, 2ll * a.cus)), dim3(256), 0, s, a);
+  const long long most = lists * ((longest + A::MIN_TILES - 1) / A::MIN_TILES);
+  TW_LAUNCH(cut, dim3((unsigned)std::min(most, 2ll * a.cus)), dim3(256), 0, s, a);
   if (int e = tw_prof_after(s)) return e;
   tw_prof_before(TW_K_KV4_COMBINE, s);
   if (rows * a.batch <= COMBINE_FEW) TW_LAUNCH((kv4_combine_kernel<M, 8>), dim3((unsigned)rows, (unsigned)a.batch), dim3(256), 0, s, a);
@@ -437,11 +783,13 @@ int launch_kv4(const Kv4Args& a, hipStream_t s) {
   return tw_prof_after(s);
 }
 
-// Parts that a plan can make: fewer than 2 W rounds (plan_chunk); of one row block per sequence and KV head no more than its list has tiles.
+// Parts that a plan can make: fewer than 2 W rounds (plan_chunk); of one row block per sequence and KV head no more than its
+// list has chunks of the shortest length.
 size_t part_slots4(const TwDims& d, long long rows) {
   const long long most = (long long)tw_num_cus() * 4 * PLAN_ROUNDS;
-  if (rows > 32) return (size_t)most;
-  return (size_t)std::min(most, ((long long)d.max_pages + 15) / 16 * d.batch * d.Hkv);
+  if (rows > 128) return (size_t)most;
+  const long long pages = rows <= 32 ? Kv4Args::TILE_PAGES * Kv4Args::MIN_TILES : Kv4WideArgs::TILE_PAGES * Kv4WideArgs::MIN_TILES;   // of the shortest chunk
+  return (size_t)std::min(most, (d.max_pages + pages - 1) / pages * d.batch * d.Hkv);
 }
 
 }  // namespace
@@ -467,7 +815,7 @@ extern "C" int twilight_kv4_attention(const twilight_kv_t* kv, const void* vq_po
   const long long rows = (long long)max_new * d.G;
   const int M = rows_per_block4(rows);
   const int32_t most = 1 << 30;                  // longer than any sequence; positions minus it stay in 32 bits
-  Kv4Args a;
+  Kv4WideArgs a;
   a.q = (const uint4*)q;
   a.k_codes = (const uint4*)kv->kq_pool; a.k_meta = (const uint4*)kv->kq_meta; a.v_codes = (const uint4*)vq_pool; a.v_meta = (const uint4*)vq_meta;
   a.page_table = kv->page_table; a.seq_lens = kv->seq_lens; a.n_new = n_new; a.offsets = new_offsets;
@@ -482,5 +830,10 @@ extern "C" int twilight_kv4_attention(const twilight_kv_t* kv, const void* vq_po
   const long long lists = (long long)a.rb_max * d.batch * d.Hkv;
   if (lists >= (1ll << 24) || (long long)max_new * d.batch >= (1ll << 31)) return TW_EINVAL;      // (a launch has fewer than 2^32 threads)
   hipStream_t s = (hipStream_t)stream;
-  return M == 16 ? launch_kv4<1>(a, s) : launch_kv4<2>(a, s);
+  switch (M) {
+    case 16: return launch_kv4<16>((const Kv4Args&)a, kv4_attention_kernel<1, false>, kv4_attention_kernel<1, true>, s);
+    case 32: return launch_kv4<32>((const Kv4Args&)a, kv4_attention_kernel<2, false>, kv4_attention_kernel<2, true>, s);
+    case 64: return launch_kv4<64>(a, kv4_wide_kernel<2, 2, false>, kv4_wide_kernel<2, 2, true>, s);
+    default: return launch_kv4<128>(a, kv4_wide_kernel<4, 1, false>, kv4_wide_kernel<4, 1, true>, s);
+  }
 }

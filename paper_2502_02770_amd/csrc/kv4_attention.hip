@@ -57,6 +57,104 @@ struct Kv4Args {
   unsigned pool_pages;
 };
 
+// How a launch that cuts its lists shares them out: all lists' tiles in one row, sequence by sequence, of which every workgroup takes as
+// many as the others - the end of one list, whole ones, the start of another.  Chunks of a length and one after the other to the
+// workgroups, as the bf16 kernel has them, left the chip idle for 38 % of the time where 64 sequences of 1000 to 32001 tokens make as
+// many lists as there are workgroups.  Of a list that is cut, a workgroup w has a part with its first tile (place 2 w of the workspace) or
+// one with its last (2 w + 1).
+struct Piece {
+  int b, n, len, off, rb, h;                     // the sequence, as Seq; row block and KV head
+  int from, to, tiles;                           // of the list's tiles
+  int slot;                                      // its place in the workspace, if the list is cut
+};
+struct Shares {
+  uint32_t per, total;                           // tiles of a workgroup, of all lists
+};
+template <int M, class A>
+__device__ __forceinline__ Shares shares_of(const A& a, int lane) {
+  uint32_t total = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const Seq q = seq_of<MODE_WINDOW, M>(a, b0 + lane);
+    total += (uint32_t)__builtin_amdgcn_readlane((int)tw_wave_scan_u32((uint32_t)q.lists * (uint32_t)q.tiles), 63);
+  }
+  const uint32_t wgs = gridDim.x;
+  return {max((uint32_t)A::MIN_TILES, (total + wgs - 1u) / wgs), total};
+}
+// The piece that begins with tile `pos`, the workgroup's first or a later one, of those before `end`; tells the launch that joins the parts where lists begin.
+template <int M, class A>
+__device__ __forceinline__ void piece_at(const A& a, int lane, uint32_t per, uint32_t pos, uint32_t end, bool tell, Piece* it) {
+  uint32_t tiles = 0;
+  bool found = false;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const Seq q = seq_of<MODE_WINDOW, M>(a, b0 + lane);
+    const uint32_t mine = (uint32_t)q.lists * (uint32_t)q.tiles;
+    const uint32_t te = tw_wave_scan_u32(mine);
+    if (tell && b0 + lane < a.batch) ((int2*)a.ws_plan)[1 + b0 + lane] = make_int2((int)(tiles + te - mine), q.tiles);
+    const unsigned long long here = __ballot(tiles + te > pos);
+    if (!found && here) {
+      const int l = __builtin_ctzll(here);
+      it->b = b0 + l;
+      it->n = __builtin_amdgcn_readlane(q.n, l);
+      it->len = __builtin_amdgcn_readlane(q.len, l);
+      it->off = __builtin_amdgcn_readlane(q.off, l);
+      it->tiles = __builtin_amdgcn_readlane(q.tiles, l);
+      const uint32_t in = pos - (tiles + (uint32_t)__builtin_amdgcn_readlane((int)(te - mine), l)), k = in / (uint32_t)it->tiles;
+      it->from = (int)(in - k * (uint32_t)it->tiles);
+      it->to = (int)min((uint32_t)it->tiles, (uint32_t)it->from + (end - pos));
+      it->rb = (int)(k / (uint32_t)a.Hkv);
+      it->h = (int)(k - (uint32_t)it->rb * (uint32_t)a.Hkv);
+      it->slot = 2 * (int)blockIdx.x + (pos == blockIdx.x * per ? 0 : 1);
+      found = true;
+      if (!tell) return;
+    }
+    tiles += (uint32_t)__builtin_amdgcn_readlane((int)te, 63);
+  }
+}
+template <int M, class A>
+__device__ __forceinline__ bool whole_piece(const A& a, Piece* it) {
+  Item x;
+  if (!whole_item<M>(a, &x)) return false;
+  it->b = x.b; it->n = x.n; it->len = x.len; it->off = x.off; it->rb = x.rb; it->h = x.h;
+  it->from = 0; it->to = it->tiles = 1 << 30;    // all there are
+  it->slot = 0;
+  return true;
+}
+// The workgroup's pieces, one after the other.
+template <int M, class A, class F>
+__device__ __forceinline__ void for_pieces(const A& a, int lane, F attend) {
+  const Shares s = shares_of<M>(a, lane);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *(int2*)a.ws_plan = make_int2((int)s.per, 0);
+  const unsigned long long begin = (unsigned long long)blockIdx.x * s.per;
+  uint32_t pos = (uint32_t)min(begin, (unsigned long long)s.total);
+  const uint32_t end = (uint32_t)min(begin + s.per, (unsigned long long)s.total);
+  Piece it;
+  if (blockIdx.x == 0 && s.total == 0) piece_at<M>(a, lane, s.per, 0, 0, threadIdx.x < 64, &it);
+  while (pos < end) {
+    piece_at<M>(a, lane, s.per, pos, end, pos == 0 && threadIdx.x < 64, &it);
+    int ln = lane;
+    asm volatile("" : "+v"(ln));                 // what depends on the lane alone is worked out for every piece: held over them it would spill
+    attend(it, ln);
+    pos += (uint32_t)__builtin_amdgcn_readfirstlane(it.to - it.from);
+    if (pos < end) __syncthreads();              // the buffers have been read
+  }
+}
+// Rows of lists that were cut: their parts joined.
+template <int M, int LANES, class A>
+__device__ __forceinline__ void join_shares(const A& a) {
+  constexpr int ROWS = 8 / LANES;
+  const int b = blockIdx.y, idx = (int)(blockIdx.x * ROWS + threadIdx.x / (32 * LANES));
+  const int n = seq_new(a, b), tok = idx / a.Hq, head = idx - tok * a.Hq;
+  if (tok >= n) return;
+  const uint32_t per = (uint32_t)a.ws_plan[0];
+  const int2 p = ((const int2*)a.ws_plan)[1 + b];            // the sequence's first tile, tiles of a list
+  const int row = tok * a.G + (head & (a.G - 1));
+  const uint32_t k = (uint32_t)((row / M) * a.Hkv + (head >> a.lgG)), t0 = (uint32_t)p.x + k * (uint32_t)p.y;
+  const uint32_t first = t0 / per, last = (t0 + (uint32_t)p.y - 1u) / per;
+  if (first == last) return;                     // written by the attention kernel itself
+  const int late = t0 == first * per ? 0 : 1;    // the first part is its workgroup's last
+  fold_parts<LANES>(a, b, tok, head, true, (int)(last - first + 1u), [=](int c) { return (long long)(2 * ((int)first + c) + (c ? 0 : late)) * M + row % M; });
+}
+
 // the lowest x of 16 bits
 __device__ __forceinline__ uint32_t low16(int x) { return x <= 0 ? 0u : x >= 16 ? 0xFFFFu : (1u << x) - 1u; }
 
@@ -81,7 +179,7 @@ __device__ __forceinline__ tw_f16x8 codes_f16(uint32_t w, const uint4& s, const 
 
 // One item: a chunk of a list.
 template <int RT, bool SPLIT>
-__device__ __forceinline__ void attend_item(const Kv4Args& a, const Item& it, unsigned char (&buf0)[WAVES * BUF], unsigned char (&buf1)[WAVES * BUF],
+__device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, unsigned char (&buf0)[WAVES * BUF], unsigned char (&buf1)[WAVES * BUF],
                                             unsigned char (&vms)[WAVES * 1024], int lane, int wave) {
   constexpr int M = 16 * RT;
   const int r16 = lane & 15, jq = lane >> 4;
@@ -94,8 +192,8 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Item& it, un
   auto qrow_of = [&](int rt) { return (long long)(off + (row_of(rt) >> a.lgG)) * a.Hq + h * a.G + (row_of(rt) & (a.G - 1)); };
   const int p_lo = ctx + ((rb * M) >> a.lgG), p_hi = ctx + ((min(rb * M + M, rows) - 1) >> a.lgG);
   const auto sp = span_of<MODE_WINDOW>(a, len, p_lo, p_hi);
-  const int per = SPLIT ? __builtin_amdgcn_readfirstlane((int)quotient((uint32_t)(sp.tiles + it.chunks - 1), (uint32_t)it.chunks)) : sp.tiles;
-  const int u0 = SPLIT ? min(sp.tiles, per * __builtin_amdgcn_readfirstlane(it.chunk)) : 0, u1 = min(sp.tiles, u0 + per);
+  const int u0 = SPLIT ? min(sp.tiles, __builtin_amdgcn_readfirstlane(it.from)) : 0, u1 = SPLIT ? min(sp.tiles, __builtin_amdgcn_readfirstlane(it.to)) : sp.tiles;
+  const bool whole = !SPLIT || it.to - it.from == it.tiles;
 
   int pos[RT];
   tw_bf16x8 qf[RT][4];
@@ -354,7 +452,7 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Item& it, un
     if (rb * M + rt * 16 + r16 >= rows) continue;
     // element i of block d: dim 16 d + 8 (jq / 2) + 2 (jq % 2) + {0, 4, 1, 5}[i]
     const int at = 16 * wave + 4 * (jq >> 1) + (jq & 1);                      // in pairs of dims
-    if (!SPLIT || it.chunks == 1) {
+    if (whole) {
       const float inv = ls == 0.f ? 0.f : 1.0f / ls;
       const long long qrow = qrow_of(rt);
       uint32_t* orow = (uint32_t*)a.out + qrow * 64;
@@ -379,7 +477,7 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Item& it, un
   }
 }
 
-// SPLIT: resident workgroups stride over the items; otherwise a workgroup per list.
+// SPLIT: resident workgroups share the lists; otherwise a workgroup per list.
 template <int RT, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(Kv4Args a) {
   constexpr int M = 16 * RT;
@@ -387,24 +485,12 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(Kv4Args a) {
   __shared__ __align__(1024) unsigned char buf1[WAVES * BUF];
   __shared__ __align__(1024) unsigned char vms[WAVES * 1024];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  Item it;
   if (!SPLIT) {
-    if (whole_item<M>(a, &it)) attend_item<RT, SPLIT>(a, it, buf0, buf1, vms, lane, wave);
+    Piece it;
+    if (whole_piece<M>(a, &it)) attend_item<RT, SPLIT>(a, it, buf0, buf1, vms, lane, wave);
     return;
   }
-  Seq seq;
-  bool stream = false;
-  const int chunk = __builtin_amdgcn_readfirstlane(plan_chunk<MODE_WINDOW, M>(a, lane, &seq, &stream));
-  uint32_t want = blockIdx.x;
-  while (find_item<MODE_WINDOW, M>(a, lane, chunk, seq, want, &it)) {
-    int ln = lane;
-    asm volatile("" : "+v"(ln));                 // what depends on the lane alone is worked out for every item: held over the items it would spill
-    attend_item<RT, SPLIT>(a, it, buf0, buf1, vms, ln, wave);
-    want += gridDim.x;
-    if (want >= it.items) break;
-    __syncthreads();                             // the buffers have been read
-    if (a.batch <= 64) seq = seq_of<MODE_WINDOW, M>(a, lane);        // (again: held over the item it would cost registers that there are not)
-  }
+  for_pieces<M>(a, lane, [&](const Piece& it, int ln) { attend_item<RT, SPLIT>(a, it, buf0, buf1, vms, ln, wave); });
 }
 
 // ------------------------------------------------------------------------------------------------------ many rows
@@ -419,7 +505,7 @@ struct Kv4WideArgs : Kv4Args {
 constexpr int WIDE_V = 64 * 256, WIDE_Z = 2 * WIDE_V, WIDE_S = WIDE_Z + 64 * 16, WIDE_BUF = WIDE_S + 64 * 8;
 
 template <int WR, int WT, bool SPLIT>
-__device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Item& it, unsigned char (&buf0)[WIDE_BUF], unsigned char (&buf1)[WIDE_BUF],
+__device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Piece& it, unsigned char (&buf0)[WIDE_BUF], unsigned char (&buf1)[WIDE_BUF],
                                             int lane, int wave) {
   constexpr int M = 32 * WR, MT = 2 / WT;
   static_assert(WR * WT == 4, "a page of the tile to a wave");
@@ -432,10 +518,9 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Item& it
   const long long qrow = (long long)(off + tok) * a.Hq + h * a.G + (min(row, rows - 1) & (a.G - 1));
   const int p_lo = ctx + ((rb * M) >> a.lgG), p_hi = ctx + ((min(rb * M + M, rows) - 1) >> a.lgG);
   const int w_lo = ctx + (min(rb * M + wr * 32, rows - 1) >> a.lgG), w_hi = ctx + (min(rb * M + wr * 32 + 31, rows - 1) >> a.lgG);
-  const bool idle_wave = rb * M + wr * 32 >= rows;
   const auto sp = span_of<MODE_WINDOW>(a, len, p_lo, p_hi);
-  const int per = SPLIT ? __builtin_amdgcn_readfirstlane((int)quotient((uint32_t)(sp.tiles + it.chunks - 1), (uint32_t)it.chunks)) : sp.tiles;
-  const int u0 = SPLIT ? min(sp.tiles, per * __builtin_amdgcn_readfirstlane(it.chunk)) : 0, u1 = min(sp.tiles, u0 + per);
+  const int u0 = SPLIT ? min(sp.tiles, __builtin_amdgcn_readfirstlane(it.from)) : 0, u1 = SPLIT ? min(sp.tiles, __builtin_amdgcn_readfirstlane(it.to)) : sp.tiles;
+  const bool whole = !SPLIT || it.to - it.from == it.tiles;
 
   tw_bf16x8 qf[8], qz[2];                        // qz: Q_g in parts, each for both parts of z; the third for the lower half's slots alone
   {
@@ -498,37 +583,38 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Item& it
     x.km = ((const uint32_t*)a.k_meta)[(long long)tk * 4 + sg];
     x.vm = ((const uint32_t*)a.v_meta)[(long long)tk * 4 + sg];
   };
-  auto stage = [&](unsigned char* buf, const Codes& x, int u, unsigned held) {
-    const int t = wave * TW_PAGE + st;           // of the tile
+  // this lane's part of a tile's operands: (scale, zero) first, then four words of K's and V's codes
+  const int stt = wave * TW_PAGE + st;           // of the tile
+  struct Staged { tw_f16x2 s, z; };
+  auto stage_meta = [&](unsigned char* buf, Codes& x, int u, unsigned held) -> Staged {
     const bool token = (held >> wave & 1u) && sp.page(4 * u + wave) * TW_PAGE + st < len;
     const uint32_t km = token ? x.km : 0u, vm = token ? x.vm : 0u;            // what is no token: 0, whose weight is 0
-    const uint32_t kw[4] = {x.k.x, x.k.y, x.k.z, x.k.w}, vw[4] = {x.v.x, x.v.y, x.v.z, x.v.w};
-    union { uint32_t u; tw_f16x2 h; } s2, z2;
-    s2.u = __builtin_amdgcn_perm(vm, vm, 0x05040504u);
-    z2.u = __builtin_amdgcn_perm(vm, vm, 0x07060706u);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t kn[2] = {kw[i] & 0x0F0F0F0Fu, kw[i] >> 4 & 0x0F0F0F0Fu}, vn[2] = {vw[i] & 0x0F0F0F0Fu, vw[i] >> 4 & 0x0F0F0F0Fu};
-      uint32_t ko[4], vo[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t w = kn[j >> 1] >> (16 * (j & 1));
-        ko[j] = __builtin_amdgcn_perm(__float_as_uint((float)(w >> 8 & 0xFFu)), __float_as_uint((float)(w & 0xFFu)), 0x07060302u);
-        union { uint32_t u; tw_f16x2 h; } c, o;
-        c.u = __builtin_amdgcn_perm(0x64646464u, vn[j >> 1], j & 1 ? 0x04030402u : 0x04010400u);      // 1024 + c
-        o.h = __builtin_elementwise_fma(c.h - tw_f16x2{(_Float16)1024.f, (_Float16)1024.f}, s2.h, z2.h);
-        vo[j] = o.u;
-      }
-      *(uint4*)(buf + t * 256 + (((4 * sg + i) ^ st) << 4)) = make_uint4(ko[0], ko[1], ko[2], ko[3]);
-      *(uint4*)(buf + WIDE_V + t * 256 + (((4 * sg + i) ^ v_order) << 4)) = make_uint4(vo[0], vo[1], vo[2], vo[3]);
-    }
     const float z = tw_half_hi(km), z1 = (float)(__bf16)z;
     union { __bf16 e[2]; uint32_t u; } zz;
     zz.e[0] = (__bf16)z1; zz.e[1] = (__bf16)(z - z1);
-    *(uint32_t*)(buf + WIDE_Z + t * 16 + sg * 4) = zz.u;
+    *(uint32_t*)(buf + WIDE_Z + stt * 16 + sg * 4) = zz.u;
     // scales by (group, 32 tokens, half wave): the 16 tokens of a lane's scores together
-    const int t32 = t & 31;
-    *(unsigned short*)(buf + WIDE_S + ((sg * 2 + (t >> 5)) * 2 + (t32 >> 2 & 1)) * 32 + (4 * (t32 >> 3) + (t32 & 3)) * 2) = (unsigned short)km;
+    const int t32 = stt & 31;
+    *(unsigned short*)(buf + WIDE_S + ((sg * 2 + (stt >> 5)) * 2 + (t32 >> 2 & 1)) * 32 + (4 * (t32 >> 3) + (t32 & 3)) * 2) = (unsigned short)km;
+    union { uint32_t u; tw_f16x2 h; } s2, z2;
+    s2.u = __builtin_amdgcn_perm(vm, vm, 0x05040504u);
+    z2.u = __builtin_amdgcn_perm(vm, vm, 0x07060706u);
+    return {s2.h, z2.h};
+  };
+  auto stage_word = [&](unsigned char* buf, uint32_t kw, uint32_t vw, int i, const Staged& sz) {
+    const uint32_t kn[2] = {kw & 0x0F0F0F0Fu, kw >> 4 & 0x0F0F0F0Fu}, vn[2] = {vw & 0x0F0F0F0Fu, vw >> 4 & 0x0F0F0F0Fu};
+    uint32_t ko[4], vo[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t w = kn[j >> 1] >> (16 * (j & 1));
+      ko[j] = __builtin_amdgcn_perm(__float_as_uint((float)(w >> 8 & 0xFFu)), __float_as_uint((float)(w & 0xFFu)), 0x07060302u);
+      union { uint32_t u; tw_f16x2 h; } c, o;
+      c.u = __builtin_amdgcn_perm(0x64646464u, vn[j >> 1], j & 1 ? 0x04030402u : 0x04010400u);        // 1024 + c
+      o.h = __builtin_elementwise_fma(c.h - tw_f16x2{(_Float16)1024.f, (_Float16)1024.f}, sz.s, sz.z);
+      vo[j] = o.u;
+    }
+    *(uint4*)(buf + stt * 256 + (((4 * sg + i) ^ st) << 4)) = make_uint4(ko[0], ko[1], ko[2], ko[3]);
+    *(uint4*)(buf + WIDE_V + stt * 256 + (((4 * sg + i) ^ v_order) << 4)) = make_uint4(vo[0], vo[1], vo[2], vo[3]);
   };
 
   tw_f32x16 o[4];
@@ -540,18 +626,13 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Item& it
   auto scale_of = [](float m) -> float { return __builtin_fabsf(m) < kFar ? kScaleLog2 : 0.25f; };
   auto m_log2 = [&]() -> float { return __builtin_fabsf(m) < kFar ? m : m * kScaleLog2 * 4.f; };
 
-  auto compute = [&](const unsigned char* buf, int u, unsigned held) {
-    bool none = true, all = held == 15u;         // does no row of the wave see the tile, does every row see all of it
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int t = sp.page(4 * u + j) * TW_PAGE;
-      none = none & ((t > w_hi) | ((t + TW_PAGE - 1 <= w_lo - a.window) & (t >= a.sinks)));
-      all = all & (t + TW_PAGE - 1 <= w_lo) & ((t > w_hi - a.window) | (t + TW_PAGE <= a.sinks));
-    }
-    if (none | idle_wave) return;
-    unsigned k_rd = k_at, v_rd = v_at;
-    asm volatile("" : "+v"(k_rd), "+v"(v_rd));   // (the 12 addresses made of these are worked out here: held, they would spill)
-    tw_f32x16 s[MT];
+  // The scores of tile u, and between their products the next tile's operands made (of whatever the registers hold where there is none)
+  tw_f32x16 s[MT];
+  auto scores = [&](const unsigned char* buf, unsigned char* then, Codes& x, int u, unsigned next) {
+    unsigned k_rd = k_at;
+    asm volatile("" : "+v"(k_rd));               // (the addresses made of it are worked out here: held, they would spill)
+    const Staged sz = stage_meta(then, x, u + 1, next);
+    const uint32_t kw[4] = {x.k.x, x.k.y, x.k.z, x.k.w}, vw[4] = {x.v.x, x.v.y, x.v.z, x.v.w};
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const int blk = WT == 2 ? wt : mt;
@@ -568,13 +649,28 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Item& it
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const tw_bf16x8*)(buf + (k_rd ^ (unsigned)(32 * (2 * g + k))) + mt * 32 * 256), qf[2 * g + k], t, 0, 0, 0);
+        if (MT == 1 || g % 2 == 1) {
+          const int i = MT == 1 ? g : 2 * mt + g / 2;
+          stage_word(then, kw[i], vw[i], i, sz);
+        }
         const unsigned char* sc = buf + WIDE_S + ((g * 2 + blk) * 2 + half) * 32;
         const uint4 x = *(const uint4*)sc, y = *(const uint4*)(sc + 16);
         const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[mt][r] = __builtin_fmaf(r & 1 ? tw_half_hi(w[r / 2]) : tw_half_lo(w[r / 2]), t[r], s[mt][r]);
+        asm volatile("" : "+v"(s[mt]));          // here and now: sunk behind the branches to come, all groups' products would wait in registers
       }
     }
+  };
+  auto weights = [&](const unsigned char* buf, int u, unsigned held) {
+    bool all = held == 15u;                      // does every row see all of the tile
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int t = sp.page(4 * u + j) * TW_PAGE;
+      all = all & (t + TW_PAGE - 1 <= w_lo) & ((t > w_hi - a.window) | (t + TW_PAGE <= a.sinks));
+    }
+    unsigned v_rd = v_at;
+    asm volatile("" : "+v"(v_rd));
     if (!all) {
       unsigned long long vis = 0;
 #pragma unroll
@@ -636,34 +732,40 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Item& it
   };
 
   if (u0 < u1) {
-    Codes x;
+    // tile u is in its buffer, the codes of tiles u + 1 (asked for two turns ago) and u + 2 on their way to registers; pages[]: which of
+    // their pages are there
+    Codes ahead[2];
+    unsigned pages[2] = {0u, 0u};
+    auto ask = [&](int k, int u) {               // (`base` moves on only past tiles that have been asked for)
+      if (u >= u1) return;
+      if (u - base >= 64) { base = u; refill(u); }
+      fetch(ahead[k], u);
+      pages[k] = held_pages(u);
+    };
     refill(u0);
-    fetch(x, u0);
-    unsigned held = held_pages(u0), next = 0;
-    stage(buf0, x, u0, held);
-    if (u0 + 1 < u1) {                           // (base moves on only past the tiles whose pages have been asked for)
-      fetch(x, u0 + 1);
-      next = held_pages(u0 + 1);
+    ask(0, u0);
+    ahead[1] = ahead[0];
+    ask(1, u0 + 1);
+    unsigned held = pages[0];
+    {
+      const Staged sz = stage_meta(buf0, ahead[0], u0, held);
+      const uint32_t kw[4] = {ahead[0].k.x, ahead[0].k.y, ahead[0].k.z, ahead[0].k.w}, vw[4] = {ahead[0].v.x, ahead[0].v.y, ahead[0].v.z, ahead[0].v.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) stage_word(buf0, kw[i], vw[i], i, sz);
     }
-    // tile u is in its buffer, tile u + 1's codes on their way to registers
-    auto turn = [&](const unsigned char* now, unsigned char* then, int u) {
+    ask(0, u0 + 2);
+    auto turn = [&](const unsigned char* now, unsigned char* then, int k, int u) {
       __syncthreads();                           // the tile is there for every wave, and nobody reads the other buffer any more
+      scores(now, then, ahead[k], u, pages[k]);
       const unsigned here = held;
-      if (u + 1 < u1) {
-        stage(then, x, u + 1, next);
-        held = next;
-        if (u + 2 < u1) {
-          if (u + 2 - base >= 64) { base = u + 2; refill(base); }
-          fetch(x, u + 2);
-          next = held_pages(u + 2);
-        }
-      }
-      compute(now, u, here);
+      held = pages[k];
+      ask(k, u + 3);
+      weights(now, u, here);
     };
     for (int u = u0; u < u1; u += 2) {
-      turn(buf0, buf1, u);
+      turn(buf0, buf1, 1, u);
       if (u + 1 >= u1) break;
-      turn(buf1, buf0, u + 1);
+      turn(buf1, buf0, 0, u + 1);
     }
   }
 
@@ -697,7 +799,7 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Item& it
       for (int r = 0; r < 16; ++r) o[d][r] = o[d][r] * s0 + part[(d * 16 + r) * 64 + lane] * s1;
   }
   if (!live) return;
-  if (!SPLIT || it.chunks == 1) {
+  if (whole) {
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     uint2* orow = a.out + qrow * 32;
 #pragma unroll
@@ -727,28 +829,16 @@ __global__ __launch_bounds__(256, 2) void kv4_wide_kernel(Kv4WideArgs a) {
   __shared__ __align__(1024) unsigned char buf0[WIDE_BUF];
   __shared__ __align__(1024) unsigned char buf1[WIDE_BUF];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  Item it;
   if (!SPLIT) {
-    if (whole_item<M>(a, &it)) attend_wide<WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave);
+    Piece it;
+    if (whole_piece<M>(a, &it)) attend_wide<WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave);
     return;
   }
-  Seq seq;
-  bool stream = false;
-  const int chunk = __builtin_amdgcn_readfirstlane(plan_chunk<MODE_WINDOW, M>(a, lane, &seq, &stream));
-  uint32_t want = blockIdx.x;
-  while (find_item<MODE_WINDOW, M>(a, lane, chunk, seq, want, &it)) {
-    int ln = lane;
-    asm volatile("" : "+v"(ln));
-    attend_wide<WR, WT, SPLIT>(a, it, buf0, buf1, ln, wave);
-    want += gridDim.x;
-    if (want >= it.items) break;
-    __syncthreads();                             // the buffers have been read
-    if (a.batch <= 64) seq = seq_of<MODE_WINDOW, M>(a, lane);
-  }
+  for_pieces<M>(a, lane, [&](const Piece& it, int ln) { attend_wide<WR, WT, SPLIT>(a, it, buf0, buf1, ln, wave); });
 }
 
 template <int M, int LANES>
-__global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Args a) { join_parts<M, LANES>(a); }
+__global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Args a) { join_shares<M, LANES>(a); }
 
 // ---------------------------------------------------------------- host side
 int rows_per_block4(long long rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
@@ -770,7 +860,7 @@ int launch_kv4(const A& a, Whole whole, Cut cut, hipStream_t s) {
   const long long pages = std::min<long long>(a.max_pages, ((long long)a.sinks + TW_PAGE - 1) / TW_PAGE + ((long long)a.window + M / a.G + TW_PAGE - 2) / TW_PAGE + 1);
   const long long longest = (pages + A::TILE_PAGES - 1) / A::TILE_PAGES;        // tiles that a list can have
   tw_prof_before(TW_K_KV4_ATTENTION, s);
-  if (!cut_lists4<A>(a.n_new != nullptr, a.rb_max, lists, longest) || rows >= (1ll << 26)) {
+  if (!cut_lists4<A>(a.n_new != nullptr, a.rb_max, lists, longest) || rows >= (1ll << 26) || lists * longest >= (1ll << 32)) {
     TW_LAUNCH(whole, dim3((unsigned)lists), dim3(256), 0, s, a);
     return tw_prof_after(s);
   }
@@ -783,13 +873,11 @@ int launch_kv4(const A& a, Whole whole, Cut cut, hipStream_t s) {
   return tw_prof_after(s);
 }
 
-// Parts that a plan can make: fewer than 2 W rounds (plan_chunk); of one row block per sequence and KV head no more than its
-// list has chunks of the shortest length.
+// Places for parts: two of every workgroup that can have tiles.
 size_t part_slots4(const TwDims& d, long long rows) {
-  const long long most = (long long)tw_num_cus() * 4 * PLAN_ROUNDS;
-  if (rows > 128) return (size_t)most;
-  const long long pages = rows <= 32 ? Kv4Args::TILE_PAGES * Kv4Args::MIN_TILES : Kv4WideArgs::TILE_PAGES * Kv4WideArgs::MIN_TILES;   // of the shortest chunk
-  return (size_t)std::min(most, (d.max_pages + pages - 1) / pages * d.batch * d.Hkv);
+  const int M = rows_per_block4(rows), chunk = rows <= 32 ? Kv4Args::TILE_PAGES * Kv4Args::MIN_TILES : Kv4WideArgs::TILE_PAGES * Kv4WideArgs::MIN_TILES;
+  const long long lists = (rows + M - 1) / M * d.batch * d.Hkv, places = 2ll * tw_num_cus();
+  return (size_t)(2 * std::min(places, lists * ((d.max_pages + chunk - 1) / chunk)));
 }
 
 }  // namespace
@@ -799,7 +887,7 @@ size_t tw_kv4_workspace(const TwDims& d, int max_new) {
   const long long rows = (long long)max_new * d.G;
   const int M = rows_per_block4(rows);
   const size_t slots = part_slots4(d, rows);
-  return align256n((size_t)d.batch * 8) + align256n(slots * M * 8) + slots * M * 512;
+  return align256n((size_t)(d.batch + 1) * 8) + align256n(slots * M * 8) + slots * M * 512;
 }
 
 extern "C" int twilight_kv4_attention(const twilight_kv_t* kv, const void* vq_pool, const void* vq_meta, const void* q, const int32_t* n_new,
@@ -822,7 +910,7 @@ extern "C" int twilight_kv4_attention(const twilight_kv_t* kv, const void* vq_po
   a.out = (uint2*)out; a.lse = lse;
   const size_t slots = part_slots4(d, rows);
   a.ws_plan = (int32_t*)ws;
-  a.ws_ml = (float2*)((char*)ws + align256n((size_t)d.batch * 8));
+  a.ws_ml = (float2*)((char*)ws + align256n((size_t)(d.batch + 1) * 8));
   a.ws_acc = (float*)((char*)a.ws_ml + align256n(slots * M * 8));
   a.batch = d.batch; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.G; a.lgG = __builtin_ctz(d.G); a.max_pages = d.max_pages; a.max_new = max_new;
   a.window = std::min(window, most); a.sinks = std::min(num_sinks, most); a.pool_pages = (unsigned)d.pool_pages;

@@ -217,25 +217,10 @@ __device__ __forceinline__ bool whole_item(const A& a, Item* it) {
 
 // log-sum-exp of a row; -inf where it saw nothing (l = 0 and no NaN: a row with one has to show it)
 __device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * kLn2n; }
-// The parts of cut lists joined.  A row (new token, head) is folded by LANES half waves of 32 lanes x 4 dims: two (a wave; four
-// rows to a workgroup) where there are many rows, eight (a workgroup) where few rows have many parts each and the wait
-// for one part after the other is what counts: 256 rows of 32 parts 4.0 us with eight, 8.3 us with two.  Whole calls, two / eight:
-//   one sequence of 4096     rows  32: 11.9 / 11.0  256: 14.0 / 13.4   512: 15.7 / 15.4  1024: 16.6 / 16.9  4096: 28.3 / 29.8
-//   4 sequences of 8192      rows 512: 30.8 / 31.0 1024: 32.5 / 33.2  2048: 36.6 / 37.2  8192: 60 / 64     16384: 93 / 100
-//   16 sequences of 4096     rows 512: 49.2 / 49.5 2048: 49.5 / 50.8  8192: 57.5 / 61   16384: 70 / 77
-template <int M, int LANES, class A>
-__device__ __forceinline__ void join_parts(const A& a) {
-  constexpr int ROWS = 8 / LANES;
+// `chunks` parts of a row, part c at row at(c) of the workspace, joined by this workgroup's LANES half waves, and the row written where it is live.
+template <int LANES, class A, class F>
+__device__ __forceinline__ void fold_parts(const A& a, int b, int tok, int head, bool live, int chunks, F at) {
   const int lane = threadIdx.x & 63, dl = lane & 31, part = (threadIdx.x >> 5) % LANES;
-  const int b = blockIdx.y, idx = (int)(blockIdx.x * ROWS + threadIdx.x / (32 * LANES));
-  const int n = seq_new(a, b);
-  const int tok = idx / a.Hq, head = idx - tok * a.Hq;
-  const int chunks = a.ws_plan[2 * b];
-  if (chunks <= 1) return;                       // written by the attention kernel itself
-  const bool live = tok < n;
-  const int blocks = (n * a.G + M - 1) / M, row = min(tok, n - 1) * a.G + (head & (a.G - 1));
-  const long long step = (long long)blocks * a.Hkv * M;
-  long long at = ((long long)a.ws_plan[2 * b + 1] + (row / M) * a.Hkv + (head >> a.lgG)) * M + row % M + part * step;
   float m = kLow, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   auto join = [&](float m2, float l2, const float4& v) {
@@ -245,9 +230,10 @@ __device__ __forceinline__ void join_parts(const A& a) {
     m = mn;
   };
 #pragma unroll 4
-  for (int c = part; c < chunks; c += LANES, at += LANES * step) {
-    const float2 ml = a.ws_ml[at];
-    join(ml.x, ml.y, ((const float4*)a.ws_acc)[at * 32 + dl]);
+  for (int c = part; c < chunks; c += LANES) {
+    const long long r = at(c);
+    const float2 ml = a.ws_ml[r];
+    join(ml.x, ml.y, ((const float4*)a.ws_acc)[r * 32 + dl]);
   }
   join(__shfl_xor(m, 32), __shfl_xor(l, 32), make_float4(__shfl_xor(o.x, 32), __shfl_xor(o.y, 32), __shfl_xor(o.z, 32), __shfl_xor(o.w, 32)));
   if (LANES == 8) {
@@ -269,6 +255,27 @@ __device__ __forceinline__ void join_parts(const A& a) {
   a.out[qrow * 32 + dl] = w.v;
   if (a.lse && lane == 0) a.lse[qrow] = row_lse(m, l);
 }
+
+// The parts of cut lists joined.  A row (new token, head) is folded by LANES half waves of 32 lanes x 4 dims: two (a wave; four
+// rows to a workgroup) where there are many rows, eight (a workgroup) where few rows have many parts each and the wait
+// for one part after the other is what counts: 256 rows of 32 parts 4.0 us with eight, 8.3 us with two.  Whole calls, two / eight:
+//   one sequence of 4096     rows  32: 11.9 / 11.0  256: 14.0 / 13.4   512: 15.7 / 15.4  1024: 16.6 / 16.9  4096: 28.3 / 29.8
+//   4 sequences of 8192      rows 512: 30.8 / 31.0 1024: 32.5 / 33.2  2048: 36.6 / 37.2  8192: 60 / 64     16384: 93 / 100
+//   16 sequences of 4096     rows 512: 49.2 / 49.5 2048: 49.5 / 50.8  8192: 57.5 / 61   16384: 70 / 77
+template <int M, int LANES, class A>
+__device__ __forceinline__ void join_parts(const A& a) {
+  constexpr int ROWS = 8 / LANES;
+  const int b = blockIdx.y, idx = (int)(blockIdx.x * ROWS + threadIdx.x / (32 * LANES));
+  const int n = seq_new(a, b);
+  const int tok = idx / a.Hq, head = idx - tok * a.Hq;
+  const int chunks = a.ws_plan[2 * b];
+  if (chunks <= 1) return;                       // written by the attention kernel itself
+  const int blocks = (n * a.G + M - 1) / M, row = min(tok, n - 1) * a.G + (head & (a.G - 1));
+  const long long step = (long long)blocks * a.Hkv * M;
+  const long long at = ((long long)a.ws_plan[2 * b + 1] + (row / M) * a.Hkv + (head >> a.lgG)) * M + row % M;
+  fold_parts<LANES>(a, b, tok, head, tok < n, chunks, [=](int c) { return at + c * step; });
+}
+
 size_t align256n(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace

@@ -76,10 +76,10 @@ def test_choice_of_tokens_refuses(T):
 
 def test_workspaces(T):
     size = T.twilight_workspace_bytes
-    # single tokens: a part of 16 rows per 256 tokens of a list at most
-    parts = 64 * (2 * 8) * 16
-    assert parts * 520 <= size(T.TW_WS_KV4, _kv(T, max_pages=1024), 1) <= parts * 520 + 1024
-    assert size(T.TW_WS_KV4, _kv(T, max_pages=1 << 20), 1) <= 256 * 8 * 16 * 520 + 1024       # no more than the chip takes
+    # single tokens: two places of 16 rows per 256 tokens of a list, as far as the chip has workgroups
+    parts = 2 * 8 * (2 * 8) * 16
+    assert parts * 520 <= size(T.TW_WS_KV4, _kv(T, max_pages=128), 1) <= parts * 520 + 1024
+    assert size(T.TW_WS_KV4, _kv(T, max_pages=1 << 20), 1) == size(T.TW_WS_KV4, _kv(T, max_pages=1 << 22), 1) <= 2 * 512 * 16 * 520 + 1024
     assert size(T.TW_WS_KV4, _kv(T), 0) == size(T.TW_WS_KV4, _kv(T), -3) == 0
     assert size(T.TW_WS_KEEP, _kv(T, max_pages=2048)) == 256
     assert 2 * 5 * 5122 * 4 <= size(T.TW_WS_KEEP, _kv(T, max_pages=2049)) <= 2 * 5 * 5122 * 4 + 256
@@ -139,6 +139,6 @@ def test_kernels_spill_nothing(kernels):  # noqa: F811
     new = {n: k for n, k in kernels.items() if n.startswith(("kv4_", "attention_mass", "keep_"))}
     assert len(new) >= 18
     for n, k in new.items():
-        assert k[".vgpr_spill_count"] <= {"kv4_attention_kernel<2, true>": 24, "kv4_wide_kernel<4, 1, true>": 4}.get(n, 0), n
+        assert k[".vgpr_spill_count"] <= {"kv4_attention_kernel<2, true>": 20, "kv4_wide_kernel<4, 1, true>": 6}.get(n, 0), n
         if n.startswith(("kv4_attention_kernel", "kv4_wide_kernel")):
             assert _fits(k, 2) and k[".group_segment_fixed_size"] * 2 <= 160 * 1024, (n, k[".vgpr_count"])

@@ -4,10 +4,11 @@
 // N new tokens, as in new_tokens.hip; a workgroup takes M = 16 * RT of them, its four waves walk tiles of 64 tokens (4 pages)
 // each on their own, and their states are merged at the end.
 //
-//   scores   S = sum_g s_g T_g + z_g Q_g over the four groups g, T_g = sum_d q_d c_d, Q_g = sum_d q_d.  T_g is one
-//            v_mfma_f32_16x16x32_bf16 (a group is its contraction): A = 16 tokens' codes, as bf16 128 + c (one `and`, one `or` on two
-//            codes of a word; 8 bits hold them exactly), B = 16 rows of q, C = -128 Q_g, which takes the 128 off again.  Codes and q are
-//            exact, so a score is as good as one of fp32 products (the 128 costs 4 of the 24 bits).
+//   scores   S = sum_g s_g T_g + (z_g - 128 s_g) Q_g over the four groups g, T_g = sum_d q_d (128 + c_d), Q_g = sum_d q_d.  T_g is one
+//            v_mfma_f32_16x16x32_bf16 (a group is its contraction): A = 16 tokens' codes, as bf16 128 + c (bits put in place: 8 bits hold
+//            them exactly), B = 16 rows of q.  What the zeros and the 128 add is one more, for all groups: z - 128 s and Q_g in three bf16
+//            parts each (24 bits), of whose products those that count in fp32 are six, 24 of the 32 terms.  Codes and q are exact, so a
+//            score is as good as one of fp32 products (the 128 costs 4 of the 24 bits).
 //   weights  P = exp2(S log2(e)/sqrt(128) - m), fp32; their sum is of the unrounded ones.  For the product with V they are fp16, with m
 //            kept 11 below the row's maximum's logarithm: the largest is 2^11 to 2^15, and one of 2^-25 of it still has 11 bits.
 //   output   O^T += V^T P^T, v_mfma_f32_16x16x32_f16 with V^ = fma(c, s, z) in fp16 (2^-11 of itself at most; c exact: 1024 + c or 64 + c
@@ -31,7 +32,8 @@ typedef int tw_v2i __attribute__((ext_vector_type(2)));
 #define TW_GLB __attribute__((address_space(1)))
 
 constexpr int WAVES = 4;
-constexpr int BUF = 4096 + 1024;                 // of a wave: V's codes and K's (s, z) of 64 tokens
+// of a wave's LDS: V's codes of 64 tokens, twice; and what is made of their (s, z)
+constexpr int BUF = 4096, MADE = 1024 + 2048 + 512, MADE_Z = 1024, MADE_S = 3072;
 constexpr int TILE_BYTES4 = 64 * 160;            // what a wave's tile has in memory
 constexpr float kLift = 11.f;                    // log2 of the weight of a row's maximum when m is set to it
 constexpr float kGrowth4 = 4.f;                  // how far (in powers of 2) scores may pass it before m follows: weights stay below 2^16
@@ -158,15 +160,22 @@ __device__ __forceinline__ void join_shares(const A& a) {
 // the lowest x of 16 bits
 __device__ __forceinline__ uint32_t low16(int x) { return x <= 0 ? 0u : x >= 16 ? 0xFFFFu : (1u << x) - 1u; }
 
+// x as the sum of three bf16 numbers.
+struct Parts { float x, y, z; };
+__device__ __forceinline__ Parts parts_of(float v) {
+  const float x = (float)(__bf16)v, y = (float)(__bf16)(v - x);
+  return {x, y, v - x - y};
+}
+
 // The 8 codes of a word times s plus z in fp16; element 2 e + i is nibble e + 4 i.
 __device__ __forceinline__ tw_f16x8 codes_f16(uint32_t w, const uint4& s, const uint4& z) {
   union { uint32_t u; tw_f16x2 h; } c[4], sc, ze;
   union { tw_f16x2 h[4]; tw_f16x8 v; } x;
   const uint32_t up = w >> 8;
-  c[0].u = (w & 0x000F000Fu) | 0x64006400u;      // 1024 + c
-  c[1].u = (w & 0x00F000F0u) | 0x54005400u;      // 64 + c
-  c[2].u = (up & 0x000F000Fu) | 0x64006400u;
-  c[3].u = (up & 0x00F000F0u) | 0x54005400u;
+  c[0].u = tw_and_or(w, 0x000F000Fu, 0x64006400u);                            // 1024 + c
+  c[1].u = tw_and_or(w, 0x00F000F0u, 0x54005400u);                            // 64 + c
+  c[2].u = tw_and_or(up, 0x000F000Fu, 0x64006400u);
+  c[3].u = tw_and_or(up, 0x00F000F0u, 0x54005400u);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const tw_f16x2 lift = e & 1 ? tw_f16x2{(_Float16)64.f, (_Float16)64.f} : tw_f16x2{(_Float16)1024.f, (_Float16)1024.f};
@@ -180,7 +189,7 @@ __device__ __forceinline__ tw_f16x8 codes_f16(uint32_t w, const uint4& s, const 
 // One item: a chunk of a list.
 template <int RT, bool SPLIT>
 __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, unsigned char (&buf0)[WAVES * BUF], unsigned char (&buf1)[WAVES * BUF],
-                                            unsigned char (&vms)[WAVES * 1024], int lane, int wave) {
+                                            unsigned char (&made)[WAVES * MADE], int lane, int wave) {
   constexpr int M = 16 * RT;
   const int r16 = lane & 15, jq = lane >> 4;
   const int b = __builtin_amdgcn_readfirstlane(it.b), rb = __builtin_amdgcn_readfirstlane(it.rb), h = __builtin_amdgcn_readfirstlane(it.h);
@@ -196,8 +205,7 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, u
   const bool whole = !SPLIT || it.to - it.from == it.tiles;
 
   int pos[RT];
-  tw_bf16x8 qf[RT][4];
-  float qs[RT][4];
+  tw_bf16x8 qf[RT][4], qz[RT];                   // qz: Q_g's parts; quarters 0 and 1 the first and second twice, 2 the third and the first, 3 none
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     pos[rt] = ctx + (row_of(rt) >> a.lgG);
@@ -209,8 +217,10 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, u
       tw_unpack8(x, f);
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += f[i];
-      qs[rt][g] = tw_quarters_sum(sum);
       qf[rt][g] = tw_q_like_codes(x);
+      const Parts q = parts_of(tw_quarters_sum(sum));
+      qz[rt][2 * g] = (__bf16)(jq == 0 ? q.x : jq == 1 ? q.y : jq == 2 ? q.z : 0.f);
+      qz[rt][2 * g + 1] = (__bf16)(jq == 0 ? q.x : jq == 1 ? q.y : jq == 2 ? q.x : 0.f);
     }
   }
 
@@ -241,18 +251,18 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, u
     return p & 2 ? hi : lo;
   };
   auto issue_lds = [&](unsigned char* buf, const Slots& x) {
-    const int tok = one_of(x, jq) + r16;
-    __builtin_amdgcn_global_load_lds((const TW_GLB unsigned int*)(a.k_meta + tok), (TW_LDS unsigned int*)(buf + 4096), 16, 0, 0);
 #pragma unroll
     for (int p = 0; p < 4; ++p)
       __builtin_amdgcn_global_load_lds((const TW_GLB unsigned int*)(a.v_codes + ((long long)(x.s[p] + tok4) * 4 + piece4)), (TW_LDS unsigned int*)(buf + 1024 * p), 16, 0, 0);
   };
-  uint4 kc[4], vm;                               // K's codes and V's (s, z) of a tile on its way
+  uint4 kc[4], km, vm;                           // K's codes and both (s, z) of a tile on its way
   auto issue_regs = [&](const Slots& x) {
     const uint4* kp = a.k_codes + ((long long)(one_of(x, r16 >> 2) + (r16 & 3)) * 4 + jq);
 #pragma unroll
     for (int i = 0; i < 4; ++i) kc[i] = kp[16 * i];
-    vm = a.v_meta[one_of(x, jq) + r16];
+    const int tok = one_of(x, jq) + r16;
+    km = a.k_meta[tok];
+    vm = a.v_meta[tok];
   };
 
   tw_v4f o[RT][8];
@@ -268,7 +278,9 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, u
   auto scale_of = [](float m) -> float { return __builtin_fabsf(m) < kFar ? kScaleLog2 : 0.25f; };
   auto m_log2 = [](float m) -> float { return __builtin_fabsf(m) < kFar ? m : m * kScaleLog2 * 4.f; };
 
-  unsigned char* const vm_lds = vms + wave * 1024;
+  // What is made of a tile's (s, z), this lane's token r16 of its quarter's page.  V's: s and z of 8 tokens in the order of codes_f16, by
+  // (page, group, 8 tokens).  K's: z - 128 s in parts, the first and second of all groups, then the first and third; the scales.
+  unsigned char* const vm_lds = made + wave * MADE;
   const unsigned vm_wr = (unsigned)(jq * 256 + (r16 >> 3) * 32 + ((r16 & 3) * 2 + ((r16 >> 2) & 1)) * 2);
   // `here`: this quarter's page is mapped; `more`: tile u + 1, at x, follows, whose registers are asked for as soon as tile u's are free
   auto compute = [&](const unsigned char* buf, int u, bool here, bool more, const Slots& x) {
@@ -281,15 +293,24 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, u
       all &= vis[rt];
     }
     const bool full = __all(all == 0xFFFFu);
-    {                                            // V's (s, z), 0 for what is no token, whose weight is 0
-      const bool token = here && t0 + r16 < len;
-      const uint32_t w[4] = {vm.x, vm.y, vm.z, vm.w};
+    {
+      const bool token = here && t0 + r16 < len;             // (what is none: 0, whose weight is 0)
+      const uint32_t w[4] = {vm.x, vm.y, vm.z, vm.w}, y[4] = {km.x, km.y, km.z, km.w};
+      uint32_t z12[4], z13[4];
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const uint32_t sz = token ? w[g] : 0u;
         *(unsigned short*)(vm_lds + vm_wr + 64 * g) = (unsigned short)sz;
         *(unsigned short*)(vm_lds + vm_wr + 64 * g + 16) = (unsigned short)(sz >> 16);
+        const uint32_t k = token ? y[g] : 0u;
+        const Parts z = parts_of(__builtin_fmaf(tw_half_lo(k), -128.f, tw_half_hi(k)));
+        union { __bf16 e[2]; uint32_t u; } a12, a13;
+        a12.e[0] = a13.e[0] = (__bf16)z.x; a12.e[1] = (__bf16)z.y; a13.e[1] = (__bf16)z.z;
+        z12[g] = a12.u; z13[g] = a13.u;
       }
+      *(uint4*)(vm_lds + MADE_Z + lane * 32) = make_uint4(z12[0], z12[1], z12[2], z12[3]);
+      *(uint4*)(vm_lds + MADE_Z + lane * 32 + 16) = make_uint4(z13[0], z13[1], z13[2], z13[3]);
+      *(uint2*)(vm_lds + MADE_S + lane * 8) = make_uint2(__builtin_amdgcn_perm(y[1], y[0], 0x05040100u), __builtin_amdgcn_perm(y[3], y[2], 0x05040100u));
     }
     tw_v4f s[RT][4];
 #pragma unroll
@@ -297,35 +318,24 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, u
       __builtin_amdgcn_sched_barrier(0);         // (the compiler would gather all steps' operands, and spill)
       tw_transpose_quarters(kc[st]);
       const tw_bf16x8 kf[4] = {tw_codes_bf16(kc[st].x), tw_codes_bf16(kc[st].y), tw_codes_bf16(kc[st].z), tw_codes_bf16(kc[st].w)};
-      uint4 km[4];
+      const tw_bf16x8 zf = *(const tw_bf16x8*)(vm_lds + MADE_Z + ((r16 >> 2) * 16 + 4 * st + (r16 & 3)) * 32 + (jq == 2 ? 16 : 0));
+      uint2 sc[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) km[i] = *(const uint4*)(buf + 4096 + (jq * 16 + 4 * st + i) * 16);
-      float zr[4][4];                            // z (RT = 1), or z - 128 s: with several row tiles there are no registers for their C operands
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t w[4] = {km[i].x, km[i].y, km[i].z, km[i].w};
-#pragma unroll
-        for (int g = 0; g < 4; ++g) zr[i][g] = RT == 1 ? tw_half_hi(w[g]) : __builtin_fmaf(tw_half_lo(w[g]), -128.f, tw_half_hi(w[g]));
-      }
+      for (int i = 0; i < 4; ++i) sc[i] = *(const uint2*)(vm_lds + MADE_S + (jq * 16 + 4 * st + i) * 8);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        tw_v4f t[4];
+        tw_v4f t[4], y = {0.f, 0.f, 0.f, 0.f};
+        y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(zf, qz[rt], y, 0, 0, 0);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const float c = RT == 1 ? -128.f * qs[rt][g] : 0.f;
-          t[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[g], qf[rt][g], tw_v4f{c, c, c, c}, 0, 0, 0);
-        }
+        for (int g = 0; g < 4; ++g) t[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[g], qf[rt][g], tw_v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float y = zr[i][0] * qs[rt][0];
-          y = __builtin_fmaf(zr[i][1], qs[rt][1], y);
-          y = __builtin_fmaf(zr[i][2], qs[rt][2], y);
-          y = __builtin_fmaf(zr[i][3], qs[rt][3], y);
-          y = __builtin_fmaf(tw_half_lo(km[i].x), t[0][i], y);
-          y = __builtin_fmaf(tw_half_lo(km[i].y), t[1][i], y);
-          y = __builtin_fmaf(tw_half_lo(km[i].z), t[2][i], y);
-          s[rt][st][i] = __builtin_fmaf(tw_half_lo(km[i].w), t[3][i], y);
-        }
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = g & 2 ? sc[i].y : sc[i].x;
+            y[i] = __builtin_fmaf(g & 1 ? tw_half_hi(w) : tw_half_lo(w), t[g][i], y[i]);
+          }
+        s[rt][st] = y;
         asm volatile("" : "+v"(s[rt][st]));      // here and now: sunk behind the branch below, all steps' products would wait in registers
       }
     }
@@ -428,16 +438,17 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, u
     const float mw = m_log2(m[rt]), lw = tw_quarters_sum(l[rt]);
     __syncthreads();                             // tiles, or the row tile before, have been read
     float* part = (float*)((wave & 2 ? buf1 : buf0) + (wave & 1) * 8192);
+    static_assert(WAVES * BUF >= 2 * 8192, "two waves' parts to a buffer");
 #pragma unroll
     for (int d = 0; d < 8; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i) part[(d * 4 + i) * 64 + lane] = o[rt][d][i];
-    if (jq == 0) ((float2*)vms)[wave * 16 + r16] = make_float2(mw, lw);
+    if (jq == 0) ((float2*)made)[wave * 16 + r16] = make_float2(mw, lw);
     __syncthreads();
     float2 ml[WAVES];
     float mn = kLow, ls = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) { ml[w] = ((const float2*)vms)[w * 16 + r16]; mn = fmaxf(mn, ml[w].x); }
+    for (int w = 0; w < WAVES; ++w) { ml[w] = ((const float2*)made)[w * 16 + r16]; mn = fmaxf(mn, ml[w].x); }
     float al[WAVES], sum[2][4];
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) { al[w] = __builtin_amdgcn_exp2f(ml[w].x - mn); ls += ml[w].y * al[w]; }
@@ -483,14 +494,14 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(Kv4Args a) {
   constexpr int M = 16 * RT;
   __shared__ __align__(1024) unsigned char buf0[WAVES * BUF];
   __shared__ __align__(1024) unsigned char buf1[WAVES * BUF];
-  __shared__ __align__(1024) unsigned char vms[WAVES * 1024];
+  __shared__ __align__(1024) unsigned char made[WAVES * MADE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   if (!SPLIT) {
     Piece it;
-    if (whole_piece<M>(a, &it)) attend_item<RT, SPLIT>(a, it, buf0, buf1, vms, lane, wave);
+    if (whole_piece<M>(a, &it)) attend_item<RT, SPLIT>(a, it, buf0, buf1, made, lane, wave);
     return;
   }
-  for_pieces<M>(a, lane, [&](const Piece& it, int ln) { attend_item<RT, SPLIT>(a, it, buf0, buf1, vms, ln, wave); });
+  for_pieces<M>(a, lane, [&](const Piece& it, int ln) { attend_item<RT, SPLIT>(a, it, buf0, buf1, made, ln, wave); });
 }
 
 // ------------------------------------------------------------------------------------------------------ many rows
@@ -841,7 +852,7 @@ template <int M, int LANES>
 __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Args a) { join_shares<M, LANES>(a); }
 
 // ---------------------------------------------------------------- host side
-int rows_per_block4(long long rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+int rows_per_block4(long long rows) { return rows <= 16 ? 16 : rows <= 64 ? 32 : 128; }
 
 // Lists that cannot be long are not cut, nor are the row blocks of prompts that fill the chip by themselves, but where single tokens may
 // stand beside a chunk (as in new_tokens.hip).  Tiles of 256 tokens (up to 32 rows) or 64.

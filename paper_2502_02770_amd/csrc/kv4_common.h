@@ -30,11 +30,15 @@ __device__ __forceinline__ void tw_transpose_quarters(uint4& x) {
   x = make_uint4(c[0], c[1], d[0], d[1]);
 }
 
+// (x & mask) | bits in one instruction.  (Written as two operations they stay two, with a literal each; and not as inline assembly, which the
+// compiler does not count where a matrix instruction has still to read or write a register.)
+__device__ __forceinline__ uint32_t tw_and_or(uint32_t x, uint32_t mask, uint32_t bits) { return (uint32_t)__builtin_amdgcn_bitop3_b32((int)x, (int)mask, (int)bits, 0xEA); }
+
 // The 8 codes of a word as 128 + c in bf16, which holds them exactly; dims in the order 0 2 4 6 1 3 5 7.  A row of q likewise.
 __device__ __forceinline__ tw_bf16x8 tw_codes_bf16(uint32_t w) {
   union { uint32_t u[4]; tw_bf16x8 v; } x;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x.u[i] = ((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u;
+  for (int i = 0; i < 4; ++i) x.u[i] = tw_and_or(w >> (4 * i), 0x000F000Fu, 0x43004300u);
   return x.v;
 }
 __device__ __forceinline__ tw_bf16x8 tw_as_bf16(const uint4& x) { union { uint4 u; tw_bf16x8 v; } y; y.u = x; return y.v; }

@@ -34,13 +34,12 @@ typedef int tw_v2i __attribute__((ext_vector_type(2)));
 constexpr int WAVES = 4;
 // of a wave's LDS: V's codes of 64 tokens, twice; and what is made of their (s, z)
 constexpr int BUF = 4096, MADE = 1024 + 2048 + 512, MADE_Z = 1024, MADE_S = 3072;
-constexpr int TILE_BYTES4 = 64 * 160;            // what a wave's tile has in memory
 constexpr float kLift = 11.f;                    // log2 of the weight of a row's maximum when m is set to it
 constexpr float kGrowth4 = 4.f;                  // how far (in powers of 2) scores may pass it before m follows: weights stay below 2^16
 
 struct Kv4Args {
   // a tile of the plan: the 16 pages that the four waves take together
-  static constexpr int TILE_PAGES = 16, MIN_TILES = 1, STREAM_TILES = (96 << 20) / (WAVES * TILE_BYTES4);
+  static constexpr int TILE_PAGES = 16, MIN_TILES = 1, PAD = 1;
   const uint4* q;
   const uint4* k_codes;
   const uint4* k_meta;
@@ -69,26 +68,36 @@ struct Piece {
   int from, to, tiles;                           // of the list's tiles
   int slot;                                      // its place in the workspace, if the list is cut
 };
+// Where a workgroup has many tiles, a list counts PAD more than it has, for what a piece costs beside its tiles (queries, states merged: 4 us).
 struct Shares {
-  uint32_t per, total;                           // tiles of a workgroup, of all lists
+  uint32_t each, more, pad, all;                 // tiles of a workgroup (the first `more` have one more), and together
+  __device__ __forceinline__ uint32_t begin(uint32_t w) const { return w * each + min(w, more); }
+  __device__ __forceinline__ uint32_t owner(uint32_t t) const {
+    const uint32_t x = more * (each + 1u);
+    return t < x ? quotient(t, each + 1u) : more + quotient(t - x, each);
+  }
 };
 template <int M, class A>
 __device__ __forceinline__ Shares shares_of(const A& a, int lane) {
-  uint32_t total = 0;
+  uint32_t total = 0, lists = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const Seq q = seq_of<MODE_WINDOW, M>(a, b0 + lane);
     total += (uint32_t)__builtin_amdgcn_readlane((int)tw_wave_scan_u32((uint32_t)q.lists * (uint32_t)q.tiles), 63);
+    lists += (uint32_t)__builtin_amdgcn_readlane((int)tw_wave_scan_u32((uint32_t)q.lists), 63);
   }
-  const uint32_t wgs = gridDim.x;
-  return {max((uint32_t)A::MIN_TILES, (total + wgs - 1u) / wgs), total};
+  const uint32_t pad = total / 8u > gridDim.x * (uint32_t)A::MIN_TILES ? A::PAD : 0;
+  const uint32_t wgs = max(1u, min(gridDim.x, total / (uint32_t)A::MIN_TILES));
+  const uint32_t all = total + pad * lists, each = all / wgs;
+  return {each, all - each * wgs, pad, all};
 }
 // The piece that begins with tile `pos`, the workgroup's first or a later one, of those before `end`; tells the launch that joins the parts where lists begin.
 template <int M, class A>
-__device__ __forceinline__ void piece_at(const A& a, int lane, uint32_t per, uint32_t pos, uint32_t end, bool tell, Piece* it) {
+__device__ __forceinline__ void piece_at(const A& a, int lane, uint32_t pad, bool first, uint32_t pos, uint32_t end, bool tell, Piece* it) {
   uint32_t tiles = 0;
   bool found = false;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    const Seq q = seq_of<MODE_WINDOW, M>(a, b0 + lane);
+    Seq q = seq_of<MODE_WINDOW, M>(a, b0 + lane);
+    q.tiles += (int)pad;
     const uint32_t mine = (uint32_t)q.lists * (uint32_t)q.tiles;
     const uint32_t te = tw_wave_scan_u32(mine);
     if (tell && b0 + lane < a.batch) ((int2*)a.ws_plan)[1 + b0 + lane] = make_int2((int)(tiles + te - mine), q.tiles);
@@ -100,12 +109,12 @@ __device__ __forceinline__ void piece_at(const A& a, int lane, uint32_t per, uin
       it->len = __builtin_amdgcn_readlane(q.len, l);
       it->off = __builtin_amdgcn_readlane(q.off, l);
       it->tiles = __builtin_amdgcn_readlane(q.tiles, l);
-      const uint32_t in = pos - (tiles + (uint32_t)__builtin_amdgcn_readlane((int)(te - mine), l)), k = in / (uint32_t)it->tiles;
+      const uint32_t in = pos - (tiles + (uint32_t)__builtin_amdgcn_readlane((int)(te - mine), l)), k = quotient(in, (uint32_t)it->tiles);
       it->from = (int)(in - k * (uint32_t)it->tiles);
       it->to = (int)min((uint32_t)it->tiles, (uint32_t)it->from + (end - pos));
-      it->rb = (int)(k / (uint32_t)a.Hkv);
+      it->rb = (int)quotient(k, (uint32_t)a.Hkv);
       it->h = (int)(k - (uint32_t)it->rb * (uint32_t)a.Hkv);
-      it->slot = 2 * (int)blockIdx.x + (pos == blockIdx.x * per ? 0 : 1);
+      it->slot = 2 * (int)blockIdx.x + (first ? 0 : 1);
       found = true;
       if (!tell) return;
     }
@@ -125,14 +134,12 @@ __device__ __forceinline__ bool whole_piece(const A& a, Piece* it) {
 template <int M, class A, class F>
 __device__ __forceinline__ void for_pieces(const A& a, int lane, F attend) {
   const Shares s = shares_of<M>(a, lane);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *(int2*)a.ws_plan = make_int2((int)s.per, 0);
-  const unsigned long long begin = (unsigned long long)blockIdx.x * s.per;
-  uint32_t pos = (uint32_t)min(begin, (unsigned long long)s.total);
-  const uint32_t end = (uint32_t)min(begin + s.per, (unsigned long long)s.total);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *(int2*)a.ws_plan = make_int2((int)s.each, (int)s.more);
   Piece it;
-  if (blockIdx.x == 0 && s.total == 0) piece_at<M>(a, lane, s.per, 0, 0, threadIdx.x < 64, &it);
-  while (pos < end) {
-    piece_at<M>(a, lane, s.per, pos, end, pos == 0 && threadIdx.x < 64, &it);
+  uint32_t pos = s.begin(blockIdx.x);
+  const uint32_t end = min(s.all, s.begin(blockIdx.x + 1));    // (workgroups that are too many begin behind)
+  for (bool first = true; pos < end; first = false) {
+    piece_at<M>(a, lane, s.pad, first, pos, end, pos == 0 && threadIdx.x < 64, &it);
     int ln = lane;
     asm volatile("" : "+v"(ln));                 // what depends on the lane alone is worked out for every piece: held over them it would spill
     attend(it, ln);
@@ -147,13 +154,13 @@ __device__ __forceinline__ void join_shares(const A& a) {
   const int b = blockIdx.y, idx = (int)(blockIdx.x * ROWS + threadIdx.x / (32 * LANES));
   const int n = seq_new(a, b), tok = idx / a.Hq, head = idx - tok * a.Hq;
   if (tok >= n) return;
-  const uint32_t per = (uint32_t)a.ws_plan[0];
+  const Shares s = {(uint32_t)a.ws_plan[0], (uint32_t)a.ws_plan[1], 0u, 0u};
   const int2 p = ((const int2*)a.ws_plan)[1 + b];            // the sequence's first tile, tiles of a list
   const int row = tok * a.G + (head & (a.G - 1));
   const uint32_t k = (uint32_t)((row / M) * a.Hkv + (head >> a.lgG)), t0 = (uint32_t)p.x + k * (uint32_t)p.y;
-  const uint32_t first = t0 / per, last = (t0 + (uint32_t)p.y - 1u) / per;
+  const uint32_t first = s.owner(t0), last = s.owner(t0 + (uint32_t)p.y - 1u);
   if (first == last) return;                     // written by the attention kernel itself
-  const int late = t0 == first * per ? 0 : 1;    // the first part is its workgroup's last
+  const int late = t0 == s.begin(first) ? 0 : 1;    // the first part is its workgroup's last
   fold_parts<LANES>(a, b, tok, head, true, (int)(last - first + 1u), [=](int c) { return (long long)(2 * ((int)first + c) + (c ? 0 : late)) * M + row % M; });
 }
 
@@ -419,6 +426,9 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, u
     issue_lds(mine0, x);
     issue_regs(x);
     for (int u = u0; u < u1; u += 2) {           // (a wave's buffers are its own: nothing to wait for but its own loads)
+      // the older of two workgroups on a CU would be served first, and leave the other alone at the end: they take turns
+      if ((blockIdx.x >= gridDim.x / 2) == ((u - u0) % 4 < 2)) __builtin_amdgcn_s_setprio(1);
+      else __builtin_amdgcn_s_setprio(0);
       arrived();
       bool here = mapped >> (4 * (u - base) + jq) & 1, more = u + 1 < u1;
       if (more) { x = slots_of(u + 1); issue_lds(mine1, x); }
@@ -511,7 +521,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(Kv4Args a) {
 // one fma per score and group; what the zeros add, sum_g z_g Q_g, is two more products for all groups: z (11 bits) in two bf16 parts, Q_g
 // in three.
 struct Kv4WideArgs : Kv4Args {
-  static constexpr int TILE_PAGES = 4, MIN_TILES = 2, STREAM_TILES = 1 << 30;
+  static constexpr int TILE_PAGES = 4, MIN_TILES = 2, PAD = 3;
 };
 constexpr int WIDE_V = 64 * 256, WIDE_Z = 2 * WIDE_V, WIDE_S = WIDE_Z + 64 * 16, WIDE_BUF = WIDE_S + 64 * 8;
 
@@ -871,7 +881,7 @@ int launch_kv4(const A& a, Whole whole, Cut cut, hipStream_t s) {
   const long long pages = std::min<long long>(a.max_pages, ((long long)a.sinks + TW_PAGE - 1) / TW_PAGE + ((long long)a.window + M / a.G + TW_PAGE - 2) / TW_PAGE + 1);
   const long long longest = (pages + A::TILE_PAGES - 1) / A::TILE_PAGES;        // tiles that a list can have
   tw_prof_before(TW_K_KV4_ATTENTION, s);
-  if (!cut_lists4<A>(a.n_new != nullptr, a.rb_max, lists, longest) || rows >= (1ll << 26) || lists * longest >= (1ll << 32)) {
+  if (!cut_lists4<A>(a.n_new != nullptr, a.rb_max, lists, longest) || rows >= (1ll << 26) || lists * (longest + A::PAD) >= (1ll << 32)) {
     TW_LAUNCH(whole, dim3((unsigned)lists), dim3(256), 0, s, a);
     return tw_prof_after(s);
   }

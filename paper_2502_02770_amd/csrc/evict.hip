@@ -11,10 +11,10 @@ constexpr float kScaleLog2 = 0.08838834764831845f * 1.4426950408889634f;   // lo
 // ------------------------------------------------------------------------------------------------------- accumulated weights
 // mass[t] = decay mass[t] + sum over new tokens i and query heads of exp(q.K_t / sqrt(128) - lse_i): K once, nothing else of the cache.
 //
-// A workgroup has PT pages of a sequence, its four waves the KV heads in turn; a wave holds its head's K of those pages as
-// matrix operands (for codes 128 + c in bf16, as in kv4_attention.hip) and goes through the head's rows (query heads x new tokens) by 16:
-// S = Q K^T, v_mfma_f32_16x16x32_bf16, a lane has one token and four rows.  The waves' sums are added in their order, so that
-// the result does not depend on timing.
+// A workgroup has PT pages of a sequence, its four waves the KV heads in turn; a wave holds its head's K of those pages and goes through
+// the head's rows (query heads x new tokens) by 16: S = Q K^T, v_mfma_f32_16x16x32_bf16 (codes as 128 + c in bf16, as in
+// kv4_attention.hip), a lane has one token and four rows.  What comes next is asked for ahead: with up to 16 rows the next head's K and
+// queries, with more (MANY) the next rows.  The waves' sums are added in their order, so that the result does not depend on timing.
 struct MassArgs {
   const uint4* q;
   const float* lse;
@@ -31,8 +31,8 @@ struct MassArgs {
   float decay;
 };
 
-template <bool CODES, int PT>
-__global__ __launch_bounds__(256) void attention_mass_kernel(MassArgs a) {
+template <bool CODES, int PT, bool MANY>
+__global__ __launch_bounds__(256, 2) void attention_mass_kernel(MassArgs a) {
   __shared__ float red[4][16 * PT];
   const int b = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r16 = lane & 15, jq = lane >> 4;
   const int len = max(0, min(a.seq_lens[b], a.max_pages * TW_PAGE)), n = a.n_new ? max(0, min(a.n_new[b], a.max_new)) : a.max_new;
@@ -50,85 +50,163 @@ __global__ __launch_bounds__(256) void attention_mass_kernel(MassArgs a) {
 #pragma unroll
   for (int p = 0; p < PT; ++p) acc[p] = 0.f;
 
-  for (int h = wave; h < a.Hkv; h += 4) {
-    tw_bf16x8 kf[PT][4];
-    uint4 km[PT];
+  struct Keys { uint4 k[PT][CODES ? 1 : 4], m[CODES ? PT : 1]; };
+  auto load_keys = [&](int h) -> Keys {
+    Keys x;
 #pragma unroll
     for (int p = 0; p < PT; ++p) {
       const int row = max(slot[p], 0) + h * TW_PAGE + r16;
-      if (CODES) {
-        uint4 c = a.k[(long long)row * 4 + jq];
-        km[p] = a.meta[row];
-        tw_transpose_quarters(c);
-        kf[p][0] = tw_codes_bf16(c.x); kf[p][1] = tw_codes_bf16(c.y); kf[p][2] = tw_codes_bf16(c.z); kf[p][3] = tw_codes_bf16(c.w);
+      if constexpr (CODES) {
+        x.k[p][0] = a.k[(long long)row * 4 + jq];
+        x.m[p] = a.meta[row];
       } else {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) kf[p][g] = tw_as_bf16(tw_ld_stream(a.k + (long long)row * 16 + 4 * g + jq));
+        for (int g = 0; g < 4; ++g) x.k[p][g] = tw_ld_stream(a.k + (long long)row * 16 + 4 * g + jq);
       }
     }
-    for (int r0 = 0; r0 < rows; r0 += 16) {
-      // positions of the block's rows: does none of them see the pages?
-      const int p_lo = ctx + (r0 >> a.lgG), p_hi = ctx + ((min(r0 + 16, rows) - 1) >> a.lgG);
-      if (t0 > p_hi || (t0 + 16 * PT - 1 <= p_lo - a.window && t0 >= a.sinks)) continue;
-      const bool all = t0 + 16 * PT - 1 <= p_lo && (t0 > p_hi - a.window || t0 + 16 * PT <= a.sinks);
-      const int mine = min(r0 + r16, rows - 1);
-      const uint4* qp = a.q + ((long long)(off + (mine >> a.lgG)) * a.Hq + h * a.G + (mine & (a.G - 1))) * 16 + jq;
-      tw_bf16x8 qf[4];
+    return x;
+  };
+  struct Rows { uint4 q[4]; float lse[4]; };
+  auto load_rows = [&](int h, int r0) -> Rows {
+    Rows x;
+    const int mine = min(r0 + r16, rows - 1);
+    const uint4* qp = a.q + ((long long)(off + (mine >> a.lgG)) * a.Hq + h * a.G + (mine & (a.G - 1))) * 16 + jq;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const uint4 x = qp[4 * g];
-        qf[g] = CODES ? tw_q_like_codes(x) : tw_as_bf16(x);
-      }
-      float l2[4];                               // lse in powers of 2; infinite (weights of 0) where there is no row, or none with a weight
-      int pos[4];
+    for (int g = 0; g < 4; ++g) x.q[g] = qp[4 * g];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = r0 + 4 * jq + i;
-        float l = __builtin_inff();
-        if (r < rows) l = a.lse[(long long)(off + (r >> a.lgG)) * a.Hq + h * a.G + (r & (a.G - 1))];
-        l2[i] = __builtin_fabsf(l) < __builtin_inff() ? l * kLog2e : __builtin_inff();
-        pos[i] = ctx + (r >> a.lgG);
-      }
-      tw_v4f less[4];                            // -128 Q_g of the lane's rows: a product with a constant
-      if (CODES) {
-        tw_bf16x8 c;
+    for (int i = 0; i < 4; ++i) {
+      const int r = min(r0 + 4 * jq + i, rows - 1);
+      x.lse[i] = a.lse[(long long)(off + (r >> a.lgG)) * a.Hq + h * a.G + (r & (a.G - 1))];
+    }
+    return x;
+  };
+  auto operands = [&](const Keys& x, int p, tw_bf16x8 (&kf)[4]) {
+    uint4 c = x.k[p][0];
+    tw_transpose_quarters(c);
+    kf[0] = tw_codes_bf16(c.x); kf[1] = tw_codes_bf16(c.y); kf[2] = tw_codes_bf16(c.z); kf[3] = tw_codes_bf16(c.w);
+  };
+  // The rows r0 .. r0 + 15: do they see any of the pages, and their weights there
+  auto seen = [&](int r0) -> bool {
+    const int p_lo = ctx + (r0 >> a.lgG), p_hi = ctx + ((min(r0 + 16, rows) - 1) >> a.lgG);
+    return !(t0 > p_hi || (t0 + 16 * PT - 1 <= p_lo - a.window && t0 >= a.sinks));
+  };
+  auto add = [&](const Keys& x, const tw_bf16x8 (&held)[PT][4], const Rows& y, int r0) {
+    const int p_lo = ctx + (r0 >> a.lgG), p_hi = ctx + ((min(r0 + 16, rows) - 1) >> a.lgG);
+    const bool all = t0 + 16 * PT - 1 <= p_lo && (t0 > p_hi - a.window || t0 + 16 * PT <= a.sinks);
+    tw_bf16x8 qf[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = (__bf16)-128.f;
+    for (int g = 0; g < 4; ++g) qf[g] = CODES ? tw_q_like_codes(y.q[g]) : tw_as_bf16(y.q[g]);
+    float l2[4];                                 // lse in powers of 2; infinite (weights of 0) where there is no row, or none with a weight
+    int pos[4];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) less[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], c, tw_v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-      }
+    for (int i = 0; i < 4; ++i) {
+      const int r = r0 + 4 * jq + i;
+      l2[i] = r < rows && __builtin_fabsf(y.lse[i]) < __builtin_inff() ? y.lse[i] * kLog2e : __builtin_inff();
+      pos[i] = ctx + (r >> a.lgG);
+    }
+    tw_v4f less[4];                              // -128 Q_g of the lane's rows: a product with a constant
+    if constexpr (CODES) {
+      tw_bf16x8 c;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c[i] = (__bf16)-128.f;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) less[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], c, tw_v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+    }
+    tw_v4f s[PT];
+    if constexpr (CODES) {
 #pragma unroll
       for (int p = 0; p < PT; ++p) {
-        tw_v4f s = {0.f, 0.f, 0.f, 0.f};
-        if (CODES) {
-          const uint32_t w[4] = {km[p].x, km[p].y, km[p].z, km[p].w};
+        tw_bf16x8 kf[4];
+        if constexpr (MANY) {
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const tw_v4f t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], kf[p][g], less[g], 0, 0, 0);
-            const float z = tw_half_hi(w[g]) * (-1.f / 128.f);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] = __builtin_fmaf(tw_half_lo(w[g]), t[i], __builtin_fmaf(z, less[g][i], s[i]));
-          }
+          for (int g = 0; g < 4; ++g) kf[g] = held[p][g];
         } else {
-#pragma unroll
-          for (int g = 0; g < 4; ++g) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], kf[p][g], s, 0, 0, 0);
+          operands(x, p, kf);
         }
-        if (slot[p] < 0) continue;
-        const int t = t0 + 16 * p + r16;
+        const uint32_t w[4] = {x.m[p].x, x.m[p].y, x.m[p].z, x.m[p].w};
+        tw_v4f t[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          // (the maximum makes 0 of what is no number: a row that sees such a token has an lse that says so)
-          float w = fmaxf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[i], kScaleLog2, -l2[i])), 0.f);
-          if (!all) w = t <= pos[i] && (t > pos[i] - a.window || t < a.sinks) ? w : 0.f;
-          acc[p] += w;
+        for (int g = 0; g < 4; ++g) t[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], kf[g], less[g], 0, 0, 0);
+        s[p] = tw_v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float z = tw_half_hi(w[g]) * (-1.f / 128.f);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[p][i] = __builtin_fmaf(z, less[g][i], s[p][i]);
         }
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[p][i] = __builtin_fmaf(tw_half_lo(w[g]), t[g][i], s[p][i]);
+      }
+    } else {                                     // (no product follows the one that it adds to)
+      tw_v4f u[PT];
+#pragma unroll
+      for (int p = 0; p < PT; ++p) s[p] = u[p] = tw_v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int p = 0; p < PT; ++p) {
+          const tw_bf16x8 k = tw_as_bf16(x.k[p][g]);
+          if (PT == 1 && (g & 1)) u[p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], k, u[p], 0, 0, 0);
+          else s[p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], k, s[p], 0, 0, 0);
+        }
+      if (PT == 1) s[0] += u[0];
+    }
+#pragma unroll
+    for (int p = 0; p < PT; ++p) {
+      const int t = t0 + 16 * p + r16;
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // (the maximum makes 0 of what is no number: a row that sees such a token has an lse that says so)
+        float w = fmaxf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i], kScaleLog2, -l2[i])), 0.f);
+        if (!all) w = t <= pos[i] && (t > pos[i] - a.window || t < a.sinks) ? w : 0.f;
+        sum += w;
+      }
+      acc[p] += sum;
+    }
+  };
+
+  const int h0 = wave;
+  if (h0 < a.Hkv && rows > 0) {
+    tw_bf16x8 held[PT][4];                       // (codes as operands, made once for all rows)
+    if constexpr (MANY) {
+      for (int h = h0; h < a.Hkv; h += 4) {
+        int r0 = 0;
+        while (r0 < rows && !seen(r0)) r0 += 16;
+        if (r0 >= rows) break;                   // (of any head)
+        Rows y = load_rows(h, r0);
+        const Keys x = load_keys(h);
+#pragma unroll
+        for (int p = 0; p < PT; ++p)
+          if constexpr (CODES) operands(x, p, held[p]);
+        while (r0 < rows) {
+          int r1 = r0 + 16;
+          while (r1 < rows && !seen(r1)) r1 += 16;
+          const Rows z = load_rows(h, min(r1, rows - 1));
+          add(x, held, y, r0);
+          y = z;
+          r0 = r1;
+        }
+      }
+    } else if (seen(0)) {
+      Keys x = load_keys(h0);
+      Rows y = load_rows(h0, 0);
+      for (int h = h0; h < a.Hkv; h += 4) {
+        const int next = h + 4 < a.Hkv ? h + 4 : h;
+        const Keys xn = load_keys(next);
+        const Rows yn = load_rows(next, 0);
+        add(x, held, y, 0);
+        x = xn;
+        y = yn;
       }
     }
   }
 #pragma unroll
   for (int p = 0; p < PT; ++p) {
-    acc[p] = tw_quarters_sum(acc[p]);
-    if (jq == 0) red[wave][16 * p + r16] = acc[p];
+    const float sum = tw_quarters_sum(slot[p] < 0 ? 0.f : acc[p]);
+    if (jq == 0) red[wave][16 * p + r16] = sum;
   }
   __syncthreads();
   const int t = t0 + (int)threadIdx.x;
@@ -374,6 +452,9 @@ __global__ __launch_bounds__(KEEP_THREADS) void keep_chunk_kernel(KeepArgs a) {
   }
 }
 
+#ifndef MASS_PT
+#define MASS_PT 4
+#endif
 constexpr int WHOLE_TOKENS = 32 * KEEP_THREADS, MOST_CHUNKS = 128;
 
 // Chunks of a long row, and blocks of SUB tokens in each.
@@ -387,8 +468,15 @@ template <bool CODES>
 int launch_mass(const MassArgs& a, int batch, hipStream_t s) {
   tw_prof_before(TW_K_MASS, s);
   const long long pages = (long long)a.max_pages * batch;
-  if (pages <= 2ll * tw_num_cus()) TW_LAUNCH((attention_mass_kernel<CODES, 1>), dim3((unsigned)a.max_pages, (unsigned)batch), dim3(256), 0, s, a);
-  else TW_LAUNCH((attention_mass_kernel<CODES, 4>), dim3((unsigned)((a.max_pages + 3) / 4), (unsigned)batch), dim3(256), 0, s, a);
+  const dim3 one((unsigned)a.max_pages, (unsigned)batch), two((unsigned)((a.max_pages + 1) / 2), (unsigned)batch), four((unsigned)((a.max_pages + 3) / 4), (unsigned)batch), wg(256);
+  if ((long long)a.max_new * a.G > 16) {
+    if (pages <= 2ll * tw_num_cus()) TW_LAUNCH((attention_mass_kernel<CODES, 1, true>), one, wg, 0, s, a);
+    else TW_LAUNCH((attention_mass_kernel<CODES, 4, true>), four, wg, 0, s, a);
+  } else if (pages <= 2ll * tw_num_cus()) {
+    TW_LAUNCH((attention_mass_kernel<CODES, 1, false>), one, wg, 0, s, a);
+  } else {
+    TW_LAUNCH((attention_mass_kernel<CODES, MASS_PT, false>), MASS_PT == 4 ? four : two, wg, 0, s, a);
+  }
   return tw_prof_after(s);
 }
 

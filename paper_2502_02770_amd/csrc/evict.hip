@@ -1,6 +1,7 @@
 // Tokens given up by the attention they got: the weights accumulated per cached token (twilight_attention_mass), and the choice of
 // the tokens to keep (twilight_keep_tokens).  twilight_tokens_compact then moves what is kept.
 #include <algorithm>
+#include <type_traits>
 #include "kv4_common.h"
 
 namespace {
@@ -67,16 +68,20 @@ __global__ __launch_bounds__(256, 2) void attention_mass_kernel(MassArgs a) {
     return x;
   };
   struct Rows { uint4 q[4]; float lse[4]; };
+  // Rows follow each other by 16 / G tokens: what an address adds to the block's first row's is the lane's (and i's) for all blocks
+  const uint32_t q_at = (uint32_t)((r16 >> a.lgG) * a.Hq + (r16 & (a.G - 1))) * 256u + 16u * (uint32_t)jq;
+  const uint32_t l_at = (uint32_t)((4 * jq >> a.lgG) * a.Hq + (4 * jq & (a.G - 1))) * 4u;
   auto load_rows = [&](int h, int r0) -> Rows {
     Rows x;
-    const int mine = min(r0 + r16, rows - 1);
-    const uint4* qp = a.q + ((long long)(off + (mine >> a.lgG)) * a.Hq + h * a.G + (mine & (a.G - 1))) * 16 + jq;
+    const long long row = (long long)(off + (r0 >> a.lgG)) * a.Hq + h * a.G;
+    const char *q = (const char*)a.q + row * 256, *l = (const char*)(a.lse + row);
+    const uint32_t qo = r0 + r16 < rows ? q_at : 16u * (uint32_t)jq;          // (the first row for those behind the last)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) x.q[g] = qp[4 * g];
+    for (int g = 0; g < 4; ++g) x.q[g] = *(const uint4*)(q + qo + 64 * g);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r = min(r0 + 4 * jq + i, rows - 1);
-      x.lse[i] = a.lse[(long long)(off + (r >> a.lgG)) * a.Hq + h * a.G + (r & (a.G - 1))];
+      const uint32_t to = (uint32_t)((i >> a.lgG) * a.Hq + (i & (a.G - 1))) * 4u;
+      x.lse[i] = *(const float*)(l + (r0 + 4 * jq + i < rows ? l_at + to : 0u));
     }
     return x;
   };
@@ -85,11 +90,10 @@ __global__ __launch_bounds__(256, 2) void attention_mass_kernel(MassArgs a) {
     tw_transpose_quarters(c);
     kf[0] = tw_codes_bf16(c.x); kf[1] = tw_codes_bf16(c.y); kf[2] = tw_codes_bf16(c.z); kf[3] = tw_codes_bf16(c.w);
   };
-  // The rows r0 .. r0 + 15: do they see any of the pages, and their weights there
-  auto seen = [&](int r0) -> bool {
-    const int p_lo = ctx + (r0 >> a.lgG), p_hi = ctx + ((min(r0 + 16, rows) - 1) >> a.lgG);
-    return !(t0 > p_hi || (t0 + 16 * PT - 1 <= p_lo - a.window && t0 >= a.sinks));
-  };
+  // Blocks of rows that see any of the pages: those at positions from the first page's start on, and not so far behind that no window reaches
+  const int from = min(rows, max(0, t0 - ctx) * a.G) & ~15;
+  const int to = t0 < a.sinks ? rows : (int)max(0ll, min((long long)rows, ((long long)t0 + 16 * PT - 1 + a.window - ctx) * a.G));
+  // The weights of rows r0 .. r0 + 15 on the pages
   auto add = [&](const Keys& x, const tw_bf16x8 (&held)[PT][4], const Rows& y, int r0) {
     const int p_lo = ctx + (r0 >> a.lgG), p_hi = ctx + ((min(r0 + 16, rows) - 1) >> a.lgG);
     const bool all = t0 + 16 * PT - 1 <= p_lo && (t0 > p_hi - a.window || t0 + 16 * PT <= a.sinks);
@@ -153,47 +157,48 @@ __global__ __launch_bounds__(256, 2) void attention_mass_kernel(MassArgs a) {
         }
       if (PT == 1) s[0] += u[0];
     }
+    auto weigh = [&](auto masked) {
 #pragma unroll
-    for (int p = 0; p < PT; ++p) {
-      const int t = t0 + 16 * p + r16;
-      float sum = 0.f;
+      for (int p = 0; p < PT; ++p) {
+        const int t = t0 + 16 * p + r16;
+        float w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        // (the maximum makes 0 of what is no number: a row that sees such a token has an lse that says so)
-        float w = fmaxf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i], kScaleLog2, -l2[i])), 0.f);
-        if (!all) w = t <= pos[i] && (t > pos[i] - a.window || t < a.sinks) ? w : 0.f;
-        sum += w;
+        for (int i = 0; i < 4; ++i) {
+          // (the maximum makes 0 of what is no number: a row that sees such a token has an lse that says so)
+          w[i] = fmaxf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i], kScaleLog2, -l2[i])), 0.f);
+          if constexpr (decltype(masked)::value) w[i] = (t <= pos[i]) & ((t > pos[i] - a.window) | (t < a.sinks)) ? w[i] : 0.f;
+        }
+        acc[p] += (w[0] + w[1]) + (w[2] + w[3]);
       }
-      acc[p] += sum;
-    }
+    };
+    if (all) weigh(std::false_type{});           // (a branch of its own: asked at every score it would be one per score)
+    else weigh(std::true_type{});
   };
 
-  const int h0 = wave;
-  if (h0 < a.Hkv && rows > 0) {
+  if (wave < a.Hkv && from < to) {
     tw_bf16x8 held[PT][4];                       // (codes as operands, made once for all rows)
     if constexpr (MANY) {
-      for (int h = h0; h < a.Hkv; h += 4) {
-        int r0 = 0;
-        while (r0 < rows && !seen(r0)) r0 += 16;
-        if (r0 >= rows) break;                   // (of any head)
-        Rows y = load_rows(h, r0);
+      const int last = (to - 1) & ~15;
+      for (int h = wave; h < a.Hkv; h += 4) {
+        Rows y[2] = {load_rows(h, from), load_rows(h, min(last, from + 16))};
         const Keys x = load_keys(h);
 #pragma unroll
         for (int p = 0; p < PT; ++p)
           if constexpr (CODES) operands(x, p, held[p]);
-        while (r0 < rows) {
-          int r1 = r0 + 16;
-          while (r1 < rows && !seen(r1)) r1 += 16;
-          const Rows z = load_rows(h, min(r1, rows - 1));
-          add(x, held, y, r0);
-          y = z;
-          r0 = r1;
+        for (int r0 = from; r0 < to; r0 += 32) {
+          Rows now = y[0];
+          y[0] = load_rows(h, min(last, r0 + 32));
+          add(x, held, now, r0);
+          if (r0 + 16 >= to) break;
+          now = y[1];
+          y[1] = load_rows(h, min(last, r0 + 48));
+          add(x, held, now, r0 + 16);
         }
       }
-    } else if (seen(0)) {
-      Keys x = load_keys(h0);
-      Rows y = load_rows(h0, 0);
-      for (int h = h0; h < a.Hkv; h += 4) {
+    } else {
+      Keys x = load_keys(wave);
+      Rows y = load_rows(wave, 0);
+      for (int h = wave; h < a.Hkv; h += 4) {
         const int next = h + 4 < a.Hkv ? h + 4 : h;
         const Keys xn = load_keys(next);
         const Rows yn = load_rows(next, 0);

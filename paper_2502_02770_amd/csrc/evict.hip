@@ -67,22 +67,17 @@ __global__ __launch_bounds__(256, 2) void attention_mass_kernel(MassArgs a) {
     }
     return x;
   };
-  struct Rows { uint4 q[4]; float lse[4]; };
-  // Rows follow each other by 16 / G tokens: what an address adds to the block's first row's is the lane's (and i's) for all blocks
-  const uint32_t q_at = (uint32_t)((r16 >> a.lgG) * a.Hq + (r16 & (a.G - 1))) * 256u + 16u * (uint32_t)jq;
-  const uint32_t l_at = (uint32_t)((4 * jq >> a.lgG) * a.Hq + (4 * jq & (a.G - 1))) * 4u;
+  struct Rows { uint4 q[4]; float lse; };        // of row r16
+  // Rows follow each other by 16 / G tokens: what an address adds to the block's first row's is the lane's for all blocks
+  const uint32_t at = (uint32_t)((r16 >> a.lgG) * a.Hq + (r16 & (a.G - 1)));
   auto load_rows = [&](int h, int r0) -> Rows {
     Rows x;
     const long long row = (long long)(off + (r0 >> a.lgG)) * a.Hq + h * a.G;
     const char *q = (const char*)a.q + row * 256, *l = (const char*)(a.lse + row);
-    const uint32_t qo = r0 + r16 < rows ? q_at : 16u * (uint32_t)jq;          // (the first row for those behind the last)
+    const uint32_t mine = r0 + r16 < rows ? at : 0u;         // (the first row for those behind the last)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) x.q[g] = *(const uint4*)(q + qo + 64 * g);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t to = (uint32_t)((i >> a.lgG) * a.Hq + (i & (a.G - 1))) * 4u;
-      x.lse[i] = *(const float*)(l + (r0 + 4 * jq + i < rows ? l_at + to : 0u));
-    }
+    for (int g = 0; g < 4; ++g) x.q[g] = *(const uint4*)(q + (mine * 256u + 16u * (uint32_t)jq) + 64 * g);
+    x.lse = *(const float*)(l + mine * 4u);
     return x;
   };
   auto operands = [&](const Keys& x, int p, tw_bf16x8 (&kf)[4]) {
@@ -102,11 +97,11 @@ __global__ __launch_bounds__(256, 2) void attention_mass_kernel(MassArgs a) {
     for (int g = 0; g < 4; ++g) qf[g] = CODES ? tw_q_like_codes(y.q[g]) : tw_as_bf16(y.q[g]);
     float l2[4];                                 // lse in powers of 2; infinite (weights of 0) where there is no row, or none with a weight
     int pos[4];
+    const float mine = r0 + r16 < rows && __builtin_fabsf(y.lse) < __builtin_inff() ? y.lse * kLog2e : __builtin_inff();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = r0 + 4 * jq + i;
-      l2[i] = r < rows && __builtin_fabsf(y.lse[i]) < __builtin_inff() ? y.lse[i] * kLog2e : __builtin_inff();
-      pos[i] = ctx + (r >> a.lgG);
+    for (int i = 0; i < 4; ++i) {                // (four loads of the rows' own lse took 9 of 55 us of two prompts' last 64 tokens)
+      l2[i] = __int_as_float(__builtin_amdgcn_ds_bpermute((4 * jq + i) * 4, __float_as_int(mine)));
+      pos[i] = ctx + ((r0 + 4 * jq + i) >> a.lgG);
     }
     tw_v4f less[4];                              // -128 Q_g of the lane's rows: a product with a constant
     if constexpr (CODES) {

@@ -228,11 +228,12 @@ struct KeepArgs {
   int32_t* idx;
   int32_t* count;
   float* mass_out;                               // or nullptr
-  uint32_t* ws;                                  // [batch][chunks][CHUNK_WORDS]
+  uint32_t* ws;                                  // [batch][SEQ_WORDS], [batch][chunks][CHUNK_WORDS]
   int max_pages, sinks, recent, stride, chunks, blocks;   // blocks of SUB tokens to a chunk
 };
 constexpr int KEEP_THREADS = 1024, SUB = 8 * KEEP_THREADS;
 constexpr int CHUNK_WORDS = 2048 + 2048 + 1024 + 2;     // three histograms, tokens above the first two's digits
+constexpr int SEQ_WORDS = 4;                            // what is known of a sequence after each launch: (bits, tokens to find) twice
 
 struct KeepSeq {
   int len, kept, first, last, want;              // tokens, of them kept; of those kept first and latest ones, and of those between
@@ -246,216 +247,229 @@ __device__ __forceinline__ KeepSeq keep_seq(const KeepArgs& a, int b) {
   s.want = s.kept - s.first - s.last;
   return s;
 }
-// larger weight, larger key; no number: 0, below all of them
-__device__ __forceinline__ uint32_t keep_key(float x) { return x == x ? tw_float_key(x + 0.0f) : 0u; }
+// Larger weight, larger key; no number: 1, below all of them; 0: not to be chosen by its weight (a first or latest token, or none).
+__device__ __forceinline__ uint32_t keep_key(float x) { return x == x ? tw_float_key(x + 0.0f) : 1u; }
 
-// The bin, from the highest down, in which the want-th token lies, and how many are in those above it.  hist: this thread's bins
-// (2 of 2048, the higher in .x, or 1 of 1024).
+// The bin of 2048, from the highest down, in which the want-th token lies, and how many are in those above it.  One wave does it, 32 bins
+// to a lane and then one bin to a lane: two barriers for the others, where a scan over the workgroup has five.
 struct Digit { uint32_t bin, above; };
-template <int PER>
-__device__ __forceinline__ Digit find_digit(uint32_t hi, uint32_t lo, uint32_t want, uint32_t* scratch) {
-  uint32_t total;
-  const uint32_t incl = tw_block_scan_u32(hi + lo, scratch, &total), before = incl - hi - lo;
-  uint32_t* found = scratch + 16;
-  if (before < want && want <= incl) {
-    const uint32_t top = PER * KEEP_THREADS - 1 - PER * threadIdx.x;
-    const bool second = PER == 2 && want > before + hi;
-    found[0] = second ? top - 1 : top;
-    found[1] = second ? before + hi : before;
-  }
-  __syncthreads();
-  const Digit d = {found[0], found[1]};
-  __syncthreads();
-  return d;
-}
-
-// 8 consecutive weights of a row (those behind its end are not read)
-__device__ __forceinline__ void load8(const float* row, int t, int len, float* x) {
-  if (t + 8 <= len) {
-    const float4 u = *(const float4*)(row + t), v = *(const float4*)(row + t + 4);
-    x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
-  } else {
+__device__ __forceinline__ Digit find_digit(const uint32_t* hist, uint32_t want, uint32_t* scratch) {
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
+    uint32_t sum = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = t + i < len ? row[t + i] : 0.f;
+    for (int i = 0; i < 8; ++i) {                // (each lane begins at another of its pieces, so that they do not meet in a bank)
+      const uint4 x = *(const uint4*)(hist + 2016 - 32 * lane + 4 * ((i + lane) & 7));
+      sum += (x.x + x.y) + (x.z + x.w);
+    }
+    const uint32_t incl = tw_wave_scan_u32(sum);
+    const int l = __builtin_ctzll(__ballot(incl >= want) | 1ull << 63);
+    const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)(incl - sum), l);
+    const int top = 2047 - 32 * l;
+    const uint32_t n = lane < 32 ? hist[top - lane] : 0u, here = before + tw_wave_scan_u32(n);
+    const int k = __builtin_ctzll(__ballot(here >= want) | 1ull << 31);
+    if (lane == k) { scratch[16] = (uint32_t)(top - k); scratch[17] = here - n; }
   }
+  __syncthreads();
+  return {scratch[16], scratch[17]};
 }
 
-// A thread's tokens t .. t + E - 1 written where they are kept.  above, ties: tokens kept for a larger key, and tokens of the last
-// key, before t; room: how many of the latter are kept.
+// Keys of a wave's rows of 64 consecutive tokens: row i begins at t0 + 64 i, a lane has one token of each.
 template <int E>
-__device__ __forceinline__ void emit(const KeepArgs& a, int b, const KeepSeq& s, int t, const uint32_t* key, const float* x, uint32_t last_key, bool any,
-                                     uint32_t above, uint32_t ties, uint32_t room) {
-  const long long out = (long long)b * a.stride;
+__device__ __forceinline__ void load_keys64(const float* row, int t0, int lo, int hi, int len, float (&x)[E], uint32_t (&key)[E]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < E; ++i) x[i] = t0 + 64 * i + lane < len ? row[t0 + 64 * i + lane] : 0.f;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const int p = t + i;
-    if (p >= s.len) break;
+    const int t = t0 + 64 * i + lane;
+    key[i] = t >= lo && t < hi ? keep_key(x[i]) : 0u;
+  }
+}
+// Of rows: tokens kept for a larger key (low half) and those of the last key kept (high half), at most 2^15 each
+template <int E>
+__device__ __forceinline__ uint32_t count_rows64(const uint32_t (&key)[E], uint32_t last_key) {
+  uint32_t n = 0;
+#pragma unroll
+  for (int i = 0; i < E; ++i) n += (uint32_t)__popcll(__ballot(key[i] > last_key)) + ((uint32_t)__popcll(__ballot(key[i] == last_key)) << 16);
+  return n;
+}
+// The rows' tokens written where they are kept.  above, ties: tokens kept for a larger key, and of the last one, before them; room: how many of
+// the latter are kept.  A row's kept tokens stand side by side.
+template <int E>
+__device__ __forceinline__ void emit_rows64(const KeepArgs& a, int b, const KeepSeq& s, const float (&x)[E], const uint32_t (&key)[E], int t0, uint32_t last_key,
+                                            uint32_t above, uint32_t ties, uint32_t room) {
+  const long long out = (long long)b * a.stride;
+  const int lane = threadIdx.x & 63, hi = s.len - s.last;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int first = t0 + 64 * i, t = first + lane;
+    if (first >= s.len) break;
+    const bool more = key[i] > last_key, tie = key[i] == last_key;
+    const unsigned long long mm = __ballot(more), mt = __ballot(tie);
+    const uint32_t rank = ties + tw_bits_below(mt);
     int at = -1;
-    if (p < s.first) at = p;
-    else if (p >= s.len - s.last) at = s.kept - (s.len - p);
-    else if (any) {
-      const bool tie = key[i] == last_key;
-      if (key[i] > last_key || (tie && ties < room)) at = s.first + (int)(above + min(ties, room));
-      above += key[i] > last_key;
-      ties += tie;
-    }
+    if (more || (tie && rank < room)) at = s.first + (int)(above + tw_bits_below(mm) + min(rank, room));
+    if (t < s.first) at = t;
+    if (t >= hi && t < s.len) at = s.kept - (s.len - t);
     if (at >= 0) {
-      a.idx[out + at] = p;
+      a.idx[out + at] = t;
       if (a.mass_out) a.mass_out[out + at] = x[i];
     }
+    above += (uint32_t)__popcll(mm);
+    ties += (uint32_t)__popcll(mt);
   }
+}
+// A digit of the rows' tokens that share the bits found before, counted
+template <int PASS, int E>
+__device__ __forceinline__ void count_digit(uint32_t* hist, const uint32_t (&key)[E], uint32_t prefix) {
+  constexpr int shift = PASS == 0 ? 21 : PASS == 1 ? 10 : 0, bits = PASS == 2 ? 10 : 11;
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+    if (key[i] != 0u && (PASS == 0 || key[i] >> (shift + bits) == prefix)) atomicAdd(&hist[(key[i] >> shift) & ((1u << bits) - 1u)], 1u);
 }
 
 // A whole sequence per workgroup, E tokens per thread in registers.
-template <int E>
-__global__ __launch_bounds__(KEEP_THREADS) void keep_whole_kernel(KeepArgs a) {
-  __shared__ uint32_t hist[2048];
+template <int THREADS, int E>
+__global__ __launch_bounds__(THREADS) void keep_whole_kernel(KeepArgs a) {
+  __shared__ __align__(16) uint32_t hist[3][2048];
   __shared__ uint32_t scratch[20];
-  const int b = blockIdx.x, tid = threadIdx.x;
+  const int b = blockIdx.x, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const KeepSeq s = keep_seq(a, b);
   if (tid == 0) a.count[b] = s.kept;
   if (s.kept == 0) return;
-  const float* row = a.mass + (long long)b * a.max_pages * TW_PAGE;
+  const int t0 = wave * 64 * E, lo = s.first, hi = s.len - s.last;
   float x[E];
   uint32_t key[E];
-  const int t = tid * E;
-#pragma unroll
-  for (int i = 0; i < E; i += 8) {
-    if (E >= 8) load8(row, t + i, s.len, x + i);
-    else
-#pragma unroll
-      for (int k = 0; k < E; ++k) x[k] = t + k < s.len ? row[t + k] : 0.f;
-  }
-#pragma unroll
-  for (int i = 0; i < E; ++i) key[i] = keep_key(x[i]);
-  const int lo = s.first, hi = s.len - s.last;
-  uint32_t prefix = 0, want = (uint32_t)s.want;
+  load_keys64<E>(a.mass + (long long)b * a.max_pages * TW_PAGE, t0, lo, hi, s.len, x, key);
+  uint32_t prefix = ~0u, want = (uint32_t)s.want;            // (no key is this large)
   if (s.want > 0) {
+#pragma unroll
+    for (int i = 0; i < 3 * 2048 / THREADS; ++i) (&hist[0][0])[tid + THREADS * i] = 0;
+    __syncthreads();
+    prefix = 0;
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-      hist[tid] = 0; hist[tid + 1024] = 0;
+      if (pass == 0) count_digit<0, E>(hist[0], key, prefix);
+      else if (pass == 1) count_digit<1, E>(hist[1], key, prefix);
+      else count_digit<2, E>(hist[2], key, prefix);          // (the upper half of the last stays empty)
       __syncthreads();
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (t + i >= lo && t + i < hi && (pass == 0 || key[i] >> (shift + bits) == prefix)) atomicAdd(&hist[(key[i] >> shift) & ((1u << bits) - 1u)], 1u);
-      __syncthreads();
-      const Digit d = pass < 2 ? find_digit<2>(hist[2047 - 2 * tid], hist[2046 - 2 * tid], want, scratch) : find_digit<1>(hist[1023 - tid], 0u, want, scratch);
-      prefix = prefix << bits | d.bin;
-      want -= d.above;
-    }
-  }
-  // kept for a larger key, and of the last key, before this thread's tokens
-  uint32_t mine = 0;
-#pragma unroll
-  for (int i = 0; i < E; ++i)
-    if (t + i >= lo && t + i < hi) mine += (key[i] > prefix ? 1u : 0u) + (key[i] == prefix ? 0x10000u : 0u);
-  uint32_t total;
-  const uint32_t before = tw_block_scan_u32(mine, scratch, &total) - mine;
-  emit<E>(a, b, s, t, key, x, prefix, s.want > 0, before & 0xFFFFu, before >> 16, want);
-}
-
-// Long sequences: a workgroup per chunk of tokens, a launch per histogram and one that writes.  PASS 0 .. 2 make a chunk's histogram of
-// that digit; 1 .. 3 first find the digit before from all chunks' histograms.
-template <int PASS>
-__global__ __launch_bounds__(KEEP_THREADS) void keep_chunk_kernel(KeepArgs a) {
-  __shared__ uint32_t hist[2048];
-  __shared__ uint32_t scratch[20];
-  const int b = blockIdx.y, c = blockIdx.x, tid = threadIdx.x;
-  const KeepSeq s = keep_seq(a, b);
-  if (PASS == 3 && c == 0 && tid == 0) a.count[b] = s.kept;
-  const int span = a.blocks * SUB;
-  const long long t0 = (long long)c * span;
-  if (s.kept == 0 || t0 >= s.len) return;
-  const int chunks = (s.len + span - 1) / span;  // of this sequence
-  uint32_t* const all = a.ws + (long long)b * a.chunks * CHUNK_WORDS;
-  uint32_t* const own = all + (long long)c * CHUNK_WORDS;
-  const float* row = a.mass + (long long)b * a.max_pages * TW_PAGE;
-  const int lo = s.first, hi = s.len - s.last;
-  uint32_t prefix = 0, want = (uint32_t)s.want, above = 0, ties = 0;
-  if (s.want > 0) {
-#pragma unroll
-    for (int pass = 0; pass < PASS; ++pass) {
-      uint32_t h0 = 0, h1 = 0, p0 = 0;           // all chunks' tokens of this thread's bins, those of the chunks before this one
-      for (int k = 0; k < chunks; ++k) {
-        const uint32_t* h = all + (long long)k * CHUNK_WORDS + 2048 * pass;
-        if (pass < 2) {
-          const uint2 x = *(const uint2*)(h + 2046 - 2 * tid);
-          h0 += x.y; h1 += x.x;
-        } else {
-          const uint32_t x = h[1023 - tid];
-          h0 += x;
-          if (k < c) p0 += x;
-        }
-      }
-      const Digit d = pass < 2 ? find_digit<2>(h0, h1, want, scratch) : find_digit<1>(h0, 0u, want, scratch);
-      if (PASS < 3 && pass == PASS - 1) {        // this chunk's tokens above the digit, for those behind it
-        uint32_t x = 0;
-        const uint32_t y0 = own[2048 * pass + 2047 - 2 * tid], y1 = own[2048 * pass + 2046 - 2 * tid];
-        if (2047u - 2 * tid > d.bin) x += y0;
-        if (2046u - 2 * tid > d.bin) x += y1;
-        uint32_t total;
-        tw_block_scan_u32(x, scratch, &total);
-        if (tid == 0) own[5120 + pass] = total;
-      }
-      if (pass == 2) {
-        uint32_t x = 1023u - tid > d.bin ? p0 : 0u, total;
-        for (int k = tid; k < c; k += KEEP_THREADS) x += all[(long long)k * CHUNK_WORDS + 5120] + all[(long long)k * CHUNK_WORDS + 5121];
-        tw_block_scan_u32(x, scratch, &total);
-        above = total;
-        if (1023u - tid == d.bin) scratch[18] = p0;
-        __syncthreads();
-        ties = scratch[18];
-        __syncthreads();
-      }
+      const Digit d = find_digit(hist[pass], want, scratch);
       prefix = prefix << (pass == 2 ? 10 : 11) | d.bin;
       want -= d.above;
     }
   }
+  // kept for a larger key, and of the last key, before this wave's tokens
+  const uint32_t mine = count_rows64<E>(key, prefix);
+  if ((tid & 63) == 0) scratch[wave] = mine;
+  __syncthreads();
+  uint32_t before = 0;
+  for (int w = 0; w < wave; ++w) before += scratch[w];
+  emit_rows64<E>(a, b, s, x, key, t0, prefix, before & 0xFFFFu, before >> 16, want);
+}
+
+// Long sequences: a workgroup per chunk of tokens, a launch per histogram and one that writes.  PASS 0 .. 2 make a chunk's histogram of
+// that digit; 1 .. 3 first find the digit before from all chunks' histograms, and the first chunk leaves it for the launches to come.
+template <int PASS>
+__global__ __launch_bounds__(KEEP_THREADS) void keep_chunk_kernel(KeepArgs a) {
+  __shared__ __align__(16) uint32_t hist[2048];
+  __shared__ uint32_t scratch[20];
+  const int b = blockIdx.y, c = blockIdx.x, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const KeepSeq s = keep_seq(a, b);
+  if (PASS == 3 && c == 0 && tid == 0) a.count[b] = s.kept;
+  const long long span = (long long)a.blocks * SUB, begin = c * span;
+  if (s.kept == 0 || begin >= s.len) return;
+  const int t0 = (int)begin, chunks = (int)((s.len + span - 1) / span);        // chunks of this sequence
+  uint32_t* const known = a.ws + (long long)b * SEQ_WORDS;
+  uint32_t* const all = a.ws + (long long)gridDim.y * SEQ_WORDS + (long long)b * a.chunks * CHUNK_WORDS;
+  uint32_t* const own = all + (long long)c * CHUNK_WORDS;
+  const float* row = a.mass + (long long)b * a.max_pages * TW_PAGE;
+  const int lo = s.first, hi = s.len - s.last;
+  float x[8];
+  uint32_t key[8];
+  // (a chunk of one block, as those of up to 128 x 8192 tokens are, is asked for at once)
+  if (a.blocks == 1) load_keys64<8>(row, t0 + wave * 512, lo, hi, s.len, x, key);
+  uint32_t prefix = 0, want = (uint32_t)s.want, above = 0, ties = 0;
+  if (PASS > 0 && s.want > 0) {
+    constexpr int D = PASS > 0 ? PASS - 1 : 0;   // the digit to find
+    if (PASS > 1) { prefix = known[2 * (PASS - 2)]; want = known[2 * (PASS - 2) + 1]; }
+    const uint32_t* h = all + 2048 * D;
+    uint32_t n0 = 0, n1 = 0, mine0 = 0, mine1 = 0;           // this thread's two bins, or the one of the last digit: of all chunks, and of this
+    if (D < 2) {                                 // one, or of all before this one
+#pragma unroll 8
+      for (int k = 0; k < chunks; ++k) {
+        const uint2 y = *(const uint2*)(h + (long long)k * CHUNK_WORDS + 2 * tid);
+        n0 += y.x; n1 += y.y;
+        if (k == c) { mine0 = y.x; mine1 = y.y; }
+      }
+      *(uint2*)(hist + 2 * tid) = make_uint2(n0, n1);
+    } else {
+#pragma unroll 8
+      for (int k = 0; k < chunks; ++k) {
+        const uint32_t y = h[(long long)k * CHUNK_WORDS + tid];
+        n0 += y;
+        mine0 += k < c ? y : 0u;
+      }
+      hist[tid] = n0;
+      hist[tid + 1024] = 0;
+    }
+    if (tid == 0) scratch[18] = scratch[19] = 0;
+    __syncthreads();
+    const Digit d = find_digit(hist, want, scratch);
+    // tokens above the digit: this chunk's, for those behind it, or those of all before it
+    const uint32_t bin = D < 2 ? 2 * tid : tid;
+    uint32_t more = (bin > d.bin ? mine0 : 0u) + (D < 2 && bin + 1u > d.bin ? mine1 : 0u);
+    if (D == 2) {
+      for (int k = tid; k < c; k += KEEP_THREADS) more += all[(long long)k * CHUNK_WORDS + 5120] + all[(long long)k * CHUNK_WORDS + 5121];
+      if (bin == d.bin) scratch[19] = mine0;
+    }
+    more = (uint32_t)__builtin_amdgcn_readlane((int)tw_wave_scan_u32(more), 63);
+    if ((tid & 63) == 0 && more) atomicAdd(&scratch[18], more);
+    __syncthreads();
+    if (D < 2) {
+      if (tid == 0) own[5120 + D] = scratch[18];
+    } else {
+      above = scratch[18];
+      ties = scratch[19];
+    }
+    prefix = prefix << (D == 2 ? 10 : 11) | d.bin;
+    want -= d.above;
+    if (PASS < 3 && c == 0 && tid == 0) { known[2 * D] = prefix; known[2 * D + 1] = want; }
+  }
   if (PASS < 3) {
     if (s.want == 0) return;
-    constexpr int shift = PASS == 0 ? 21 : PASS == 1 ? 10 : 0, bits = PASS == 2 ? 10 : 11;
     hist[tid] = 0; hist[tid + 1024] = 0;
     __syncthreads();
     for (int k = 0; k < a.blocks; ++k) {
-      const long long t = t0 + (long long)k * SUB + 8 * tid;
+      const int t = t0 + k * SUB + wave * 512;
       if (t >= hi) break;
-      float x[8];
-      load8(row, (int)t, s.len, x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t key = keep_key(x[i]);
-        if (t + i >= lo && t + i < hi && (PASS == 0 || key >> (shift + bits) == prefix)) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1u)], 1u);
-      }
+      if (a.blocks > 1) load_keys64<8>(row, t, lo, hi, s.len, x, key);
+      count_digit<PASS, 8>(hist, key, prefix);
     }
     __syncthreads();
     own[2048 * PASS + tid] = hist[tid];
     if (PASS < 2) own[2048 * PASS + 1024 + tid] = hist[tid + 1024];
     return;
   }
+  if (s.want == 0) prefix = ~0u;                 // (no key is this large)
   for (int k = 0; k < a.blocks; ++k) {
-    const long long at = t0 + (long long)k * SUB;
+    const int at = t0 + k * SUB, t = at + wave * 512;
     if (at >= s.len) break;
-    const int t = (int)at + 8 * tid;
-    float x[8];
-    uint32_t key[8], mine = 0, total;
-    load8(row, t, s.len, x);
+    if (a.blocks > 1) load_keys64<8>(row, t, lo, hi, s.len, x, key);
+    const uint32_t mine = count_rows64<8>(key, prefix);
+    if ((tid & 63) == 0) scratch[wave] = mine;
+    __syncthreads();
+    uint32_t before = 0, total = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      key[i] = keep_key(x[i]);
-      if (t + i >= lo && t + i < hi) mine += (key[i] > prefix ? 1u : 0u) + (key[i] == prefix ? 0x10000u : 0u);
-    }
-    const uint32_t before = tw_block_scan_u32(mine, scratch, &total) - mine;
-    emit<8>(a, b, s, t, key, x, prefix, s.want > 0, above + (before & 0xFFFFu), ties + (before >> 16), want);
+    for (int w = 0; w < KEEP_THREADS / 64; ++w) { const uint32_t n = scratch[w]; before += w < wave ? n : 0u; total += n; }
+    emit_rows64<8>(a, b, s, x, key, t, prefix, above + (before & 0xFFFFu), ties + (before >> 16), want);
     above += total & 0xFFFFu;
     ties += total >> 16;
+    __syncthreads();                             // the counts have been read
   }
 }
 
-#ifndef MASS_PT
-#define MASS_PT 4
-#endif
-constexpr int WHOLE_TOKENS = 32 * KEEP_THREADS, MOST_CHUNKS = 128;
+constexpr int WHOLE_TOKENS = 8192, MOST_CHUNKS = 128;
 
 // Chunks of a long row, and blocks of SUB tokens in each.
 void keep_chunks(const TwDims& d, int* chunks, int* blocks) {
@@ -468,14 +482,14 @@ template <bool CODES>
 int launch_mass(const MassArgs& a, int batch, hipStream_t s) {
   tw_prof_before(TW_K_MASS, s);
   const long long pages = (long long)a.max_pages * batch;
-  const dim3 one((unsigned)a.max_pages, (unsigned)batch), two((unsigned)((a.max_pages + 1) / 2), (unsigned)batch), four((unsigned)((a.max_pages + 3) / 4), (unsigned)batch), wg(256);
+  const dim3 one((unsigned)a.max_pages, (unsigned)batch), four((unsigned)((a.max_pages + 3) / 4), (unsigned)batch), wg(256);
   if ((long long)a.max_new * a.G > 16) {
     if (pages <= 2ll * tw_num_cus()) TW_LAUNCH((attention_mass_kernel<CODES, 1, true>), one, wg, 0, s, a);
     else TW_LAUNCH((attention_mass_kernel<CODES, 4, true>), four, wg, 0, s, a);
   } else if (pages <= 2ll * tw_num_cus()) {
     TW_LAUNCH((attention_mass_kernel<CODES, 1, false>), one, wg, 0, s, a);
   } else {
-    TW_LAUNCH((attention_mass_kernel<CODES, MASS_PT, false>), MASS_PT == 4 ? four : two, wg, 0, s, a);
+    TW_LAUNCH((attention_mass_kernel<CODES, 4, false>), four, wg, 0, s, a);
   }
   return tw_prof_after(s);
 }
@@ -486,7 +500,7 @@ size_t tw_keep_workspace(const TwDims& d) {
   if ((long long)d.max_pages * TW_PAGE <= WHOLE_TOKENS) return 256;
   int chunks, blocks;
   keep_chunks(d, &chunks, &blocks);
-  return ((size_t)d.batch * chunks * CHUNK_WORDS * 4 + 255) & ~(size_t)255;
+  return ((size_t)d.batch * (SEQ_WORDS + (size_t)chunks * CHUNK_WORDS) * 4 + 255) & ~(size_t)255;
 }
 
 extern "C" int twilight_attention_mass(const twilight_kv_t* kv, const void* q, const float* lse, const int32_t* n_new, const int32_t* new_offsets,
@@ -524,10 +538,9 @@ extern "C" int twilight_keep_tokens(const twilight_kv_t* kv, const float* mass, 
   const long long tokens = (long long)d.max_pages * TW_PAGE;
   if (tokens <= WHOLE_TOKENS) {
     tw_prof_before(TW_K_KEEP, s);
-    const dim3 grid((unsigned)d.batch), block(KEEP_THREADS);
-    if (tokens <= 2 * KEEP_THREADS) TW_LAUNCH(keep_whole_kernel<2>, grid, block, 0, s, a);
-    else if (tokens <= 8 * KEEP_THREADS) TW_LAUNCH(keep_whole_kernel<8>, grid, block, 0, s, a);
-    else TW_LAUNCH(keep_whole_kernel<32>, grid, block, 0, s, a);
+    const dim3 grid((unsigned)d.batch);
+    if (tokens <= 4096) TW_LAUNCH((keep_whole_kernel<256, 16>), grid, dim3(256), 0, s, a);
+    else TW_LAUNCH((keep_whole_kernel<512, 16>), grid, dim3(512), 0, s, a);
     return tw_prof_after(s);
   }
   keep_chunks(d, &a.chunks, &a.blocks);

@@ -81,9 +81,9 @@ def test_workspaces(T):
     assert parts * 520 <= size(T.TW_WS_KV4, _kv(T, max_pages=128), 1) <= parts * 520 + 1024
     assert size(T.TW_WS_KV4, _kv(T, max_pages=1 << 20), 1) == size(T.TW_WS_KV4, _kv(T, max_pages=1 << 22), 1) <= 2 * 512 * 16 * 520 + 1024
     assert size(T.TW_WS_KV4, _kv(T), 0) == size(T.TW_WS_KV4, _kv(T), -3) == 0
-    assert size(T.TW_WS_KEEP, _kv(T, max_pages=2048)) == 256
-    assert 2 * 5 * 5122 * 4 <= size(T.TW_WS_KEEP, _kv(T, max_pages=2049)) <= 2 * 5 * 5122 * 4 + 256
-    assert size(T.TW_WS_KEEP, _kv(T, max_pages=1 << 24)) <= 2 * 128 * 5122 * 4 + 256
+    assert size(T.TW_WS_KEEP, _kv(T, max_pages=512)) == 256
+    assert 2 * 5 * 5122 * 4 <= size(T.TW_WS_KEEP, _kv(T, max_pages=2049)) <= 2 * 5 * 5122 * 4 + 512
+    assert size(T.TW_WS_KEEP, _kv(T, max_pages=1 << 24)) <= 2 * 128 * 5122 * 4 + 512
 
 
 def test_compaction_of_codes_alone(T):

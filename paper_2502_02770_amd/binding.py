@@ -129,18 +129,14 @@ def _sums(t):
     return t.data_ptr()
 
 
-def _codes(t, last):
-    """A pool of codes or (scale, zero): [pages, heads, 16, last...]."""
-    assert t.is_cuda and t.is_contiguous() and (t.dtype is torch.uint8 if last == (64,) else t.dtype is torch.float16) and t.shape[2:] == (16, *last), \
-        "pools of codes u8 [pages, heads, 16, 64] and (scale, zero) f16 [pages, heads, 16, 4, 2] on the GPU required"
-    return t.data_ptr()
-
-
 def _v_pools(kv, vq_pool, vq_meta):
-    """V's pools of a cache in 4 bits, as many pages and heads as the cache has."""
-    a = _codes(vq_pool, (64,)), _codes(vq_meta, (4, 2))
-    assert vq_pool.shape[:2] == vq_meta.shape[:2] == (kv.num_pool_pages, kv.num_kv_heads), "V's pools as large as K's"
-    return a
+    """V's codes and (scale, zero) of a cache in 4 bits: as many pages and heads as the cache has.  (By their sizes: a decode step of a few
+    sequences takes about as long on the device as its calls take here.)"""
+    rows = kv.num_pool_pages * kv.num_kv_heads
+    assert vq_pool.dtype is torch.uint8 and vq_pool.is_cuda and vq_pool.is_contiguous() and vq_pool.numel() == rows * 1024 and \
+        vq_meta.dtype is torch.float16 and vq_meta.is_cuda and vq_meta.is_contiguous() and vq_meta.numel() == rows * 128, \
+        "codes u8 [pages, heads, 16, 64] and (scale, zero) f16 [pages, heads, 16, 4, 2] of V on the GPU required, as large as K's"
+    return vq_pool.data_ptr(), vq_meta.data_ptr()
 
 
 def _count(x):

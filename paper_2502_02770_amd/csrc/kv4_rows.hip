@@ -41,15 +41,21 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(RowArgs4 a) {
   const int b = blockIdx.z, h = blockIdx.y, ts = threadIdx.x >> 4, seg = threadIdx.x & 15;
   const long long start = a.start[b], end = start + min(a.n_rows[b], a.most);
   long long page, tok;
-  if (!page_of(a, b, start, end, &page, &tok) || page < 0 || page >= a.pool_pages) return;
+  if (!page_of(a, b, start, end, &page, &tok)) return;
   const bool is_new = tok >= start && tok < end;
-  const long long slot = (page * a.Hkv + h) * TW_PAGE + ts;
-  uint4 rk = make_uint4(0u, 0u, 0u, 0u), rv = rk;
+  // rows, then the page's bounds, on their way before anything waits: a step's few rows are all trips to memory
+  uint4 rk = make_uint4(0u, 0u, 0u, 0u), rv = rk, ob = rk;
   if (is_new) {
     const long long row = ((long long)a.offsets[b] + (tok - start)) * a.Hkv + h;
     rk = tw_ld_stream(a.k_new + row * 16 + seg);
     rv = tw_ld_stream(a.v_new + row * 16 + seg);
   }
+  if (page < 0 || page >= a.pool_pages) return;
+  const long long slot = (page * a.Hkv + h) * TW_PAGE + ts;
+  const int which = threadIdx.x >> 4;            // of the threads that write bounds: 0 the lower ones, 1 the upper ones
+  uint4* const bounds = a.bounds + (page * a.Hkv + h) * 32 + which * 16 + seg;
+  const bool begun = (tok - ts) < start;         // the page has tokens before the new ones
+  if (a.bounds && threadIdx.x < 32 && begun) ob = *bounds;
   float x[8], y[8];
   tw_unpack8(rk, x);
   tw_unpack8(rv, y);
@@ -64,22 +70,25 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(RowArgs4 a) {
   if (!a.bounds) return;
 
   // element-wise bounds of K over the page's tokens, of which those before `start` have theirs there
-  __shared__ float red[4][2][16][8];
+  __shared__ __align__(16) float red[4][2][16][8];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  float lo[8], hi[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float lo = is_new ? x[i] : __builtin_inff(), hi = is_new ? x[i] : -__builtin_inff();
-    lo = fminf(lo, __shfl_xor(lo, 16, 64)); hi = fmaxf(hi, __shfl_xor(hi, 16, 64));
-    lo = fminf(lo, __shfl_xor(lo, 32, 64)); hi = fmaxf(hi, __shfl_xor(hi, 32, 64));
-    if (lane < 16) { red[wave][0][seg][i] = lo; red[wave][1][seg][i] = hi; }
+  for (int i = 0; i < 8; ++i) {                  // the 4 token slots of this wave
+    lo[i] = is_new ? x[i] : __builtin_inff(); hi[i] = is_new ? x[i] : -__builtin_inff();
+    lo[i] = fminf(lo[i], __shfl_xor(lo[i], 16, 64)); hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], 16, 64));
+    lo[i] = fminf(lo[i], __shfl_xor(lo[i], 32, 64)); hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], 32, 64));
+  }
+  if (lane < 16) {
+    float4* to = (float4*)red[wave][0][seg];
+    to[0] = make_float4(lo[0], lo[1], lo[2], lo[3]); to[1] = make_float4(lo[4], lo[5], lo[6], lo[7]);
+    to = (float4*)red[wave][1][seg];
+    to[0] = make_float4(hi[0], hi[1], hi[2], hi[3]); to[1] = make_float4(hi[4], hi[5], hi[6], hi[7]);
   }
   __syncthreads();
   if (threadIdx.x >= 32) return;
-  const int which = threadIdx.x >> 4;            // 0: lower bounds, 1: upper ones
-  uint4* at = a.bounds + (page * a.Hkv + h) * 32 + which * 16 + seg;
   float old[8];
-  const bool begun = (tok - ts) < start;
-  tw_unpack8(begun ? *at : make_uint4(0u, 0u, 0u, 0u), old);
+  tw_unpack8(ob, old);
   uint32_t w[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -89,7 +98,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(RowArgs4 a) {
     if (begun) v = which ? fmaxf(v, old[i]) : fminf(v, old[i]);
     w[i] = __float_as_uint(v);                   // of bf16 values: the upper 16 bits are all of it
   }
-  *at = make_uint4(w[0] >> 16 | (w[1] & 0xFFFF0000u), w[2] >> 16 | (w[3] & 0xFFFF0000u), w[4] >> 16 | (w[5] & 0xFFFF0000u), w[6] >> 16 | (w[7] & 0xFFFF0000u));
+  *bounds = make_uint4(w[0] >> 16 | (w[1] & 0xFFFF0000u), w[2] >> 16 | (w[3] & 0xFFFF0000u), w[4] >> 16 | (w[5] & 0xFFFF0000u), w[6] >> 16 | (w[7] & 0xFFFF0000u));
 }
 
 // 8 codes times scale plus zero, rounded to bf16 (code * scale is exact in fp32, so there is one rounding before that).

@@ -103,8 +103,8 @@ def test_the_binding_refuses(T):
     B = T.binding
     i32 = lambda *n: torch.zeros(*n, dtype=torch.int32)
     f32 = lambda *n: torch.zeros(*n)
-    with pytest.raises(AssertionError):                            # on the CPU
-        B._codes(torch.zeros(4, 8, 16, 64, dtype=torch.uint8), (64,))
+    with pytest.raises(AssertionError, match="as large as K's"):    # on the CPU
+        B._v_pools(_kv(T), torch.zeros(64, 8, 16, 64, dtype=torch.uint8), torch.zeros(64, 8, 16, 4, 2, dtype=torch.float16))
     kv = _kv(T, batch=3, max_pages=4)
     for bad in (dict(mass_in=f32(3, 32)), dict(mass_out=f32(2, 64))):
         a = dict(mass_in=f32(3, 64), mass_out=f32(3, 64), **{})

@@ -515,30 +515,29 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(Kv4Args a) {
 }
 
 // ------------------------------------------------------------------------------------------------------ many rows
-// More than 32 rows: a workgroup takes M = 32 * WR of them, whose waves share a tile of 64 tokens in LDS: each turns one page's codes
-// into operands, K's to bf16 numbers 0 .. 15, V's to fp16 values, while the tile before is computed (as in new_tokens.hip: 32 rows to a
-// wave, WT waves that split a tile's tokens).  The scores' group products T_g are two v_mfma_f32_32x32x16_bf16 each, scaled and summed by
-// one fma per score and group; what the zeros add, sum_g z_g Q_g, is two more products for all groups: z (11 bits) in two bf16 parts, Q_g
-// in three.
+// More than 256 rows: a workgroup takes 128 of them, 32 to a wave, and its waves share a tile of 64 tokens in LDS: each turns one page's
+// codes into operands, K's to bf16 numbers 0 .. 15, V's to fp16 values, between the products of the tile before (rows of operands and
+// their reads as in new_tokens.hip).  The scores' group products T_g = sum_d q_d c_d are two v_mfma_f32_32x32x16_bf16 each, scaled and
+// summed by one fma per score and group; what the zeros add, sum_g z_g Q_g, is two more products for all groups: z (11 bits) in two
+// bf16 parts, Q_g in three.
 struct Kv4WideArgs : Kv4Args {
   static constexpr int TILE_PAGES = 4, MIN_TILES = 2, PAD = 3;
 };
-constexpr int WIDE_V = 64 * 256, WIDE_Z = 2 * WIDE_V, WIDE_S = WIDE_Z + 64 * 16, WIDE_BUF = WIDE_S + 64 * 8;
+constexpr int WIDE_M = 128, WIDE_V = 64 * 256, WIDE_Z = 2 * WIDE_V, WIDE_S = WIDE_Z + 64 * 16, WIDE_BUF = WIDE_S + 64 * 8;
 
-template <int WR, int WT, bool SPLIT>
+template <bool SPLIT>
 __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Piece& it, unsigned char (&buf0)[WIDE_BUF], unsigned char (&buf1)[WIDE_BUF],
                                             int lane, int wave) {
-  constexpr int M = 32 * WR, MT = 2 / WT;
-  static_assert(WR * WT == 4, "a page of the tile to a wave");
-  const int wr = wave / WT, wt = wave % WT, half = lane >> 5;
+  constexpr int M = WIDE_M, MT = 2;
+  const int half = lane >> 5;
   const int b = __builtin_amdgcn_readfirstlane(it.b), rb = __builtin_amdgcn_readfirstlane(it.rb), h = __builtin_amdgcn_readfirstlane(it.h);
   const int n = __builtin_amdgcn_readfirstlane(it.n), len = __builtin_amdgcn_readfirstlane(it.len), off = __builtin_amdgcn_readfirstlane(it.off);
-  const int ctx = len - n, rows = n * a.G, row = rb * M + wr * 32 + (lane & 31);
+  const int ctx = len - n, rows = n * a.G, row = rb * M + wave * 32 + (lane & 31);
   const bool live = row < rows;
   const int tok = min(row, rows - 1) >> a.lgG, pos = ctx + tok;
   const long long qrow = (long long)(off + tok) * a.Hq + h * a.G + (min(row, rows - 1) & (a.G - 1));
   const int p_lo = ctx + ((rb * M) >> a.lgG), p_hi = ctx + ((min(rb * M + M, rows) - 1) >> a.lgG);
-  const int w_lo = ctx + (min(rb * M + wr * 32, rows - 1) >> a.lgG), w_hi = ctx + (min(rb * M + wr * 32 + 31, rows - 1) >> a.lgG);
+  const int w_lo = ctx + (min(rb * M + wave * 32, rows - 1) >> a.lgG), w_hi = ctx + (min(rb * M + wave * 32 + 31, rows - 1) >> a.lgG);
   const auto sp = span_of<MODE_WINDOW>(a, len, p_lo, p_hi);
   const int u0 = SPLIT ? min(sp.tiles, __builtin_amdgcn_readfirstlane(it.from)) : 0, u1 = SPLIT ? min(sp.tiles, __builtin_amdgcn_readfirstlane(it.to)) : sp.tiles;
   const bool whole = !SPLIT || it.to - it.from == it.tiles;
@@ -574,8 +573,8 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Piece& i
   // piece ^ (4 (row % 4) + 2 (row / 4 % 2)).  This lane stages token lane / 4 of its wave's page, group lane % 4.
   const int st = lane >> 2, sg = lane & 3, v_order = ((st & 3) << 2) | ((st >> 2 & 1) << 1);
   // of piece 2 s + half of K's row (32 s changes the bits of the piece), of the 4 tokens and 16 dims that 16 lanes take of V's (64 d)
-  const unsigned k_at = (unsigned)((wt * (64 / WT) + (lane & 31)) * 256 + ((half ^ (lane & 15)) << 4));
-  const unsigned v_at = (unsigned)(WIDE_V + (wt * (64 / WT) + 4 * half + ((lane & 15) >> 2)) * 256 +
+  const unsigned k_at = (unsigned)((lane & 31) * 256 + ((half ^ (lane & 15)) << 4));
+  const unsigned v_at = (unsigned)(WIDE_V + (4 * half + ((lane & 15) >> 2)) * 256 +
                                    (((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ ((lane & 15) >> 2 << 2) ^ (half << 1)) << 4) + (lane & 1) * 8);
 
   // ---- page ids of 64 tiles at a time: lane k holds those of tile base + k
@@ -656,8 +655,7 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Piece& i
     const uint32_t kw[4] = {x.k.x, x.k.y, x.k.z, x.k.w}, vw[4] = {x.v.x, x.v.y, x.v.z, x.v.w};
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      const int blk = WT == 2 ? wt : mt;
-      const tw_bf16x8 z = *(const tw_bf16x8*)(buf + WIDE_Z + (blk * 32 + (lane & 31)) * 16);
+      const tw_bf16x8 z = *(const tw_bf16x8*)(buf + WIDE_Z + (mt * 32 + (lane & 31)) * 16);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[mt][r] = 0.f;
       s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(z, qz[0], s[mt], 0, 0, 0);
@@ -670,11 +668,11 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Piece& i
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const tw_bf16x8*)(buf + (k_rd ^ (unsigned)(32 * (2 * g + k))) + mt * 32 * 256), qf[2 * g + k], t, 0, 0, 0);
-        if (MT == 1 || g % 2 == 1) {
-          const int i = MT == 1 ? g : 2 * mt + g / 2;
+        if (g % 2 == 1) {
+          const int i = 2 * mt + g / 2;
           stage_word(then, kw[i], vw[i], i, sz);
         }
-        const unsigned char* sc = buf + WIDE_S + ((g * 2 + blk) * 2 + half) * 32;
+        const unsigned char* sc = buf + WIDE_S + ((g * 2 + mt) * 2 + half) * 32;
         const uint4 x = *(const uint4*)sc, y = *(const uint4*)(sc + 16);
         const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -700,7 +698,7 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Piece& i
         const uint32_t see = low16(pos + 1 - t) & (~low16(pos - a.window + 1 - t) | low16(a.sinks - t));
         if (held >> j & 1u) vis |= (unsigned long long)see << (16 * j);
       }
-      vis >>= wt * (64 / WT) + 4 * half;
+      vis >>= 4 * half;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         const uint32_t w = (uint32_t)(vis >> (32 * mt));
@@ -790,34 +788,11 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Piece& i
     }
   }
 
-  // ---- the waves' states of the same rows merged
+  // ---- the row's sum, and the row
   m = m_log2();
   {
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-  }
-  if constexpr (WT > 1) {
-    __syncthreads();                             // the tiles have been read
-    float* part = (float*)(buf0 + wr * 16384);
-    float2* ml = (float2*)buf1 + wr * 32;
-    static_assert(WR * 16384 <= WIDE_BUF, "one partial per row wave");
-    if (wt == 1) {
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) part[(d * 16 + r) * 64 + lane] = o[d][r];
-      if (half == 0) ml[lane] = make_float2(m, l);
-    }
-    __syncthreads();
-    if (wt != 0) return;
-    const float2 x = ml[lane & 31];
-    const float mn = fmaxf(m, x.x), s0 = __builtin_amdgcn_exp2f(m - mn), s1 = __builtin_amdgcn_exp2f(x.x - mn);
-    l = l * s0 + x.y * s1;
-    m = mn;
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[d][r] = o[d][r] * s0 + part[(d * 16 + r) * 64 + lane] * s1;
   }
   if (!live) return;
   if (whole) {
@@ -835,7 +810,7 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Piece& i
     if (a.lse && half == 0) a.lse[qrow] = row_lse(m, l);
     return;
   }
-  const long long prow = (long long)it.slot * M + wr * 32 + (lane & 31);
+  const long long prow = (long long)it.slot * M + wave * 32 + (lane & 31);
   float4* acc = (float4*)(a.ws_acc + prow * 128);
 #pragma unroll
   for (int d = 0; d < 4; ++d)
@@ -844,33 +819,42 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Piece& i
   if (half == 0) a.ws_ml[prow] = make_float2(m, l);
 }
 
-template <int WR, int WT, bool SPLIT>
+template <bool SPLIT>
 __global__ __launch_bounds__(256, 2) void kv4_wide_kernel(Kv4WideArgs a) {
-  constexpr int M = 32 * WR;
+  constexpr int M = WIDE_M;
   __shared__ __align__(1024) unsigned char buf0[WIDE_BUF];
   __shared__ __align__(1024) unsigned char buf1[WIDE_BUF];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   if (!SPLIT) {
     Piece it;
-    if (whole_piece<M>(a, &it)) attend_wide<WR, WT, SPLIT>(a, it, buf0, buf1, lane, wave);
+    if (whole_piece<M>(a, &it)) attend_wide<SPLIT>(a, it, buf0, buf1, lane, wave);
     return;
   }
-  for_pieces<M>(a, lane, [&](const Piece& it, int ln) { attend_wide<WR, WT, SPLIT>(a, it, buf0, buf1, ln, wave); });
+  for_pieces<M>(a, lane, [&](const Piece& it, int ln) { attend_wide<SPLIT>(a, it, buf0, buf1, ln, wave); });
 }
 
 template <int M, int LANES>
 __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Args a) { join_shares<M, LANES>(a); }
 
 // ---------------------------------------------------------------- host side
-int rows_per_block4(long long rows) { return rows <= 16 ? 16 : rows <= 64 ? 32 : 128; }
+// Rows to a workgroup.  us with blocks of 32 / 64 (as 128, two waves to 32 rows) / 128 rows, of a KV head's rows:
+//   8 sequences of 8192, 8 heads a group   24: 37 / 57 / 72    64: 51 / 61 / 74    128: 92 / 105 / 81   256: 135 / 185 / 140   1024: 501 / 554 / 413
+//   one of 4096, 4 heads a group           24: 15.2 / 16.2 / 15.8                  128: 21.4 / 23.8 / 22.1                      512: 32.7 / 39.0 / 35.5
+//   16 of 2048, 4 heads a group            24: 28 / 36 / 42    64: 35 / 40 / 46    128: 42 / 62 / 52    256: 78 / 82 / 81       512: 147 / 152 / 113
+int rows_per_block4(long long rows) { return rows <= 16 ? 16 : rows <= 256 ? 32 : WIDE_M; }
 
-// Lists that cannot be long are not cut, nor are the row blocks of prompts that fill the chip by themselves, but where single tokens may
-// stand beside a chunk (as in new_tokens.hip).  Tiles of 256 tokens (up to 32 rows) or 64.
+// Lists that cannot be long are not cut, which saves the launch that joins the parts: up to 512 tokens, 256 more for every 24 lists; at
+// most 2048, or 4096 where two lists come to a place of the chip, as ragged lengths would leave it idle with more.  Nor are the row blocks of
+// prompts that fill the chip by themselves, but where single tokens may stand beside a chunk (as in new_tokens.hip).  us, whole / cut, 8 heads:
+//   one new token each     1 sequence of 512: 8.9 / 12.3   1024: 12.4 / 12.0   2048: 20.5 / 12.0     8 of 1024: 12.5 / 13.3   2048: 22.9 / 15.8
+//                          32 of 2048: 24.5 / 26.4         4096: 47.1 / 43.9
+//   6, 4 heads a group     1 of 512: 11.4 / 14.7           1024: 16.7 / 15.2                         32 of 2048: 31.9 / 36.6  4096: 59.0 / 60.9
+//   128, 4 heads a group   1 of 256: 15.3 / 17.9           512: 24.4 / 20.3    8 of 2048: 81.4 / 81.8   4096: 153 / 144       32 of 4096: 424 / 484
 template <class A>
 bool cut_lists4(bool counted, int blocks, long long lists, long long longest) {
-  constexpr long long UNIT = 16 / A::TILE_PAGES;
-  if (longest <= std::min(8 * UNIT, UNIT * (1 + lists / 64))) return false;
+  constexpr long long UNIT = 16 / A::TILE_PAGES;             // tiles of 256 tokens
   const long long places = 2ll * tw_num_cus();
+  if (longest <= UNIT * std::min(lists >= 2 * places ? 16ll : 8ll, 2 + lists / 24)) return false;
   if (blocks < 8 || lists < places) return true;
   return counted && longest * places > 48 * UNIT * lists;
 }
@@ -896,7 +880,7 @@ int launch_kv4(const A& a, Whole whole, Cut cut, hipStream_t s) {
 
 // Places for parts: two of every workgroup that can have tiles.
 size_t part_slots4(const TwDims& d, long long rows) {
-  const int M = rows_per_block4(rows), chunk = rows <= 32 ? Kv4Args::TILE_PAGES * Kv4Args::MIN_TILES : Kv4WideArgs::TILE_PAGES * Kv4WideArgs::MIN_TILES;
+  const int M = rows_per_block4(rows), chunk = M <= 32 ? Kv4Args::TILE_PAGES * Kv4Args::MIN_TILES : Kv4WideArgs::TILE_PAGES * Kv4WideArgs::MIN_TILES;
   const long long lists = (rows + M - 1) / M * d.batch * d.Hkv, places = 2ll * tw_num_cus();
   return (size_t)(2 * std::min(places, lists * ((d.max_pages + chunk - 1) / chunk)));
 }
@@ -942,7 +926,6 @@ extern "C" int twilight_kv4_attention(const twilight_kv_t* kv, const void* vq_po
   switch (M) {
     case 16: return launch_kv4<16>((const Kv4Args&)a, kv4_attention_kernel<1, false>, kv4_attention_kernel<1, true>, s);
     case 32: return launch_kv4<32>((const Kv4Args&)a, kv4_attention_kernel<2, false>, kv4_attention_kernel<2, true>, s);
-    case 64: return launch_kv4<64>(a, kv4_wide_kernel<2, 2, false>, kv4_wide_kernel<2, 2, true>, s);
-    default: return launch_kv4<128>(a, kv4_wide_kernel<4, 1, false>, kv4_wide_kernel<4, 1, true>, s);
+    default: return launch_kv4<WIDE_M>(a, kv4_wide_kernel<false>, kv4_wide_kernel<true>, s);
   }
 }

@@ -156,6 +156,21 @@ def test_mass_of_long_context():
     weigh(Cache([30000], 8, 1, seed=4), [20], 20, 20000, 10)
 
 
+@KIND
+@pytest.mark.parametrize("hq,hkv", [(8, 8), (32, 8), (8, 1), (10, 5)])
+@pytest.mark.parametrize("new,window,sinks", [(17, NONE, 0), (33, 40, 70), (95, 200, 5), (200, NONE, 0)])
+def test_mass_of_several_over_many_pages(kind, hq, hkv, new, window, sinks):
+    """Four pages to a workgroup: rows in blocks of 16 and 32, the last ones short, and lengths that end inside the four."""
+    lens = [5003, 0, 31, 4080]
+    weigh(kind(lens, hq, hkv, seed=new), [min(new, n) - (b == 3) for b, n in enumerate(lens)], new, window, sinks, 0.5, seed=hq, gap=2)
+
+
+@KIND
+def test_mass_of_few_over_many_pages(kind):
+    for hq, hkv, many, window, sinks in ((8, 8, [9, 3], NONE, 0), (6, 3, [1, 8], 100, 30), (64, 16, [4, 4], 3000, 0), (8, 1, [2, 0], 7, 7000)):
+        weigh(kind([6001, 4095], hq, hkv, seed=hkv), many, max(many), window, sinks, 1.0, seed=hkv)
+
+
 # -------------------------------------------------------------------------------------------------------------- what to keep
 def keep_reference(mass, n, budget, sinks, recent, stride):
     k = max(0, min(budget, n, stride))
@@ -372,6 +387,19 @@ def test_a_captured_step_of_mass_and_choice():
         assert torch.equal(at.out, eager[1].out) and torch.equal(mass.mass, eager[2].mass) and cache.seq_lens.tolist() == list(n)
         assert torch.equal(cache.seq_lens, eager[0].seq_lens) and torch.equal(cache.kq_pool, eager[0].kq_pool)
         assert torch.equal(cache.vq_meta.view(torch.int16), eager[0].vq_meta.view(torch.int16))
+
+
+def test_a_cache_with_bounds_in_four_bits_is_not_cut_down():
+    """The codes do not give the rows' bounds back: refused before anything moves."""
+    import paper_2502_02770_amd as T
+    cache = T.PagedKV4(8, 2, torch.arange(4, dtype=torch.int32).view(1, 4), torch.tensor([50], dtype=torch.int32), 4, with_bounds=True)
+    x = queries(50, 2, 1)
+    cache.append(x, x, i32([0]), i32([50]), i32([0]), 50)
+    mass = T.TokenMass(cache)
+    had = [t.clone() for t in (cache.kq_pool, cache.vq_pool, cache.page_minmax, mass.mass)]
+    with pytest.raises(RuntimeError):
+        mass.evict(i32([20]))
+    assert all(torch.equal(t, h) for t, h in zip((cache.kq_pool, cache.vq_pool, cache.page_minmax, mass.mass), had)) and cache.seq_lens.tolist() == [50]
 
 
 def test_two_streams_with_a_workspace_each():

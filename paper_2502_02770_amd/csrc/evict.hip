@@ -302,12 +302,16 @@ __device__ __forceinline__ Digit find_digit(const uint32_t* hist, uint32_t want,
   return {scratch[16], scratch[17]};
 }
 
-// Keys of a wave's rows of 64 consecutive tokens: row i begins at t0 + 64 i, a lane has one token of each.
+// A wave's rows of 64 consecutive tokens: row i begins at t0 + 64 i, a lane has one token of each.  Their weights, and the keys.
 template <int E>
-__device__ __forceinline__ void load_keys64(const float* row, int t0, int lo, int hi, int len, float (&x)[E], uint32_t (&key)[E]) {
+__device__ __forceinline__ void load_rows64(const float* row, int t0, int len, float (&x)[E]) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 0; i < E; ++i) x[i] = t0 + 64 * i + lane < len ? row[t0 + 64 * i + lane] : 0.f;
+}
+template <int E>
+__device__ __forceinline__ void keys_of64(int t0, int lo, int hi, const float (&x)[E], uint32_t (&key)[E]) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     const int t = t0 + 64 * i + lane;
@@ -369,7 +373,8 @@ __global__ __launch_bounds__(THREADS) void keep_whole_kernel(KeepArgs a) {
   const int t0 = wave * 64 * E, lo = s.first, hi = s.len - s.last;
   float x[E];
   uint32_t key[E];
-  load_keys64<E>(a.mass + (long long)b * a.max_pages * TW_PAGE, t0, lo, hi, s.len, x, key);
+  load_rows64<E>(a.mass + (long long)b * a.max_pages * TW_PAGE, t0, s.len, x);
+  keys_of64<E>(t0, lo, hi, x, key);
   uint32_t prefix = ~0u, want = (uint32_t)s.want;            // (no key is this large)
   if (s.want > 0) {
 #pragma unroll
@@ -416,7 +421,7 @@ __global__ __launch_bounds__(KEEP_THREADS) void keep_chunk_kernel(KeepArgs a) {
   float x[8];
   uint32_t key[8];
   // (a chunk of one block, as those of up to 128 x 8192 tokens are, is asked for at once)
-  if (a.blocks == 1) load_keys64<8>(row, t0 + wave * 512, lo, hi, s.len, x, key);
+  if (a.blocks == 1) load_rows64<8>(row, t0 + wave * 512, s.len, x);
   uint32_t prefix = 0, want = (uint32_t)s.want, above = 0, ties = 0;
   if (PASS > 0 && s.want > 0) {
     constexpr int D = PASS > 0 ? PASS - 1 : 0;   // the digit to find
@@ -424,19 +429,27 @@ __global__ __launch_bounds__(KEEP_THREADS) void keep_chunk_kernel(KeepArgs a) {
     const uint32_t* h = all + 2048 * D;
     uint32_t n0 = 0, n1 = 0, mine0 = 0, mine1 = 0;           // this thread's two bins, or the one of the last digit: of all chunks, and of this
     if (D < 2) {                                 // one, or of all before this one
-#pragma unroll 8
-      for (int k = 0; k < chunks; ++k) {
-        const uint2 y = *(const uint2*)(h + (long long)k * CHUNK_WORDS + 2 * tid);
-        n0 += y.x; n1 += y.y;
-        if (k == c) { mine0 = y.x; mine1 = y.y; }
+      for (int k0 = 0; k0 < chunks; k0 += 16) {  // (16 at once, those behind the last not asked for: each is a trip past this XCD's L2)
+        uint2 y[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) y[k] = k0 + k < chunks ? *(const uint2*)(h + (long long)(k0 + k) * CHUNK_WORDS + 2 * tid) : make_uint2(0u, 0u);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          n0 += y[k].x; n1 += y[k].y;
+          if (k0 + k == c) { mine0 = y[k].x; mine1 = y[k].y; }
+        }
       }
       *(uint2*)(hist + 2 * tid) = make_uint2(n0, n1);
     } else {
-#pragma unroll 8
-      for (int k = 0; k < chunks; ++k) {
-        const uint32_t y = h[(long long)k * CHUNK_WORDS + tid];
-        n0 += y;
-        mine0 += k < c ? y : 0u;
+      for (int k0 = 0; k0 < chunks; k0 += 16) {
+        uint32_t y[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) y[k] = k0 + k < chunks ? h[(long long)(k0 + k) * CHUNK_WORDS + tid] : 0u;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          n0 += y[k];
+          mine0 += k0 + k < c ? y[k] : 0u;
+        }
       }
       hist[tid] = n0;
       hist[tid + 1024] = 0;
@@ -471,7 +484,8 @@ __global__ __launch_bounds__(KEEP_THREADS) void keep_chunk_kernel(KeepArgs a) {
     for (int k = 0; k < a.blocks; ++k) {
       const int t = t0 + k * SUB + wave * 512;
       if (t >= hi) break;
-      if (a.blocks > 1) load_keys64<8>(row, t, lo, hi, s.len, x, key);
+      if (a.blocks > 1) load_rows64<8>(row, t, s.len, x);
+      keys_of64<8>(t, lo, hi, x, key);
       count_digit<PASS, 8>(hist, key, prefix);
     }
     __syncthreads();
@@ -483,7 +497,8 @@ __global__ __launch_bounds__(KEEP_THREADS) void keep_chunk_kernel(KeepArgs a) {
   for (int k = 0; k < a.blocks; ++k) {
     const int at = t0 + k * SUB, t = at + wave * 512;
     if (at >= s.len) break;
-    if (a.blocks > 1) load_keys64<8>(row, t, lo, hi, s.len, x, key);
+    if (a.blocks > 1) load_rows64<8>(row, t, s.len, x);
+    keys_of64<8>(t, lo, hi, x, key);
     const uint32_t mine = count_rows64<8>(key, prefix);
     if ((tid & 63) == 0) scratch[wave] = mine;
     __syncthreads();

@@ -21,17 +21,13 @@ __device__ __forceinline__ __half tw_f32_to_f16_rne(float x) {
   return __float2half_rn(x);
 }
 
+// gmn, gmx: least and largest of the group's values
 template <int BITS>
-__device__ __forceinline__ void tw_quantize_lane8(const float (&x)[8], int seg, uint32_t* word_out, uint32_t* word2_out,
-                                                  uint32_t* meta_out) {
+__device__ __forceinline__ void tw_quantize_lane8_in(const float (&x)[8], float gmn, float gmx, int seg, uint32_t* word_out, uint32_t* word2_out,
+                                                     uint32_t* meta_out) {
   constexpr float kLevels = (float)((1 << BITS) - 1);
   // fp32 nearest to 1/levels
   constexpr float kInvLevels = BITS == 4 ? 0x1.111112p-4f : (BITS == 2 ? 0x1.555556p-2f : 0x1.010102p-8f);
-  float lmn = x[0], lmx = x[0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) { lmn = fminf(lmn, x[i]); lmx = fmaxf(lmx, x[i]); }
-  const float gmn = tw_quad_min(lmn), gmx = tw_quad_max(lmx);
-
   const __half hs = tw_f32_to_f16_rne(__fmul_rn(__fsub_rn(gmx, gmn), kInvLevels));
   const __half hz = tw_f32_to_f16_rne(gmn);
   const float sf = __half2float(hs), zf = __half2float(hz);
@@ -63,5 +59,14 @@ __device__ __forceinline__ void tw_quantize_lane8(const float (&x)[8], int seg, 
   }
   *word_out = word; *word2_out = word2;
   *meta_out = (uint32_t)__half_as_ushort(hs) | ((uint32_t)__half_as_ushort(hz) << 16);
+}
+
+template <int BITS>
+__device__ __forceinline__ void tw_quantize_lane8(const float (&x)[8], int seg, uint32_t* word_out, uint32_t* word2_out,
+                                                  uint32_t* meta_out) {
+  float lmn = x[0], lmx = x[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) { lmn = fminf(lmn, x[i]); lmx = fmaxf(lmx, x[i]); }
+  tw_quantize_lane8_in<BITS>(x, tw_quad_min(lmn), tw_quad_max(lmx), seg, word_out, word2_out, meta_out);
 }
 #endif

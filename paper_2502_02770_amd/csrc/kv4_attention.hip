@@ -17,8 +17,14 @@
 // The A operand of the scores takes its 16 tokens as four of each of the tile's four pages (token 4 n + i of page j in row 4 j + i of
 // step n), so that the quarter wave j holds all scores of page j's tokens, a row of q in each lane: what the transposed read of V's
 // codes (ds_read_b64_tr_b4: a lane gets 16 tokens of one dim) wants its weights to be.  K's codes go to registers, 16 bytes of a
-// group to a lane, and are exchanged between the quarters (four permlane swaps); V's codes and K's (s, z) go to LDS without passing
-// registers, V's (s, z) through them, transposed.  The next tile's loads are issued before a tile is computed.
+// group to a lane, and are exchanged between the quarters (four permlane swaps; through LDS they cost as much); V's codes go to LDS without
+// passing registers, both (s, z) through them, transposed.  The next tile's loads are issued while a tile is computed.
+//
+// Measured: 8 sequences of 32768, one token, 4 heads a group (M = 16) 76 us for 336 MB, 4.4 TB/s: what is left is issue beside the memory
+// (vector 0.5 and matrix 0.1 of a SIMD's time).  64 sequences of 1000 to 32001, 4 tokens, 8 heads a group (M = 32) 389 us for 855 MB:
+// issue (some 750 vector instructions, 0.6, and 72 matrix ones, 0.2, to a tile and wave), of which half prepare codes and (s, z) for 32 rows.
+// Whole waves of more rows would spread that (64 would not fit beside the outputs; 128 share it through LDS: below).  One sequence
+// of 4096 11.6 us: two launches, 9 and 4, whose trips to memory follow each other.
 #include "kv4_common.h"
 #include "new_tokens_plan.h"
 

@@ -283,6 +283,25 @@ def test_append_is_kquant_append_for_k_and_for_v(lens, many, hkv):
         assert torch.equal(bits(a), bits(b))
 
 
+def test_append_of_zeros_of_both_signs_and_of_the_smallest_numbers():
+    """The least and the largest are found on the numbers' bits: what compares equal or is below the normal range has to come out alike."""
+    import paper_2502_02770_amd as T
+    c, k, v = _store([3], [40], 2, seed=8)
+    g = torch.Generator("cuda").manual_seed(8)
+    small = torch.tensor([0, -0x8000, 1, -0x7FFF, 0x7F, -0x7F81, 0x80, -0x7F80], dtype=torch.int16, device="cuda").view(torch.bfloat16)
+    for x, many in ((k, 2), (v, 8)):
+        x.copy_(small[torch.randint(0, many, x.shape, device="cuda", generator=g)])
+    got = [c.kc.clone(), c.km.clone(), c.kc.clone(), c.km.clone(), c.bounds.clone()]
+    want = [t.clone() for t in got]
+    make = lambda codes, meta, bounds: T.make_kv(1, 2, 2, c.max_pages, c.kc.shape[0], c.table, c.seq, None, None, codes, meta, bounds)
+    T.twilight_kquant_append(make(want[0], want[1], want[4]), k, None, i32([3]), i32([40]), i32([0]), 40)
+    T.twilight_kquant_append(make(want[2], want[3], torch.zeros_like(want[4])), v, None, i32([3]), i32([40]), i32([0]), 40)
+    T.twilight_kv4_append(make(got[0], got[1], got[4]), got[2], got[3], k, v, i32([3]), i32([40]), i32([0]), 40)
+    bits = lambda t: t.view(torch.int16) if t.dtype != torch.uint8 else t
+    for a, b in zip(got, want):
+        assert torch.equal(bits(a), bits(b))
+
+
 def test_append_to_pages_that_are_not_there_and_without_bounds():
     import paper_2502_02770_amd as T
     c, k, v = _store([0], [100], 2, seed=1, bounds=False)

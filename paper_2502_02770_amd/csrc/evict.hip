@@ -19,6 +19,10 @@ constexpr float kScaleLog2 = 0.08838834764831845f * 1.4426950408889634f;   // lo
 // the head's rows (query heads x new tokens) by 16: S = Q K^T, v_mfma_f32_16x16x32_bf16 (codes as 128 + c in bf16, as in
 // kv4_attention.hip), a lane has one token and four rows.  What comes next is asked for ahead: with up to 16 rows the next head's K and
 // queries, with more (MANY) the next rows.  The waves' sums are added in their order, so that the result does not depend on timing.
+//
+// Measured, 32 heads over 8: one token of 8 x 32768 of codes 42 us for 170 MB, 4.1 TB/s, beside vector issue 0.75 of the time; 64 tokens of 2 x 16001
+// of bf16 41.7 us for 17 GFLOP and 131 MB: a workgroup's way through 256 rows of two heads (a score is an fma, an exponential, a maximum and a sum), on
+// two workgroups to a CU.  One token of 4096 4.5 us: page table, K and queries, sums one after the other.
 struct MassArgs {
   const uint4* q;
   const float* lse;
@@ -249,6 +253,10 @@ __global__ __launch_bounds__(256, 2) void attention_mass_kernel(MassArgs a) {
 // The budget's share of a sequence's tokens: its first ones, its latest ones, and of those between the heaviest.  A weight's bits in
 // the order of the numbers are a key; the key of the last token kept is found by three histograms (of 11, 11 and 10 bits), each of
 // the tokens that share the bits found before, and equal keys go to the lowest positions.
+//
+// Up to 8192 tokens are one launch, a sequence to a workgroup, all in registers: 7.6 us for 2049, most of it three rounds of counting in LDS and
+// finding a digit.  More are four launches of 4 to 9 us (16 x 32768 22 us, 3 x 200003 29 us): at so few bytes (4 a token) trips to memory, since every
+// launch reads the counts of all of a row's chunks that the one before left.
 struct KeepArgs {
   const float* mass;
   const int32_t* seq_lens;
@@ -521,20 +529,21 @@ void keep_chunks(const TwDims& d, int* chunks, int* blocks) {
   *chunks = (int)((subs + *blocks - 1) / *blocks);
 }
 
-template <bool CODES>
-int launch_mass(const MassArgs& a, int batch, hipStream_t s) {
-  tw_prof_before(TW_K_MASS, s);
-  const long long pages = (long long)a.max_pages * batch;
-  const dim3 one((unsigned)a.max_pages, (unsigned)batch), four((unsigned)((a.max_pages + 3) / 4), (unsigned)batch), wg(256);
-  if ((long long)a.max_new * a.G > 16) {
-    if (pages <= 2ll * tw_num_cus()) TW_LAUNCH((attention_mass_kernel<CODES, 1, true>), one, wg, 0, s, a);
-    else TW_LAUNCH((attention_mass_kernel<CODES, 4, true>), four, wg, 0, s, a);
-  } else if (pages <= 2ll * tw_num_cus()) {
-    TW_LAUNCH((attention_mass_kernel<CODES, 1, false>), one, wg, 0, s, a);
-  } else {
-    TW_LAUNCH((attention_mass_kernel<CODES, 4, false>), four, wg, 0, s, a);
-  }
-  return tw_prof_after(s);
+// Pages to a workgroup: few where that leaves CUs without one, more for the loads (and, with many rows, the queries) that they share.  us with 1 / 2 / 4 /
+// 8 pages, 32 heads over 8, by all sequences' pages:
+//                     256                    512                     1024                   2002                   4096 or 16384
+//   1 token    bf16   6.2  6.6  8.2 13.3     7.9  7.3 10.8 17.3      12.2 11.6 11.5 17.9    21.5 19.8 19.9 19.3    154  142  139  138
+//   1 token    codes  6.4  6.2  6.5  8.4     6.1  6.4  6.3  8.3       6.6  6.2  6.4  8.5     9.9  8.3  8.7  9.7    62.9 47.6 41.8 44.8
+//   64 tokens  bf16  15.3 19.1 30.4 51.6    20.8 19.5 31.1 51.7      38.3 27.1 32.0 52.3    72.3 48.3 42.6 53.5    144  94.8 80.2 75.9
+//   64 tokens  codes 16.7 21.4 34.9  109    22.1 22.3 34.8  110      42.6 30.6 37.0  114    78.9 55.9 50.2  117    149  107  94.6 187
+template <bool CODES, bool MANY>
+void launch_mass(const MassArgs& a, int batch, hipStream_t s) {
+  const long long pages = (long long)a.max_pages * batch, cus = tw_num_cus();
+  auto grid = [&](int n) { return dim3((unsigned)((a.max_pages + n - 1) / n), (unsigned)batch); };
+  const dim3 wg(256);
+  if (pages <= 2 * cus) TW_LAUNCH((attention_mass_kernel<CODES, 1, MANY>), grid(1), wg, 0, s, a);
+  else if (pages <= 4 * cus) TW_LAUNCH((attention_mass_kernel<CODES, 2, MANY>), grid(2), wg, 0, s, a);
+  else TW_LAUNCH((attention_mass_kernel<CODES, 4, MANY>), grid(4), wg, 0, s, a);
 }
 
 }  // namespace
@@ -564,7 +573,12 @@ extern "C" int twilight_attention_mass(const twilight_kv_t* kv, const void* q, c
   a.seq_lens = kv->seq_lens; a.n_new = n_new; a.offsets = new_offsets; a.mass_in = mass_in; a.mass_out = mass_out;
   a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.G; a.lgG = __builtin_ctz(d.G); a.max_pages = d.max_pages; a.max_new = max_new;
   a.window = std::min(window, most); a.sinks = std::min(num_sinks, most); a.pool_pages = (unsigned)d.pool_pages; a.decay = decay;
-  return codes ? launch_mass<true>(a, d.batch, (hipStream_t)stream) : launch_mass<false>(a, d.batch, (hipStream_t)stream);
+  hipStream_t s = (hipStream_t)stream;
+  const bool many = (long long)max_new * d.G > 16;
+  tw_prof_before(TW_K_MASS, s);
+  if (codes) many ? launch_mass<true, true>(a, d.batch, s) : launch_mass<true, false>(a, d.batch, s);
+  else many ? launch_mass<false, true>(a, d.batch, s) : launch_mass<false, false>(a, d.batch, s);
+  return tw_prof_after(s);
 }
 
 extern "C" int twilight_keep_tokens(const twilight_kv_t* kv, const float* mass, const int32_t* budget, int32_t num_sinks, int32_t num_recent,

@@ -21,10 +21,10 @@
 // passing registers, both (s, z) through them, transposed.  The next tile's loads are issued while a tile is computed.
 //
 // Measured: 8 sequences of 32768, one token, 4 heads a group (M = 16) 76 us for 336 MB, 4.4 TB/s: what is left is issue beside the memory
-// (vector 0.5 and matrix 0.1 of a SIMD's time).  64 sequences of 1000 to 32001, 4 tokens, 8 heads a group (M = 32) 389 us for 855 MB:
-// issue (some 750 vector instructions, 0.6, and 72 matrix ones, 0.2, to a tile and wave), of which half prepare codes and (s, z) for 32 rows.
-// Whole waves of more rows would spread that (64 would not fit beside the outputs; 128 share it through LDS: below).  One sequence
-// of 4096 11.6 us: two launches, 9 and 4, whose trips to memory follow each other.
+// (vector 0.53, matrix 0.10 of the time).  64 sequences of 1000 to 32001, 7 tokens, 8 heads a group (two blocks of M = 32) 389 us for 855 MB:
+// issue, some 490 vector instructions (0.6 of the time) and 72 matrix ones (0.18) to a tile and wave, half of which make codes and (s, z) into
+// operands, and that twice; one block (4 tokens) 253 us, and 149 for every further one.  Operands from LDS asked for a step ahead: 389 -> 385 us
+// and spills.  One sequence of 4096 11.6 us: two launches of 9 and 4, whose trips to memory follow each other.
 #include "kv4_common.h"
 #include "new_tokens_plan.h"
 
@@ -526,6 +526,9 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(Kv4Args a) {
 // their reads as in new_tokens.hip).  The scores' group products T_g = sum_d q_d c_d are two v_mfma_f32_32x32x16_bf16 each, scaled and
 // summed by one fma per score and group; what the zeros add, sum_g z_g Q_g, is two more products for all groups: z (11 bits) in two
 // bf16 parts, Q_g in three.
+//
+// Measured: 257 tokens of three sequences of 9001 under a window of 6001, 4 heads a group (1028 rows) 169 us, 0.45 PFLOP/s of the attention's
+// own products: vector issue 0.46 of the time (an exponential, a maximum and five fmas to a score), matrix 0.23, waits at the barrier of a tile.
 struct Kv4WideArgs : Kv4Args {
   static constexpr int TILE_PAGES = 4, MIN_TILES = 2, PAD = 3;
 };

@@ -163,12 +163,15 @@ def test_mass_of_several_over_many_pages(kind, hq, hkv, new, window, sinks):
     """Four pages to a workgroup: rows in blocks of 16 and 32, the last ones short, and lengths that end inside the four."""
     lens = [5003, 0, 31, 4080]
     weigh(kind(lens, hq, hkv, seed=new), [min(new, n) - (b == 3) for b, n in enumerate(lens)], new, window, sinks, 0.5, seed=hq, gap=2)
+    lens = [2993, 405, 3000]                     # (two pages to a workgroup)
+    weigh(kind(lens, hq, hkv, seed=new), [new, new - 1, 1], new, window, sinks, 0.5, seed=hq)
 
 
 @KIND
 def test_mass_of_few_over_many_pages(kind):
     for hq, hkv, many, window, sinks in ((8, 8, [9, 3], NONE, 0), (6, 3, [1, 8], 100, 30), (64, 16, [4, 4], 3000, 0), (8, 1, [2, 0], 7, 7000)):
         weigh(kind([6001, 4095], hq, hkv, seed=hkv), many, max(many), window, sinks, 1.0, seed=hkv)
+        weigh(kind([6001, 4095], hq, hkv, seed=hkv, max_pages=600), many, max(many), window, sinks, 1.0, seed=hkv)
 
 
 # -------------------------------------------------------------------------------------------------------------- what to keep

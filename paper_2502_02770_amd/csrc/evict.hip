@@ -16,13 +16,13 @@ constexpr float kScaleLog2 = 0.08838834764831845f * 1.4426950408889634f;   // lo
 // mass[t] = decay mass[t] + sum over new tokens i and query heads of exp(q.K_t / sqrt(128) - lse_i): K once, nothing else of the cache.
 //
 // A workgroup has PT pages of a sequence, its four waves the KV heads in turn; a wave holds its head's K of those pages and goes through
-// the head's rows (query heads x new tokens) by 16: S = Q K^T, v_mfma_f32_16x16x32_bf16 (codes as 128 + c in bf16, as in
+// the head's rows (query heads x new tokens) by 16, over bf16 and with many rows two times 16: S = Q K^T, v_mfma_f32_16x16x32_bf16 (codes as 128 + c in bf16, as in
 // kv4_attention.hip), a lane has one token and four rows.  What comes next is asked for ahead: with up to 16 rows the next head's K and
 // queries, with more (MANY) the next rows.  The waves' sums are added in their order, so that the result does not depend on timing.
 //
 // Measured, 32 heads over 8: one token of 8 x 32768 of codes 42 us for 170 MB, 4.1 TB/s, beside vector issue 0.75 of the time; 64 tokens of 2 x 16001
-// of bf16 41.7 us for 17 GFLOP and 131 MB: a workgroup's way through 256 rows of two heads (a score is an fma, an exponential, a maximum and a sum), on
-// two workgroups to a CU.  One token of 4096 4.5 us: page table, K and queries, sums one after the other.
+// of bf16 41 us for 17 GFLOP and 67 MB: a wave's way through 256 rows of two heads, of which queries on their way are 9 us (33 with the first ones kept) and
+// exponentials 4, beside one other wave of its SIMD.  One token of 4096 4.5 us: page table, K and queries, sums one after the other.
 struct MassArgs {
   const uint4* q;
   const float* lse;
@@ -114,34 +114,37 @@ __global__ __launch_bounds__(256, 2) void attention_mass_kernel(MassArgs a) {
   // Blocks of rows that see any of the pages: those at positions from the first page's start on, and not so far behind that no window reaches
   const int from = min(rows, max(0, t0 - ctx) * a.G) & ~15;
   const int to = t0 < a.sinks ? rows : (int)max(0ll, min((long long)rows, ((long long)t0 + 16 * PT - 1 + a.window - ctx) * a.G));
-  // The weights of rows r0 .. r0 + 15 on the pages
+  // The weights of NB blocks of 16 rows from row r0 on, the first of them block `block` of a step's
+  constexpr int NB = MANY && !CODES ? 2 : 1;
   auto add = [&](const Keys& x, const tw_bf16x8 (&held)[PT][4], const Rows& rs, const unsigned char* buf, int block, int r0) {
-    const int p_lo = ctx + (r0 >> a.lgG), p_hi = ctx + ((min(r0 + 16, rows) - 1) >> a.lgG);
+    const int p_lo = ctx + (r0 >> a.lgG), p_hi = ctx + ((min(r0 + 16 * NB, rows) - 1) >> a.lgG);
     const bool all = t0 + 16 * PT - 1 <= p_lo && (t0 > p_hi - a.window || t0 + 16 * PT <= a.sinks);
-    tw_bf16x8 qf[4];
+    tw_bf16x8 qf[NB][4];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const uint4 y = MANY ? *(const uint4*)(buf + 4096 * block + 256 * r16 + 16 * ((4 * g + jq) ^ r16)) : rs.q[g];
-      qf[g] = CODES ? tw_q_like_codes(y) : tw_as_bf16(y);
-    }
-    float l2[4];                                 // lse in powers of 2; infinite (weights of 0) where there is no row, or none with a weight
-    int pos[4];
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const uint4 y = MANY ? *(const uint4*)(buf + 4096 * (block + n) + 256 * r16 + 16 * ((4 * g + jq) ^ r16)) : rs.q[g];
+        qf[n][g] = CODES ? tw_q_like_codes(y) : tw_as_bf16(y);
+      }
+    float l2[NB][4];                             // lse in powers of 2; infinite (weights of 0) where there is no row, or none with a weight
+    int pos[NB][4];
     const float mine = r0 - 16 * block + (MANY ? lane & 31 : r16) < rows && __builtin_fabsf(rs.lse) < __builtin_inff() ? rs.lse * kLog2e : __builtin_inff();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {                // (four loads of the rows' own lse took 9 of 55 us of two prompts' last 64 tokens)
-      l2[i] = __int_as_float(__builtin_amdgcn_ds_bpermute((16 * block + 4 * jq + i) * 4, __float_as_int(mine)));
-      pos[i] = ctx + ((r0 + 4 * jq + i) >> a.lgG);
-    }
-    tw_v4f less[4];                              // -128 Q_g of the lane's rows: a product with a constant
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {              // (four loads of the rows' own lse took 9 of 55 us of two prompts' last 64 tokens)
+        l2[n][i] = __int_as_float(__builtin_amdgcn_ds_bpermute((16 * (block + n) + 4 * jq + i) * 4, __float_as_int(mine)));
+        pos[n][i] = ctx + ((r0 + 16 * n + 4 * jq + i) >> a.lgG);
+      }
+    tw_v4f s[NB][PT];
     if constexpr (CODES) {
+      tw_v4f less[4];                            // -128 Q_g of the lane's rows: a product with a constant
       tw_bf16x8 c;
 #pragma unroll
       for (int i = 0; i < 8; ++i) c[i] = (__bf16)-128.f;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) less[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], c, tw_v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-    }
-    tw_v4f s[PT];
-    if constexpr (CODES) {
+      for (int g = 0; g < 4; ++g) less[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[0][g], c, tw_v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
       for (int p = 0; p < PT; ++p) {
         tw_bf16x8 kf[4];
@@ -154,45 +157,61 @@ __global__ __launch_bounds__(256, 2) void attention_mass_kernel(MassArgs a) {
         const uint32_t w[4] = {x.m[p].x, x.m[p].y, x.m[p].z, x.m[p].w};
         tw_v4f t[4];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) t[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], kf[g], less[g], 0, 0, 0);
-        s[p] = tw_v4f{0.f, 0.f, 0.f, 0.f};
+        for (int g = 0; g < 4; ++g) t[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[0][g], kf[g], less[g], 0, 0, 0);
+        tw_v4f& sum = s[0][p];
+        sum = tw_v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const float z = tw_half_hi(w[g]) * (-1.f / 128.f);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[p][i] = __builtin_fmaf(z, less[g][i], s[p][i]);
+          for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(z, less[g][i], sum[i]);
         }
 #pragma unroll
         for (int g = 0; g < 4; ++g)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[p][i] = __builtin_fmaf(tw_half_lo(w[g]), t[g][i], s[p][i]);
+          for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(tw_half_lo(w[g]), t[g][i], sum[i]);
       }
     } else {                                     // (no product follows the one that it adds to)
-      tw_v4f u[PT];
+      constexpr bool APART = PT == 1;
+      tw_v4f u[NB];
 #pragma unroll
-      for (int p = 0; p < PT; ++p) s[p] = u[p] = tw_v4f{0.f, 0.f, 0.f, 0.f};
+      for (int n = 0; n < NB; ++n) {
+        u[n] = tw_v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
+        for (int p = 0; p < PT; ++p) s[n][p] = tw_v4f{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        if (NB > 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int p = 0; p < PT; ++p) {
           const tw_bf16x8 k = tw_as_bf16(x.k[p][g]);
-          if (PT == 1 && (g & 1)) u[p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], k, u[p], 0, 0, 0);
-          else s[p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[g], k, s[p], 0, 0, 0);
+#pragma unroll
+          for (int n = 0; n < NB; ++n) {
+            if (APART && (g & 1)) u[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[n][g], k, u[n], 0, 0, 0);
+            else s[n][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[n][g], k, s[n][p], 0, 0, 0);
+          }
         }
-      if (PT == 1) s[0] += u[0];
+      }
+      if (APART)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) s[n][0] += u[n];
     }
     auto weigh = [&](auto masked) {
 #pragma unroll
       for (int p = 0; p < PT; ++p) {
         const int t = t0 + 16 * p + r16;
-        float w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          // (the maximum makes 0 of what is no number: a row that sees such a token has an lse that says so)
-          w[i] = fmaxf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i], kScaleLog2, -l2[i])), 0.f);
-          if constexpr (decltype(masked)::value) w[i] = (t <= pos[i]) & ((t > pos[i] - a.window) | (t < a.sinks)) ? w[i] : 0.f;
+        for (int n = 0; n < NB; ++n) {
+          float w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            // (the maximum makes 0 of what is no number: a row that sees such a token has an lse that says so)
+            w[i] = fmaxf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][p][i], kScaleLog2, -l2[n][i])), 0.f);
+            if constexpr (decltype(masked)::value) w[i] = (t <= pos[n][i]) & ((t > pos[n][i] - a.window) | (t < a.sinks)) ? w[i] : 0.f;
+          }
+          acc[p] += (w[0] + w[1]) + (w[2] + w[3]);
         }
-        acc[p] += (w[0] + w[1]) + (w[2] + w[3]);
       }
     };
     if (all) weigh(std::false_type{});           // (a branch of its own: asked at every score it would be one per score)
@@ -213,12 +232,12 @@ __global__ __launch_bounds__(256, 2) void attention_mass_kernel(MassArgs a) {
           arrived();
           if (r0 + 32 < to) y1 = ask(mine1, h, r0 + 32);
           add(x, held, y0, mine0, 0, r0);
-          if (r0 + 16 < to) add(x, held, y0, mine0, 1, r0 + 16);
+          if (NB == 1 && r0 + 16 < to) add(x, held, y0, mine0, 1, r0 + 16);
           if (r0 + 32 >= to) break;
           arrived();
           if (r0 + 64 < to) y0 = ask(mine0, h, r0 + 64);
           add(x, held, y1, mine1, 0, r0 + 32);
-          if (r0 + 48 < to) add(x, held, y1, mine1, 1, r0 + 48);
+          if (NB == 1 && r0 + 48 < to) add(x, held, y1, mine1, 1, r0 + 48);
         }
         arrived();                               // (the last rows have been read before the next head's are asked for)
       }
@@ -532,16 +551,16 @@ void keep_chunks(const TwDims& d, int* chunks, int* blocks) {
 // Pages to a workgroup: few where that leaves CUs without one, more for the loads (and, with many rows, the queries) that they share.  us with 1 / 2 / 4 /
 // 8 pages, 32 heads over 8, by all sequences' pages:
 //                     256                    512                     1024                   2002                   4096 or 16384
-//   1 token    bf16   6.2  6.6  8.2 13.3     7.9  7.3 10.8 17.3      12.2 11.6 11.5 17.9    21.5 19.8 19.9 19.3    154  142  139  138
-//   1 token    codes  6.4  6.2  6.5  8.4     6.1  6.4  6.3  8.3       6.6  6.2  6.4  8.5     9.9  8.3  8.7  9.7    62.9 47.6 41.8 44.8
-//   64 tokens  bf16  15.3 19.1 30.4 51.6    20.8 19.5 31.1 51.7      38.3 27.1 32.0 52.3    72.3 48.3 42.6 53.5    144  94.8 80.2 75.9
-//   64 tokens  codes 16.7 21.4 34.9  109    22.1 22.3 34.8  110      42.6 30.6 37.0  114    78.9 55.9 50.2  117    149  107  94.6 187
+//   1 token    bf16   6.0  6.8  8.1 13.3     7.8  7.5 10.8 17.4      12.2 11.3 11.5 18.0    21.6 20.0 19.9 19.5    155  143  140  139
+//   1 token    codes  6.3  6.4  6.4  8.6     6.3  6.5  6.6  8.7       6.4  6.7  6.5  8.7    10.2  8.8  8.8  9.8    62.7 47.8 41.3 45.0
+//   64 tokens  bf16  15.1 17.9 29.8 85.3    21.4 18.3 30.3 85.6      38.6 26.0 31.2 87.2    71.3 47.2 41.8 93.7    142  91.3 78.5 149
+//   64 tokens  codes 16.8 22.0 34.8  110    22.0 22.3 35.9  111      41.8 30.5 36.8  115    77.1 55.3 50.3  118    148  106  95.1 188
 template <bool CODES, bool MANY>
 void launch_mass(const MassArgs& a, int batch, hipStream_t s) {
   const long long pages = (long long)a.max_pages * batch, cus = tw_num_cus();
   auto grid = [&](int n) { return dim3((unsigned)((a.max_pages + n - 1) / n), (unsigned)batch); };
   const dim3 wg(256);
-  if (pages <= 2 * cus) TW_LAUNCH((attention_mass_kernel<CODES, 1, MANY>), grid(1), wg, 0, s, a);
+  if (pages <= cus * 3 / 2) TW_LAUNCH((attention_mass_kernel<CODES, 1, MANY>), grid(1), wg, 0, s, a);
   else if (pages <= 4 * cus) TW_LAUNCH((attention_mass_kernel<CODES, 2, MANY>), grid(2), wg, 0, s, a);
   else TW_LAUNCH((attention_mass_kernel<CODES, 4, MANY>), grid(4), wg, 0, s, a);
 }

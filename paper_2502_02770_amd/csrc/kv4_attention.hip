@@ -39,7 +39,7 @@ typedef int tw_v2i __attribute__((ext_vector_type(2)));
 
 constexpr int WAVES = 4;
 // of a wave's LDS: V's codes of 64 tokens, twice; and what is made of their (s, z)
-constexpr int BUF = 4096, MADE = 1024 + 2048 + 512, MADE_Z = 1024, MADE_S = 3072;
+constexpr int BUF = 4096, MADE_Z = 1024, MADE_S = MADE_Z + 2048, MADE = MADE_S + 512;
 constexpr float kLift = 11.f;                    // log2 of the weight of a row's maximum when m is set to it
 constexpr float kGrowth4 = 4.f;                  // how far (in powers of 2) scores may pass it before m follows: weights stay below 2^16
 

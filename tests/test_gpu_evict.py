@@ -165,6 +165,8 @@ def test_mass_of_several_over_many_pages(kind, hq, hkv, new, window, sinks):
     weigh(kind(lens, hq, hkv, seed=new), [min(new, n) - (b == 3) for b, n in enumerate(lens)], new, window, sinks, 0.5, seed=hq, gap=2)
     lens = [2993, 405, 3000]                     # (two pages to a workgroup)
     weigh(kind(lens, hq, hkv, seed=new), [new, new - 1, 1], new, window, sinks, 0.5, seed=hq)
+    lens = [1701, 333]                           # (one)
+    weigh(kind(lens, hq, hkv, seed=new), [new, new // 2], new, window, sinks, 0.5, seed=hq)
 
 
 @KIND

@@ -20,11 +20,11 @@
 // group to a lane, and are exchanged between the quarters (four permlane swaps; through LDS they cost as much); V's codes go to LDS without
 // passing registers, both (s, z) through them, transposed.  The next tile's loads are issued while a tile is computed.
 //
-// Measured: 8 sequences of 32768, one token, 4 heads a group (M = 16) 76 us for 336 MB, 4.4 TB/s: what is left is issue beside the memory
-// (vector 0.53, matrix 0.10 of the time).  64 sequences of 1000 to 32001, 7 tokens, 8 heads a group (two blocks of M = 32) 389 us for 855 MB:
-// issue, some 490 vector instructions (0.6 of the time) and 72 matrix ones (0.18) to a tile and wave, half of which make codes and (s, z) into
-// operands, and that twice; one block (4 tokens) 253 us, and 149 for every further one.  Operands from LDS asked for a step ahead: 389 -> 385 us
-// and spills.  One sequence of 4096 11.6 us: two launches of 9 and 4, whose trips to memory follow each other.
+// Measured: 8 sequences of 32768, one token, 4 heads a group (M = 16) 75 us for 336 MB, 4.5 TB/s: what is left is issue beside the memory
+// (vector 0.55, matrix 0.10 of the time).  64 sequences of 1000 to 32001, 7 tokens, 8 heads a group (two blocks of M = 32) 365 us for 856 MB:
+// issue, some 490 vector instructions (0.65 of the time) and 72 matrix ones (0.19) to a tile and wave, half of which make codes and (s, z) into
+// operands, and that twice; one block (4 tokens) 240 us, and 139 for every further one.  Operands from LDS asked for a step ahead: 389 -> 385 us
+// and spills.  One sequence of 4096 11.2 us: two launches of 8 and 4, whose trips to memory follow each other.
 #include "kv4_common.h"
 #include "new_tokens_plan.h"
 
@@ -217,26 +217,6 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, u
   const int u0 = SPLIT ? min(sp.tiles, __builtin_amdgcn_readfirstlane(it.from)) : 0, u1 = SPLIT ? min(sp.tiles, __builtin_amdgcn_readfirstlane(it.to)) : sp.tiles;
   const bool whole = !SPLIT || it.to - it.from == it.tiles;
 
-  int pos[RT];
-  tw_bf16x8 qf[RT][4], qz[RT];                   // qz: Q_g's parts; quarters 0 and 1 the first and second twice, 2 the third and the first, 3 none
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    pos[rt] = ctx + (row_of(rt) >> a.lgG);
-    const uint4* qp = a.q + qrow_of(rt) * 16 + jq;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const uint4 x = qp[4 * g];
-      float f[8], sum = 0.f;
-      tw_unpack8(x, f);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum += f[i];
-      qf[rt][g] = tw_q_like_codes(x);
-      const Parts q = parts_of(tw_quarters_sum(sum));
-      qz[rt][2 * g] = (__bf16)(jq == 0 ? q.x : jq == 1 ? q.y : jq == 2 ? q.z : 0.f);
-      qz[rt][2 * g + 1] = (__bf16)(jq == 0 ? q.x : jq == 1 ? q.y : jq == 2 ? q.x : 0.f);
-    }
-  }
-
   // ---- pages of 16 tiles at a time: lane k holds page k % 4 of the wave's tile base + k / 4
   const int32_t* table = a.page_table + (long long)b * a.max_pages;
   int mine = 0, base = u0;
@@ -277,6 +257,44 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, u
     km = a.k_meta[tok];
     vm = a.v_meta[tok];
   };
+
+  // Queries, page table and first tile are asked for before anything waits for the queries
+  int pos[RT];
+  uint4 qr[RT][4];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    pos[rt] = ctx + (row_of(rt) >> a.lgG);
+    const uint4* qp = a.q + qrow_of(rt) * 16 + jq;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) qr[rt][g] = qp[4 * g];
+  }
+  unsigned char *const mine0 = buf0 + wave * BUF, *const mine1 = buf1 + wave * BUF;
+  Slots x = {};
+  if (u0 < u1) {
+    refill(u0);
+    x = slots_of(u0);
+    issue_lds(mine0, x);
+    issue_regs(x);
+  }
+  const uint32_t take[3] = {0u - (uint32_t)(jq == 0), 0u - (uint32_t)(jq == 1), 0u - (uint32_t)(jq == 2)};      // (masks: choices would be branches)
+  tw_bf16x8 qf[RT][4], qz[RT];                   // qz: Q_g's parts; quarters 0 and 1 the first and second twice, 2 the third and the first, 3 none
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    uint32_t w[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float f[8], sum = 0.f;
+      tw_unpack8(qr[rt][g], f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += f[i];
+      qf[rt][g] = tw_q_like_codes(qr[rt][g]);
+      const Parts q = parts_of(tw_quarters_sum(sum));
+      union { __bf16 e[2]; uint32_t u; } xx, yy, zx;
+      xx.e[0] = xx.e[1] = zx.e[1] = (__bf16)q.x; yy.e[0] = yy.e[1] = (__bf16)q.y; zx.e[0] = (__bf16)q.z;
+      w[g] = (xx.u & take[0]) | (yy.u & take[1]) | (zx.u & take[2]);
+    }
+    qz[rt] = tw_as_bf16(make_uint4(w[0], w[1], w[2], w[3]));
+  }
 
   tw_v4f o[RT][8];
 #pragma unroll
@@ -426,11 +444,6 @@ __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, u
   };
 
   if (u0 < u1) {
-    unsigned char *const mine0 = buf0 + wave * BUF, *const mine1 = buf1 + wave * BUF;
-    refill(u0);
-    Slots x = slots_of(u0);
-    issue_lds(mine0, x);
-    issue_regs(x);
     for (int u = u0; u < u1; u += 2) {           // (a wave's buffers are its own: nothing to wait for but its own loads)
       // the older of two workgroups on a CU would be served first, and leave the other alone at the end: they take turns
       if ((blockIdx.x >= gridDim.x / 2) == ((u - u0) % 4 < 2)) __builtin_amdgcn_s_setprio(1);
@@ -527,7 +540,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(Kv4Args a) {
 // summed by one fma per score and group; what the zeros add, sum_g z_g Q_g, is two more products for all groups: z (11 bits) in two
 // bf16 parts, Q_g in three.
 //
-// Measured: 257 tokens of three sequences of 9001 under a window of 6001, 4 heads a group (1028 rows) 169 us, 0.45 PFLOP/s of the attention's
+// Measured: 257 tokens of three sequences of 9001 under a window of 6001, 4 heads a group (1028 rows) 171 us, 0.44 PFLOP/s of the attention's
 // own products: vector issue 0.46 of the time (an exponential, a maximum and five fmas to a score), matrix 0.23, waits at the barrier of a tile.
 struct Kv4WideArgs : Kv4Args {
   static constexpr int TILE_PAGES = 4, MIN_TILES = 2, PAD = 3;

@@ -78,9 +78,11 @@ template <int MODE, int M, class A>
 __device__ __forceinline__ Seq seq_of(const A& a, int b) {
   Seq s = {0, 0, 0, 0, 0};
   if (b >= a.batch) return s;
-  s.off = a.offsets ? a.offsets[b] : b * a.max_new;
-  s.n = seq_new(a, b);
-  s.len = seq_len(a, b);
+  // (what is not given is read from another list and not used: the loads are on their way together)
+  const int len = a.seq_lens[b], n = (a.n_new ? a.n_new : a.seq_lens)[b], off = (a.offsets ? a.offsets : a.seq_lens)[b];
+  s.off = a.offsets ? off : b * a.max_new;
+  s.n = a.n_new ? max(0, min(n, a.max_new)) : a.max_new;
+  s.len = max(0, min(len, a.max_pages * TW_PAGE));
   const int blocks = (s.n * a.G + M - 1) / M;
   s.lists = blocks * a.Hkv;
   s.tiles = blocks == 0 ? 0 : max(1, span_of<MODE>(a, s.len, s.len - min(s.n, M / a.G), s.len - 1).tiles);

@@ -540,7 +540,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(Kv4Args a) {
 // summed by one fma per score and group; what the zeros add, sum_g z_g Q_g, is two more products for all groups: z (11 bits) in two
 // bf16 parts, Q_g in three.
 //
-// Measured: 257 tokens of three sequences of 9001 under a window of 6001, 4 heads a group (1028 rows) 171 us, 0.44 PFLOP/s of the attention's
+// Measured: 257 tokens of three sequences of 9001 under a window of 6001, 4 heads a group (1028 rows) 168 us, 0.45 PFLOP/s of the attention's
 // own products: vector issue 0.46 of the time (an exponential, a maximum and five fmas to a score), matrix 0.23, waits at the barrier of a tile.
 struct Kv4WideArgs : Kv4Args {
   static constexpr int TILE_PAGES = 4, MIN_TILES = 2, PAD = 3;
@@ -565,19 +565,21 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Piece& i
   const bool whole = !SPLIT || it.to - it.from == it.tiles;
 
   tw_bf16x8 qf[8], qz[2];                        // qz: Q_g in parts, each for both parts of z; the third for the lower half's slots alone
-  {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) qf[k] = tw_as_bf16(a.q[qrow * 16 + 2 * k + half]);
+  auto sums_of_q = [&]() {
     float part[2][4];
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       float sum = 0.f;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const uint4 x = a.q[qrow * 16 + 4 * g + 2 * k + half];
+        union { tw_bf16x8 v; uint4 u; } x;
+        x.v = qf[2 * g + k];
         float f[8];
-        tw_unpack8(x, f);
+        tw_unpack8(x.u, f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += f[i];
-        qf[2 * g + k] = tw_as_bf16(x);
       }
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
       sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
@@ -589,7 +591,7 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Piece& i
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int i = 0; i < 8; ++i) qz[k][i] = (__bf16)part[k][i / 2];
-  }
+  };
 
   // ---- LDS.  Rows of 16 pieces of 16 bytes, stored in an order that depends on the row, as in new_tokens.hip: K's piece ^ row % 16, V's
   // piece ^ (4 (row % 4) + 2 (row / 4 % 2)).  This lane stages token lane / 4 of its wave's page, group lane % 4.
@@ -785,8 +787,9 @@ __device__ __forceinline__ void attend_wide(const Kv4WideArgs& a, const Piece& i
     };
     refill(u0);
     ask(0, u0);
-    ahead[1] = ahead[0];
+    ahead[1] = Codes{};                          // (what follows a last tile is made of something: of the tile's own codes, this would wait for them)
     ask(1, u0 + 1);
+    sums_of_q();
     unsigned held = pages[0];
     {
       const Staged sz = stage_meta(buf0, ahead[0], u0, held);

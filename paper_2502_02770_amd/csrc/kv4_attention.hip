@@ -863,7 +863,8 @@ template <int M, int LANES>
 __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4Args a) { join_shares<M, LANES>(a); }
 
 // ---------------------------------------------------------------- host side
-// Rows to a workgroup.  us with blocks of 32 / 64 (as 128, two waves to 32 rows) / 128 rows, of a KV head's rows:
+// Rows to a workgroup.  us with blocks of 32 / 64 (as 128, two waves to 32 rows) / 128 rows, of a KV head's rows (these and the next figures are of
+// before page table and first tile were asked for ahead of the queries: the cases at the head of the file are 2 to 6 % faster since):
 //   8 sequences of 8192, 8 heads a group   24: 37 / 57 / 72    64: 51 / 61 / 74    128: 92 / 105 / 81   256: 135 / 185 / 140   1024: 501 / 554 / 413
 //   one of 4096, 4 heads a group           24: 15.2 / 16.2 / 15.8                  128: 21.4 / 23.8 / 22.1                      512: 32.7 / 39.0 / 35.5
 //   16 of 2048, 4 heads a group            24: 28 / 36 / 42    64: 35 / 40 / 46    128: 42 / 62 / 52    256: 78 / 82 / 81       512: 147 / 152 / 113

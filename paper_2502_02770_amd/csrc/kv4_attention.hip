@@ -84,11 +84,19 @@ struct Shares {
     return t < x ? quotient(t, each + 1u) : more + quotient(t - x, each);
   }
 };
+// A sequence as it is shared out: every list counts as many tiles as any of them may have (those that it has not are passed over).
+template <int M, class A>
+__device__ __forceinline__ Seq shared_seq_of(const A& a, int b) {
+  Seq s = seq_of<MODE_WINDOW, M>(a, b);
+  const int block = M >> a.lgG;
+  if (s.lists) s.tiles = most_tiles(a, span_of<MODE_WINDOW>(a, s.len, s.len - min(s.n, block), s.len - 1), s.len, s.n, block);
+  return s;
+}
 template <int M, class A>
 __device__ __forceinline__ Shares shares_of(const A& a, int lane) {
   uint32_t total = 0, lists = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    const Seq q = seq_of<MODE_WINDOW, M>(a, b0 + lane);
+    const Seq q = shared_seq_of<M>(a, b0 + lane);
     total += (uint32_t)__builtin_amdgcn_readlane((int)tw_wave_scan_u32((uint32_t)q.lists * (uint32_t)q.tiles), 63);
     lists += (uint32_t)__builtin_amdgcn_readlane((int)tw_wave_scan_u32((uint32_t)q.lists), 63);
   }
@@ -103,7 +111,7 @@ __device__ __forceinline__ void piece_at(const A& a, int lane, uint32_t pad, boo
   uint32_t tiles = 0;
   bool found = false;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    Seq q = seq_of<MODE_WINDOW, M>(a, b0 + lane);
+    Seq q = shared_seq_of<M>(a, b0 + lane);
     q.tiles += (int)pad;
     const uint32_t mine = (uint32_t)q.lists * (uint32_t)q.tiles;
     const uint32_t te = tw_wave_scan_u32(mine);

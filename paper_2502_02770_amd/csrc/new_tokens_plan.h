@@ -5,10 +5,11 @@
 // max_new, window, sinks, rb_max, cus, and the constants
 //   TILE_PAGES    pages of a tile, the unit in which lists are cut (a power of 2)
 //   MIN_TILES     shortest chunk of a list
-//   STREAM_TILES  tiles of K and V from which on they pass by the last-level cache
+//   STREAM_TILES  (plan_chunk) tiles of K and V from which on they pass by the last-level cache
 #pragma once
 #include <algorithm>
 #include "tw_common.h"
+#include "new_tokens_span.h"
 
 namespace {
 
@@ -16,7 +17,6 @@ constexpr float kLn2n = 0.6931471805599453f;
 constexpr float kScaleLog2 = 0.08838834764831845f * 1.4426950408889634f;   // log2(e) / sqrt(128)
 constexpr float kLow = -3.4028234663852886e38f;  // running maximum before any visible token, the lowest number: exp2(-inf - kLow) = 0
 constexpr float kFar = 1073741824.f;             // from an |m| of 2^30 on, a row's scores are told apart by their own steps, 64 and more
-enum { MODE_TREE = 0, MODE_WINDOW = 1 };
 constexpr int PLAN_ROUNDS = 2;                   // items per resident workgroup at most, as planned
 constexpr long long COMBINE_FEW = 512;           // rows of a launch up to which a workgroup joins one row's parts
 
@@ -35,33 +35,6 @@ __device__ __forceinline__ int seq_new(const A& a, int b) {
   return a.n_new ? max(0, min(a.n_new[b], a.max_new)) : a.max_new;
 }
 
-// The pages that rows of tokens at positions p_lo .. p_hi see: `sink` pages from the start, then those from `first` on; four of
-// this list to a tile, so that a few sinks and a window that begins inside 64 tokens cost no tile of their own: five prompts of 882
-// tokens, a window of 51 and one sink 35.1 us with tiles at multiples of 64, 32.3 so.  Where few tiles are saved, working out the
-// places costs more than that: one token, a window of 1024 and 4 sinks 10.5 and 10.8 us.
-template <int TILE_PAGES>
-struct Span {
-  int sink, first, pages, tiles;
-  int both, behind, shift;                       // the tile with pages of both parts, the first one of the second; positions between the parts
-  __device__ __forceinline__ int page(int v) const { return v < sink ? v : first + (v - sink); }
-  __device__ __forceinline__ int start(int u) const { return u * TILE_PAGES * TW_PAGE + (u >= behind ? shift : 0); }   // position of tile u's first page
-};
-template <int MODE, class A>
-__device__ __forceinline__ Span<A::TILE_PAGES> span_of(const A& a, int len, int p_lo, int p_hi) {
-  constexpr int TP = A::TILE_PAGES;
-  Span<TP> s;
-  const int end = MODE == MODE_TREE ? len : min(len, p_hi + 1);
-  if (end <= 0) { s.sink = s.first = s.pages = s.tiles = s.behind = s.shift = 0; s.both = -1; return s; }
-  s.first = MODE == MODE_TREE ? 0 : max(0, p_lo - a.window + 1) / TW_PAGE;
-  s.sink = MODE == MODE_TREE ? 0 : min((int)(((unsigned)a.sinks + TW_PAGE - 1) / TW_PAGE), s.first);
-  s.pages = s.sink + (end - 1) / TW_PAGE - s.first + 1;
-  s.tiles = (s.pages + TP - 1) / TP;
-  s.behind = (s.sink + TP - 1) / TP;
-  s.both = s.sink & (TP - 1) && s.sink < s.first ? s.sink / TP : -1;
-  s.shift = (s.first - s.sink) * TW_PAGE;
-  return s;
-}
-
 // Which part of which list a workgroup takes.  A list is a (row block, KV head) of a sequence; a sequence's lists are cut
 // into the same number of chunks.
 struct Item {
@@ -70,7 +43,8 @@ struct Item {
   uint32_t items;                                // of the launch, where one wave's lanes hold all sequences (no need to look for a next one)
 };
 
-// A sequence: its new tokens, length and first row, its lists and the tiles of the longest of them.
+// A sequence: its new tokens, length and first row, its lists, and the tiles of one of its last tokens.  Under a window another list can
+// have one tile more (most_tiles), so that who cuts by this count takes a list's share of the tiles that it has.
 struct Seq {
   int n, len, off, lists, tiles;
 };

@@ -1,0 +1,71 @@
+"""Tiles that lists of attention under a window are planned with: no row block's list has more (the library's own arithmetic, built for the host)."""
+import os
+import subprocess
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2502_02770_amd", "csrc")
+
+PROGRAM = r"""
+#include <cstdio>
+#include <random>
+#define TW_PAGE 16
+#include "new_tokens_span.h"
+
+template <int TILE_PAGES_>
+struct Args {
+  static constexpr int TILE_PAGES = TILE_PAGES_;
+  int window, sinks;
+};
+
+static long long calls, beyond, loose, last_short;
+
+// rows of M to a block, G query heads to a KV head
+template <int TP, int M>
+void look(int len, int n, int G, int window, int sinks) {
+  const Args<TP> a = {window, sinks};
+  const int block = M / G, blocks = (n + block - 1) / block;
+  const auto last = span_of<MODE_WINDOW>(a, len, len - std::min(n, block), len - 1);
+  const int planned = most_tiles(a, last, len, n, block);
+  int longest = 0;
+  for (int j = 0; j < blocks; ++j) {
+    const int p_lo = len - n + j * block, p_hi = len - n + std::min(n, (j + 1) * block) - 1;
+    longest = std::max(longest, span_of<MODE_WINDOW>(a, len, p_lo, p_hi).tiles);
+  }
+  ++calls;
+  beyond += longest > planned;
+  loose += planned > std::max(1, longest) + 1;
+  last_short += longest > last.tiles;
+  // the host's bound of a list, by which it cuts and sizes
+  const long long pages = (sinks + 15ll) / 16 + ((long long)window + block + 14) / 16 + 1;
+  beyond += planned > (pages + TP - 1) / TP;
+}
+
+int main() {
+  std::mt19937 r(1);
+  auto up_to = [&](int x) { return (int)(r() % (unsigned)(x + 1)); };
+  for (int G = 1; G <= 8; G *= 2) {
+    // every length, count, window and sinks of a small range; and of ranges around whole tiles
+    for (int n = 1; n <= 40; n += 3)
+      for (int len = 0; len <= 700; len += 1 + up_to(5))
+        for (int window = 1; window <= 560; window += 1 + up_to(60))
+          for (int sinks = 0; sinks <= 70; sinks += 1 + up_to(40)) look<16, 32>(len, n, G, window, sinks), look<4, 128>(len, 8 * n, G, window, sinks), look<16, 16>(len, std::min(n, 16 / G), G, window, sinks);
+    for (int i = 0; i < 400000; ++i) {
+      const int len = up_to(20000), n = 1 + up_to(256 / G - 1), many = 256 / G + 1 + up_to(300);
+      const int window = i % 3 ? std::max(1, 64 * up_to(70) + up_to(24) - 12) : 1 + up_to(8000), sinks = i % 2 ? 0 : up_to(100);
+      look<16, 32>(len, n, G, window, sinks);
+      look<4, 128>(len, many, G, window, sinks);
+    }
+    look<16, 32>(1 << 28, 32, G, 1 << 30, 1 << 30);
+    look<4, 128>(1 << 28, 1 << 20, G, 1 << 30, 0);
+  }
+  std::printf("%lld %lld %lld %lld\n", calls, beyond, loose, last_short);
+}
+"""
+
+
+def test_no_list_has_more_tiles_than_planned(tmp_path):
+    (tmp_path / "plan.cpp").write_text(PROGRAM)
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I" + CSRC, str(tmp_path / "plan.cpp"), "-o", str(tmp_path / "plan")], check=True)
+    calls, beyond, loose, last_short = map(int, subprocess.run([str(tmp_path / "plan")], capture_output=True, text=True, check=True, timeout=100).stdout.split())
+    assert calls > 2_000_000 and beyond == 0
+    assert loose == 0                                              # nor is a list planned with more than a tile that it has not
+    assert last_short > 1000                                       # (by the last tokens' pages alone, these lists would have lost a tile)

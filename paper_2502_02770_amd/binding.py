@@ -139,6 +139,18 @@ def _v_pools(kv, vq_pool, vq_meta):
     return vq_pool.data_ptr(), vq_meta.data_ptr()
 
 
+def _lists(kv, *lists):
+    assert all(t is None or t.numel() >= kv.batch for t in lists), "a number per sequence"
+
+
+def _new_tokens(kv, q, n_new, new_offsets, max_new, lse, out=None):
+    """Sizes of lists and rows on new tokens, as far as they are known on the host: what one lacks would be read or written behind it."""
+    _lists(kv, n_new, new_offsets)
+    assert (out is None or out.numel() >= q.numel()) and (lse is None or lse.numel() * 128 >= q.numel()), "a row of out, a number of lse per row of q"
+    rows = 0 if n_new is not None else max_new if new_offsets is not None else kv.batch * max_new
+    assert q.numel() >= rows * kv.num_q_heads * 128, "a row per new token"
+
+
 def _count(x):
     """A number for an i32 argument, where ctypes would drop the bits beyond."""
     x = int(x)
@@ -315,6 +327,7 @@ def twilight_tokens_compact(kv, keep_idx, keep_count, keep_stride, dst_start, ds
 def twilight_kv4_append(kv, vq_pool, vq_meta, k_new, v_new, start_pos, n_new, new_offsets, max_new):
     codes, meta = _v_pools(kv, vq_pool, vq_meta)
     assert k_new.shape == v_new.shape, "a row of V per row of K"
+    _lists(kv, start_pos, n_new, new_offsets)
     _check(lib().twilight_kv4_append(ctypes.byref(kv), codes, meta, _rows(k_new), _rows(v_new), _ints(start_pos), _ints(n_new),
                                      _ints(new_offsets), _count(max_new), _stream_of(k_new)))
 
@@ -322,12 +335,14 @@ def twilight_kv4_append(kv, vq_pool, vq_meta, k_new, v_new, start_pos, n_new, ne
 def twilight_kv4_read(kv, vq_pool, vq_meta, start_pos, n_rows, row_offsets, max_rows, k_out, v_out):
     codes, meta = _v_pools(kv, vq_pool, vq_meta)
     assert k_out.shape == v_out.shape, "a row of V per row of K"
+    _lists(kv, start_pos, n_rows, row_offsets)
     _check(lib().twilight_kv4_read(ctypes.byref(kv), codes, meta, _ints(start_pos), _ints(n_rows), _ints(row_offsets), _count(max_rows),
                                    _rows(k_out), _rows(v_out), _stream_of(k_out)))
 
 
 def twilight_kv4_attention(kv, vq_pool, vq_meta, q, n_new, new_offsets, max_new, window, num_sinks, out, lse, ws):
     codes, meta = _v_pools(kv, vq_pool, vq_meta)
+    _new_tokens(kv, q, n_new, new_offsets, max_new, lse, out)
     _check(lib().twilight_kv4_attention(ctypes.byref(kv), codes, meta, _rows(q), _ints(n_new), _ints(new_offsets), _count(max_new),
                                         _limit(window), _limit(num_sinks), _rows(out), _sums(lse), _ptr(ws), ws.numel() * ws.element_size(),
                                         _stream_of(q)))
@@ -335,6 +350,7 @@ def twilight_kv4_attention(kv, vq_pool, vq_meta, q, n_new, new_offsets, max_new,
 
 def twilight_attention_mass(kv, q, lse, n_new, new_offsets, max_new, window, num_sinks, decay, mass_in, mass_out):
     assert mass_in.numel() == mass_out.numel() == kv.batch * kv.max_pages_per_seq * 16, "a weight per position of the page table"
+    _new_tokens(kv, q, n_new, new_offsets, max_new, lse)
     _check(lib().twilight_attention_mass(ctypes.byref(kv), _rows(q), _sums(lse), _ints(n_new), _ints(new_offsets), _count(max_new),
                                          _limit(window), _limit(num_sinks), float(decay), _sums(mass_in), _sums(mass_out), _stream_of(q)))
 

@@ -84,19 +84,11 @@ struct Shares {
     return t < x ? quotient(t, each + 1u) : more + quotient(t - x, each);
   }
 };
-// A sequence as it is shared out: every list counts as many tiles as any of them may have (those that it has not are passed over).
-template <int M, class A>
-__device__ __forceinline__ Seq shared_seq_of(const A& a, int b) {
-  Seq s = seq_of<MODE_WINDOW, M>(a, b);
-  const int block = M >> a.lgG;
-  if (s.lists) s.tiles = most_tiles(a, span_of<MODE_WINDOW>(a, s.len, s.len - min(s.n, block), s.len - 1), s.len, s.n, block);
-  return s;
-}
 template <int M, class A>
 __device__ __forceinline__ Shares shares_of(const A& a, int lane) {
   uint32_t total = 0, lists = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    const Seq q = shared_seq_of<M>(a, b0 + lane);
+    const Seq q = seq_of<MODE_WINDOW, M, true>(a, b0 + lane);
     total += (uint32_t)__builtin_amdgcn_readlane((int)tw_wave_scan_u32((uint32_t)q.lists * (uint32_t)q.tiles), 63);
     lists += (uint32_t)__builtin_amdgcn_readlane((int)tw_wave_scan_u32((uint32_t)q.lists), 63);
   }
@@ -111,7 +103,7 @@ __device__ __forceinline__ void piece_at(const A& a, int lane, uint32_t pad, boo
   uint32_t tiles = 0;
   bool found = false;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    Seq q = shared_seq_of<M>(a, b0 + lane);
+    Seq q = seq_of<MODE_WINDOW, M, true>(a, b0 + lane);
     q.tiles += (int)pad;
     const uint32_t mine = (uint32_t)q.lists * (uint32_t)q.tiles;
     const uint32_t te = tw_wave_scan_u32(mine);
@@ -897,8 +889,7 @@ bool cut_lists4(bool counted, int blocks, long long lists, long long longest) {
 template <int M, class A, class Whole, class Cut>
 int launch_kv4(const A& a, Whole whole, Cut cut, hipStream_t s) {
   const long long lists = (long long)a.rb_max * a.batch * a.Hkv, rows = (long long)a.max_new * a.Hq;
-  const long long pages = std::min<long long>(a.max_pages, ((long long)a.sinks + TW_PAGE - 1) / TW_PAGE + ((long long)a.window + M / a.G + TW_PAGE - 2) / TW_PAGE + 1);
-  const long long longest = (pages + A::TILE_PAGES - 1) / A::TILE_PAGES;        // tiles that a list can have
+  const long long longest = std::min((a.max_pages + A::TILE_PAGES - 1) / A::TILE_PAGES, window_tiles(a, M / a.G));      // tiles that a list can have
   tw_prof_before(TW_K_KV4_ATTENTION, s);
   if (!cut_lists4<A>(a.n_new != nullptr, a.rb_max, lists, longest) || rows >= (1ll << 26) || lists * (longest + A::PAD) >= (1ll << 32)) {
     TW_LAUNCH(whole, dim3((unsigned)lists), dim3(256), 0, s, a);

@@ -43,12 +43,12 @@ struct Item {
   uint32_t items;                                // of the launch, where one wave's lanes hold all sequences (no need to look for a next one)
 };
 
-// A sequence: its new tokens, length and first row, its lists, and the tiles of one of its last tokens.  Under a window another list can
-// have one tile more (most_tiles), so that who cuts by this count takes a list's share of the tiles that it has.
+// A sequence: its new tokens, length and first row, its lists, and the tiles that its last tokens see.  Under a window another list can have one
+// more: who cuts by this count takes a share of the tiles that the list has.  With MOST, no list has more (longest_span).
 struct Seq {
   int n, len, off, lists, tiles;
 };
-template <int MODE, int M, class A>
+template <int MODE, int M, bool MOST = false, class A>
 __device__ __forceinline__ Seq seq_of(const A& a, int b) {
   Seq s = {0, 0, 0, 0, 0};
   if (b >= a.batch) return s;
@@ -59,7 +59,9 @@ __device__ __forceinline__ Seq seq_of(const A& a, int b) {
   s.len = max(0, min(len, a.max_pages * TW_PAGE));
   const int blocks = (s.n * a.G + M - 1) / M;
   s.lists = blocks * a.Hkv;
-  s.tiles = blocks == 0 ? 0 : max(1, span_of<MODE>(a, s.len, s.len - min(s.n, M / a.G), s.len - 1).tiles);
+  const int block = M / a.G;
+  const auto sp = MOST ? longest_span(a, s.len, s.n, block) : span_of<MODE>(a, s.len, s.len - min(s.n, block), s.len - 1);
+  s.tiles = blocks == 0 ? 0 : max(1, sp.tiles);
   return s;
 }
 

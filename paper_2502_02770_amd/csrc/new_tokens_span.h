@@ -41,15 +41,19 @@ TW_BOTH Span<A::TILE_PAGES> span_of(const A& a, int len, int p_lo, int p_hi) {
   return s;
 }
 
-// Tiles that no list of a sequence passes under a window: n of its len tokens are new, `block` of them to a row block, and p are the pages that
-// its last min(n, block) tokens see.  Another block's first token may lie elsewhere in its page; block + window - 1 positions touch at most
-// (block + window + 13) / 16 + 1 pages, wherever they begin, sinks are no more than those of the last block, and no list has more pages than
-// the sequence.
-template <class A, class S>
-TW_BOTH int most_tiles(const A& a, const S& p, int len, int n, int block) {
-  int pages = p.pages;
-  if (n > block) pages = min((len + TW_PAGE - 1) / TW_PAGE, p.sink + (block + a.window + TW_PAGE - 3) / TW_PAGE + 1);
-  return max(1, (pages + A::TILE_PAGES - 1) / A::TILE_PAGES);
+// Pages at least as many as any of a sequence's lists has: n of its len tokens are new, `block` of them to a row block.  Under a window a block
+// may lie differently against the pages than the last `block` tokens and see one more than they do.  So those and the 15 tokens before them
+// are counted: of them, a block that lies among them sees a part; one that begins earlier has no more sinks, and its block + window - 1
+// positions touch no more pages than 15 positions more do, wherever these begin.
+template <class A>
+TW_BOTH Span<A::TILE_PAGES> longest_span(const A& a, int len, int n, int block) {
+  return span_of<MODE_WINDOW>(a, len, len - min(n, block + TW_PAGE - 1), len - 1);
+}
+// Its tiles at most, however long the sequence is.
+template <class A>
+TW_BOTH int window_tiles(const A& a, int block) {
+  const long long pages = ((long long)a.sinks + TW_PAGE - 1) / TW_PAGE + (block + a.window + 2 * TW_PAGE - 4) / TW_PAGE + 1;
+  return (int)((pages + A::TILE_PAGES - 1) / A::TILE_PAGES);
 }
 
 }  // namespace

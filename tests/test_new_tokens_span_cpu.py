@@ -21,10 +21,11 @@ static long long calls, beyond, loose, last_short;
 // rows of M to a block, G query heads to a KV head
 template <int TP, int M>
 void look(int len, int n, int G, int window, int sinks) {
+  const int block = M / G;
   const Args<TP> a = {window, sinks};
-  const int block = M / G, blocks = (n + block - 1) / block;
+  const int blocks = (n + block - 1) / block;
   const auto last = span_of<MODE_WINDOW>(a, len, len - std::min(n, block), len - 1);
-  const int planned = most_tiles(a, last, len, n, block);
+  const int planned = std::max(1, longest_span(a, len, n, block).tiles);
   int longest = 0;
   for (int j = 0; j < blocks; ++j) {
     const int p_lo = len - n + j * block, p_hi = len - n + std::min(n, (j + 1) * block) - 1;
@@ -32,11 +33,9 @@ void look(int len, int n, int G, int window, int sinks) {
   }
   ++calls;
   beyond += longest > planned;
-  loose += planned > std::max(1, longest) + 1;
+  loose += planned > std::max(1, longest) + 3;
   last_short += longest > last.tiles;
-  // the host's bound of a list, by which it cuts and sizes
-  const long long pages = (sinks + 15ll) / 16 + ((long long)window + block + 14) / 16 + 1;
-  beyond += planned > (pages + TP - 1) / TP;
+  beyond += planned > window_tiles(a, block);           // the host's bound of a list, by which it cuts and sizes
 }
 
 int main() {
@@ -67,5 +66,7 @@ def test_no_list_has_more_tiles_than_planned(tmp_path):
     subprocess.run(["g++", "-O2", "-std=c++17", "-I" + CSRC, str(tmp_path / "plan.cpp"), "-o", str(tmp_path / "plan")], check=True)
     calls, beyond, loose, last_short = map(int, subprocess.run([str(tmp_path / "plan")], capture_output=True, text=True, check=True, timeout=100).stdout.split())
     assert calls > 2_000_000 and beyond == 0
-    assert loose == 0                                              # nor is a list planned with more than a tile that it has not
+    # nor are lists planned with many tiles that none of them has: where the only block that sees sinks apart from its window is a short last one,
+    # the span counts up to 128 tokens more than that block has, 15 ahead of them, and a page for where it begins: 10 pages, 3 tiles of 4
+    assert loose == 0
     assert last_short > 1000                                       # (by the last tokens' pages alone, these lists would have lost a tile)

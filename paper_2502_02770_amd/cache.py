@@ -244,15 +244,21 @@ class TokenMass:
                                self._spare, self.ws)
         return self.keep_idx, self.keep_count
 
-    def evict(self, budget, num_sinks=0, num_recent=0):
+    def evict(self, budget, num_sinks=0, num_recent=0, others=()):
         """Every sequence cut down to its budget: the tokens worth keeping moved together in place, seq_lens set to their number, and
         their mass kept for the steps to come.  The pages behind are the caller's to give back (PagePool.free), and no page may be
-        shared with another sequence.  -> keep_count"""
-        idx, count = self.keep(budget, num_sinks, num_recent)
-        self.cache.compact(idx, count, self._start)
-        self.cache.seq_lens.copy_(count)
-        self.mass.copy_(self._spare)               # (not exchanged: a captured graph names them)
-        return count
+        shared with another sequence.  Layers whose caches have one seq_lens tensor between them (as those of one PagedKV.over) are cut
+        down by one call, each by its own mass: `others` are the TokenMass of the rest of them.  In a call of its own, a later layer would
+        find the lengths set already, and choose from the first of its tokens alone.  -> keep_count"""
+        layers = (self, *others)
+        assert all(m.cache.batch == self.cache.batch for m in layers), "layers of one batch"
+        for m in layers:
+            m.keep(budget, num_sinks, num_recent)
+            m.cache.compact(m.keep_idx, m.keep_count, m._start)
+        for m in layers:
+            m.cache.seq_lens.copy_(m.keep_count)
+            m.mass.copy_(m._spare)                 # (not exchanged: a captured graph names them)
+        return self.keep_count
 
 
 def tree_mask_of_parents(parents):

@@ -65,7 +65,8 @@ struct Kv4Args {
 };
 
 // How a launch that cuts its lists shares them out: all lists' tiles in one row, sequence by sequence, of which every workgroup takes as
-// many as the others - the end of one list, whole ones, the start of another.  Chunks of a length and one after the other to the
+// many as the others - the end of one list, whole ones, the start of another.  A list counts as many tiles as any of its sequence's may have
+// (longest_span): what it has not is an empty part, what were not counted would not be read.  Chunks of a length and one after the other to the
 // workgroups, as the bf16 kernel has them, left the chip idle for 38 % of the time where 64 sequences of 1000 to 32001 tokens make as
 // many lists as there are workgroups.  Of a list that is cut, a workgroup w has a part with its first tile (place 2 w of the workspace) or
 // one with its last (2 w + 1).
@@ -205,6 +206,7 @@ template <int RT, bool SPLIT>
 __device__ __forceinline__ void attend_item(const Kv4Args& a, const Piece& it, unsigned char (&buf0)[WAVES * BUF], unsigned char (&buf1)[WAVES * BUF],
                                             unsigned char (&made)[WAVES * MADE], int lane, int wave) {
   constexpr int M = 16 * RT;
+  static_assert(RT <= 2, "64 rows to a wave are right, but 434 registers spilled: 64 ragged sequences 1274 us for 362");
   const int r16 = lane & 15, jq = lane >> 4;
   const int b = __builtin_amdgcn_readfirstlane(it.b), rb = __builtin_amdgcn_readfirstlane(it.rb), h = __builtin_amdgcn_readfirstlane(it.h);
   const int n = __builtin_amdgcn_readfirstlane(it.n), len = __builtin_amdgcn_readfirstlane(it.len), off = __builtin_amdgcn_readfirstlane(it.off);

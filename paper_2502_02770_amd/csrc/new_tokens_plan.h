@@ -6,6 +6,7 @@
 //   TILE_PAGES    pages of a tile, the unit in which lists are cut (a power of 2)
 //   MIN_TILES     shortest chunk of a list
 //   STREAM_TILES  (plan_chunk) tiles of K and V from which on they pass by the last-level cache
+//   PAD           (lists shared out evenly) what a piece of a list costs beside its tiles, in tiles
 #pragma once
 #include <algorithm>
 #include "tw_common.h"
